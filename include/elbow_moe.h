@@ -272,6 +272,100 @@ int elb_moe_forward_packed(const void *x, const void *W_router, const void *W_ga
                            int32_t *ids_out, float *w_out, int32_t *counts_out, void *stream);
 
 /*
+ * The dense gated feed-forward block: the bias-free SwiGLU MLP of elb_moe_experts as a block that
+ * every token goes through (a shared expert beside the routed ones, whose output is then the
+ * residual here; or a dense layer of its own).
+ *   y_t = [residual_t +] W_down h_t,  h_t = silu(W_gate x_t) * (W_up x_t)
+ *   x         [T, d]   dtype
+ *   W_gate_up [2m, d]  dtype   rows [0, m) = W_gate, rows [m, 2m) = W_up
+ *   W_down    [d, m]   dtype
+ *   residual  [T, d]   dtype   optional (NULL: none)
+ *   y         [T, d]   dtype   output; may alias residual, must not alias another input
+ *   gate_up   [T, 2m]  float   optional output (NULL: not written): W_gate x_t and W_up x_t, for
+ *                              elb_ffn_backward
+ *   workspace          at least elb_ffn_workspace_bytes(T, d, m, dtype) bytes
+ * Sums are fp32; for ELB_BF16 h is rounded to bf16 before the second product and y at the end.
+ * Requirements: d and m positive multiples of 16, at most 2^20; T < 2^31.
+ */
+size_t elb_ffn_workspace_bytes(int64_t T, int32_t d, int32_t m, int32_t dtype);
+int elb_ffn_forward(const void *x, const void *W_gate_up, const void *W_down,
+                    const void *residual, int64_t T, int32_t d, int32_t m, int32_t dtype, void *y,
+                    float *gate_up, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Gradients of the block from dy, the gradient of y (that of residual is dy itself):
+ *   dh = dy W_down,  s = 1 / (1 + e^-g),  dg = dh u s (1 + g (1 - s)),  du = dh g s,
+ *   dx = dg W_gate + du W_up,  dW_gate = dg^T x,  dW_up = du^T x,  dW_down = dy^T h
+ *   dy         [T, d]   dtype   gradient of y
+ *   x, W_gate_up, W_down        as given to elb_ffn_forward
+ *   gate_up    [T, 2m]  float   as written by elb_ffn_forward (g and u)
+ *   dx         [T, d]   dtype   output, or NULL: not computed
+ *   dW_gate_up [2m, d]  dtype   output, or NULL: not computed
+ *   dW_down    [d, m]   dtype   output, or NULL: not computed
+ *   workspace           at least elb_ffn_backward_workspace_bytes(T, d, m, dtype) bytes
+ * Outputs are overwritten, not added to, and must not alias an input.  Sums are fp32 in a fixed
+ * order (the same bits on every call); for ELB_BF16 dg, du and h are rounded to bf16 before the
+ * products they enter.  With T = 0 the weight gradients are sums over no token: they are
+ * written as zeros (the one case in which T = 0 enqueues work).  Requirements as elb_ffn_forward.
+ */
+size_t elb_ffn_backward_workspace_bytes(int64_t T, int32_t d, int32_t m, int32_t dtype);
+int elb_ffn_backward(const void *dy, const void *x, const void *W_gate_up, const void *W_down,
+                     const float *gate_up, int64_t T, int32_t d, int32_t m, int32_t dtype,
+                     void *dx, void *dW_gate_up, void *dW_down, void *workspace,
+                     size_t workspace_bytes, void *stream);
+
+/*
+ * Rows to 8-bit integers with one scale per row (symmetric):
+ *   scale_t = fl32(max_i |x_ti| / 127),  q_ti = the whole number nearest to x_ti / scale_t (of the
+ *   exact quotient; ties to even), at most 127 in magnitude; 0 where scale_t = 0
+ *   x     [T, d]  dtype
+ *   q     [T, d]  int8 output
+ *   scale [T]     float output: q_ti scale_t stands for x_ti
+ * Quantises tokens for elb_gemm_i8, and weights too (rows = output channels).
+ * Requirements: d a positive multiple of 16, at most 2^20; T < 2^31.
+ */
+int elb_quantize_rows(const void *x, int64_t T, int32_t d, int32_t dtype, int8_t *q, float *scale,
+                      void *stream);
+
+/*
+ * Product of 8-bit integers with a scale per token and per output channel:
+ *   y_tn = [residual_tn +] (sum_i q_ti W_ni) scale_t W_scale_n
+ *   q        [T, k]  int8, scale [T] float     tokens (elb_quantize_rows)
+ *   W        [n, k]  int8, W_scale [n] float   weights
+ *   residual [T, n]  dtype   optional (NULL: none)
+ *   y        [T, n]  dtype   output; may alias residual
+ * The sum is exact (int32); its scaling and the residual are fp32, rounded to dtype once.
+ * Requirements: n and k positive multiples of 16, n at most 2^20, k at most 131071; T < 2^31.
+ */
+int elb_gemm_i8(const int8_t *q, const float *scale, const int8_t *W, const float *W_scale,
+                const void *residual, int64_t T, int32_t n, int32_t k, int32_t dtype, void *y,
+                void *stream);
+
+/*
+ * elb_quantize_rows and elb_gemm_i8 in one call, for activations x [T, k] of dtype.
+ *   workspace  at least elb_linear_i8_workspace_bytes(T, k) bytes; y must not alias x
+ */
+size_t elb_linear_i8_workspace_bytes(int64_t T, int32_t k);
+int elb_linear_i8(const void *x, const int8_t *W, const float *W_scale, const void *residual,
+                  int64_t T, int32_t n, int32_t k, int32_t dtype, void *y, void *workspace,
+                  size_t workspace_bytes, void *stream);
+
+/*
+ * The dense gated feed-forward block with 8-bit weights (and activations quantised on the way):
+ * x is quantised by rows, g and u are its 8-bit products with W_gate_up, h = silu(g) u is kept in
+ * fp32 and quantised by rows, and y = [residual +] the 8-bit product of that with W_down.
+ *   x [T, d], residual [T, d] (or NULL), y [T, d]   dtype; y may alias residual, not x
+ *   W_gate_up [2m, d] int8, gate_up_scale [2m] float; W_down [d, m] int8, down_scale [d] float
+ *   workspace  at least elb_ffn_i8_workspace_bytes(T, d, m) bytes
+ * Requirements: d and m positive multiples of 16, at most 131071; T < 2^31.
+ */
+size_t elb_ffn_i8_workspace_bytes(int64_t T, int32_t d, int32_t m);
+int elb_ffn_forward_i8(const void *x, const int8_t *W_gate_up, const float *gate_up_scale,
+                       const int8_t *W_down, const float *down_scale, const void *residual,
+                       int64_t T, int32_t d, int32_t m, int32_t dtype, void *y, void *workspace,
+                       size_t workspace_bytes, void *stream);
+
+/*
  * Calibration of the matrix-core roofline (a measurement aid, not part of the layer): a
  * kernel of `blocks` blocks of 4 waves, each wave issuing iters x 8 back-to-back
  * v_mfma_f32_32x32x16_bf16 instructions (32 x 32 x 16 multiply-adds each) on register

@@ -73,6 +73,16 @@ def lib():
                                    C.c_int),
         "elb_moe_forward_noalloc": ([P, P, P, P, P, I64, I32, I32, I32, I32,
                                      C.POINTER(RouteParams), P, P, P, P, P, P, P], C.c_int),
+        "elb_ffn_workspace_bytes": ([I64, I32, I32, I32], SZ),
+        "elb_ffn_forward": ([P, P, P, P, I64, I32, I32, I32, P, P, P, SZ, P], C.c_int),
+        "elb_ffn_backward_workspace_bytes": ([I64, I32, I32, I32], SZ),
+        "elb_ffn_backward": ([P, P, P, P, P, I64, I32, I32, I32, P, P, P, P, SZ, P], C.c_int),
+        "elb_quantize_rows": ([P, I64, I32, I32, P, P, P], C.c_int),
+        "elb_gemm_i8": ([P, P, P, P, P, I64, I32, I32, I32, P, P], C.c_int),
+        "elb_linear_i8_workspace_bytes": ([I64, I32], SZ),
+        "elb_linear_i8": ([P, P, P, P, I64, I32, I32, I32, P, P, SZ, P], C.c_int),
+        "elb_ffn_i8_workspace_bytes": ([I64, I32, I32], SZ),
+        "elb_ffn_forward_i8": ([P, P, P, P, P, P, I64, I32, I32, I32, P, P, SZ, P], C.c_int),
         "elb_calibrate_mfma_bf16": ([I32, I32, P, P], C.c_int64),
         "elb_calibrate_read_stream": ([P, I64, I32, P, P], C.c_int),
         "elb_profile_enable": ([C.c_int], C.c_int),
@@ -402,6 +412,161 @@ def elb_moe_forward_prepared(x, W_router, W_gate_up, W_down, K: int = 8, eps: fl
             _check(name, rc)
         return keep
     return call, y
+
+
+def _want(name: str, t: Optional[torch.Tensor], shape, dtype: torch.dtype):
+    """t: None, or a contiguous tensor of that shape and type on the current device."""
+    if t is None:
+        return
+    if not t.is_cuda or t.get_device() != torch._C._cuda_getDevice():
+        raise ValueError("%s must be on the current GPU" % name)
+    if t.dtype != dtype:
+        raise TypeError("%s must be %s, not %s" % (name, dtype, t.dtype))
+    if t.shape != shape:
+        raise ValueError("%s must have shape %s, not %s" % (name, tuple(shape), tuple(t.shape)))
+    if not t.is_contiguous():
+        raise ValueError("%s must be contiguous" % name)
+
+
+def _matrix(name: str, t: torch.Tensor):
+    if t.dim() != 2:
+        raise ValueError("%s must have two dimensions, not %d" % (name, t.dim()))
+    return t.shape
+
+
+def _ffn_dims(x, W_gate_up, W_down):
+    """(T, d, m, dtype code) of the dense block; its operands checked."""
+    T, d = _matrix("x", x)
+    m = _matrix("W_down", W_down)[1]
+    dt = _dtype_code(x)
+    _want("x", x, (T, d), x.dtype)
+    _want("W_gate_up", W_gate_up, (2 * m, d), x.dtype)
+    _want("W_down", W_down, (d, m), x.dtype)
+    return T, d, m, dt
+
+
+@functools.lru_cache(maxsize=256)
+def elb_ffn_workspace_bytes(T: int, d: int, m: int, dtype: int) -> int:
+    return int(lib().elb_ffn_workspace_bytes(T, d, m, dtype))
+
+
+def elb_ffn_forward(x, W_gate_up, W_down, residual=None, out=None, keep: bool = False):
+    """The dense gated feed-forward block.  -> y, or with keep=True (y, gate_up): gate_up
+    [T, 2m] float32 is what elb_ffn_backward needs of the forward pass."""
+    T, d, m, dt = _ffn_dims(x, W_gate_up, W_down)
+    _want("residual", residual, (T, d), x.dtype)
+    _want("out", out, (T, d), x.dtype)
+    y = torch.empty_like(x) if out is None else out
+    gate_up = torch.empty((T, 2 * m), dtype=torch.float32, device=x.device) if keep else None
+    stream = _stream()
+    ws = workspace(elb_ffn_workspace_bytes(T, d, m, dt), x.device, stream)
+    _check("elb_ffn_forward", lib().elb_ffn_forward(
+        _ptr(x), _ptr(W_gate_up), _ptr(W_down), _ptr(residual), T, d, m, dt, _ptr(y),
+        _ptr(gate_up), _ptr(ws), ws.numel(), stream))
+    return (y, gate_up) if keep else y
+
+
+@functools.lru_cache(maxsize=256)
+def elb_ffn_backward_workspace_bytes(T: int, d: int, m: int, dtype: int) -> int:
+    return int(lib().elb_ffn_backward_workspace_bytes(T, d, m, dtype))
+
+
+def elb_ffn_backward(dy, x, W_gate_up, W_down, gate_up, need=(True, True, True)):
+    """-> (dx, dW_gate_up, dW_down), None where need is false; gate_up from
+    elb_ffn_forward(..., keep=True)."""
+    T, d, m, dt = _ffn_dims(x, W_gate_up, W_down)
+    _want("dy", dy, (T, d), x.dtype)
+    _want("gate_up", gate_up, (T, 2 * m), torch.float32)
+    dx, dWgu, dWd = (torch.empty_like(t) if n else None
+                     for t, n in zip((x, W_gate_up, W_down), need))
+    stream = _stream()
+    ws = workspace(elb_ffn_backward_workspace_bytes(T, d, m, dt), x.device, stream)
+    _check("elb_ffn_backward", lib().elb_ffn_backward(
+        _ptr(dy), _ptr(x), _ptr(W_gate_up), _ptr(W_down), _ptr(gate_up), T, d, m, dt, _ptr(dx),
+        _ptr(dWgu), _ptr(dWd), _ptr(ws), ws.numel(), stream))
+    return dx, dWgu, dWd
+
+
+def elb_quantize_rows(x: torch.Tensor):
+    """-> (q [T, d] int8, scale [T] float32): q scale[:, None] stands for x"""
+    T, d = _matrix("x", x)
+    dt = _dtype_code(x)
+    _want("x", x, (T, d), x.dtype)
+    q = torch.empty((T, d), dtype=torch.int8, device=x.device)
+    scale = torch.empty(T, dtype=torch.float32, device=x.device)
+    _check("elb_quantize_rows", lib().elb_quantize_rows(_ptr(x), T, d, dt, _ptr(q), _ptr(scale),
+                                                        _stream()))
+    return q, scale
+
+
+def elb_gemm_i8(q, scale, W, W_scale, dtype: torch.dtype = torch.bfloat16, residual=None,
+                out=None) -> torch.Tensor:
+    """y [T, n] of dtype (bfloat16 or float32) from q [T, k] int8 and W [n, k] int8."""
+    T, k = _matrix("q", q)
+    n = _matrix("W", W)[0]
+    _want("q", q, (T, k), torch.int8)
+    _want("scale", scale, (T,), torch.float32)
+    _want("W", W, (n, k), torch.int8)
+    _want("W_scale", W_scale, (n,), torch.float32)
+    _want("residual", residual, (T, n), dtype)
+    _want("out", out, (T, n), dtype)
+    y = torch.empty((T, n), dtype=dtype, device=q.device) if out is None else out
+    _check("elb_gemm_i8", lib().elb_gemm_i8(
+        _ptr(q), _ptr(scale), _ptr(W), _ptr(W_scale), _ptr(residual), T, n, k, _dtype_code(y),
+        _ptr(y), _stream()))
+    return y
+
+
+@functools.lru_cache(maxsize=256)
+def elb_linear_i8_workspace_bytes(T: int, k: int) -> int:
+    return int(lib().elb_linear_i8_workspace_bytes(T, k))
+
+
+def elb_linear_i8(x, W, W_scale, residual=None, out=None) -> torch.Tensor:
+    """y [T, n] = x [T, k], quantised by rows on the way, times W [n, k] int8."""
+    T, k = _matrix("x", x)
+    n = _matrix("W", W)[0]
+    dt = _dtype_code(x)
+    _want("x", x, (T, k), x.dtype)
+    _want("W", W, (n, k), torch.int8)
+    _want("W_scale", W_scale, (n,), torch.float32)
+    _want("residual", residual, (T, n), x.dtype)
+    _want("out", out, (T, n), x.dtype)
+    y = torch.empty((T, n), dtype=x.dtype, device=x.device) if out is None else out
+    stream = _stream()
+    ws = workspace(elb_linear_i8_workspace_bytes(T, k), x.device, stream)
+    _check("elb_linear_i8", lib().elb_linear_i8(
+        _ptr(x), _ptr(W), _ptr(W_scale), _ptr(residual), T, n, k, dt, _ptr(y), _ptr(ws),
+        ws.numel(), stream))
+    return y
+
+
+@functools.lru_cache(maxsize=256)
+def elb_ffn_i8_workspace_bytes(T: int, d: int, m: int) -> int:
+    return int(lib().elb_ffn_i8_workspace_bytes(T, d, m))
+
+
+def elb_ffn_forward_i8(x, W_gate_up, gate_up_scale, W_down, down_scale, residual=None,
+                       out=None) -> torch.Tensor:
+    """The dense gated feed-forward block with int8 weights (elb_quantize_rows of the float
+    ones): W_gate_up [2m, d], gate_up_scale [2m], W_down [d, m], down_scale [d]."""
+    T, d = _matrix("x", x)
+    m = _matrix("W_down", W_down)[1]
+    dt = _dtype_code(x)
+    _want("x", x, (T, d), x.dtype)
+    _want("W_gate_up", W_gate_up, (2 * m, d), torch.int8)
+    _want("gate_up_scale", gate_up_scale, (2 * m,), torch.float32)
+    _want("W_down", W_down, (d, m), torch.int8)
+    _want("down_scale", down_scale, (d,), torch.float32)
+    _want("residual", residual, (T, d), x.dtype)
+    _want("out", out, (T, d), x.dtype)
+    y = torch.empty_like(x) if out is None else out
+    stream = _stream()
+    ws = workspace(elb_ffn_i8_workspace_bytes(T, d, m), x.device, stream)
+    _check("elb_ffn_forward_i8", lib().elb_ffn_forward_i8(
+        _ptr(x), _ptr(W_gate_up), _ptr(gate_up_scale), _ptr(W_down), _ptr(down_scale),
+        _ptr(residual), T, d, m, dt, _ptr(y), _ptr(ws), ws.numel(), stream))
+    return y
 
 
 def elb_calibrate_read_stream(buf: torch.Tensor, blocks: int, out: torch.Tensor) -> None:

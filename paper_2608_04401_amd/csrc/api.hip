@@ -135,6 +135,61 @@ int check_expert_dims(int64_t T, int d, int N, int m, int K, int dtype) {
     return ELB_OK;
 }
 
+// ---- the dense block and the 8-bit products ----
+// Largest row length: a tile's byte offsets (256 rows of 2 m bf16, 32 or 64 of 2 m fp32) stay
+// below 2^31.
+constexpr int kMaxDim = 1 << 20;
+// Largest contraction of an int8 product: 2^14 k must stay below 2^31.
+constexpr int kMaxI8K = 131071;
+
+int check_dense(int64_t T, int a, const char* an, int b, const char* bn) {
+    if (T < 0) return fail(ELB_ERR_INVALID_ARG, "T = %lld < 0", (long long)T);
+    if (a < 1 || b < 1 || a % 16 || b % 16)
+        return fail(ELB_ERR_INVALID_ARG, "%s = %d and %s = %d must be positive multiples of 16", an,
+                    a, bn, b);
+    if (a > kMaxDim || b > kMaxDim)
+        return fail(ELB_ERR_UNSUPPORTED, "%s = %d or %s = %d exceeds %d", an, a, bn, b, kMaxDim);
+    if (T >= (int64_t)1 << 31)
+        return fail(ELB_ERR_UNSUPPORTED, "T = %lld exceeds 2^31 - 1", (long long)T);
+    return ELB_OK;
+}
+
+int check_workspace(const void* workspace, size_t bytes, size_t need) {
+    if (!workspace || bytes < need)
+        return fail(ELB_ERR_WORKSPACE, "workspace of %zu bytes, need %zu", bytes, need);
+    if ((uintptr_t)workspace % kAlign)
+        return fail(ELB_ERR_WORKSPACE, "workspace not %zu-byte aligned", kAlign);
+    return ELB_OK;
+}
+
+int check_i8_k(int k, const char* name) {
+    if (k > kMaxI8K)
+        return fail(ELB_ERR_UNSUPPORTED, "%s = %d: int32 sums hold a contraction of %d", name, k,
+                    kMaxI8K);
+    return ELB_OK;
+}
+
+// sub-buffers of the int8 block's workspace
+struct I8Layout {
+    size_t xq, xs, h, hq, hs, total;
+};
+I8Layout i8_layout(int64_t T, int d, int m) {
+    I8Layout L{};
+    size_t o = 0;
+    auto take = [&](size_t bytes) {
+        const size_t at = o;
+        o += align_up(bytes);
+        return at;
+    };
+    L.xq = take((size_t)T * d);
+    L.xs = take((size_t)T * 4);
+    L.h = take((size_t)T * m * 4);
+    L.hq = take((size_t)T * m);
+    L.hs = take((size_t)T * 4);
+    L.total = o;
+    return L;
+}
+
 // ---- the static scratch of the allocation-free entry point ----
 // One array per GPU the library runs on (a __device__ variable lives in each device's copy of
 // the code object).  In host code `scratch` is only a stand-in symbol: its device address is
@@ -592,6 +647,140 @@ int elb_pack_expert_weights(const void* W_gate_up, const void* W_down, int32_t N
     return hip_status(launch_pack_experts(W_gate_up, W_down, N, d, m, packed,
                                           (hipStream_t)stream),
                       "pack_experts");
+}
+
+size_t elb_ffn_workspace_bytes(int64_t T, int32_t d, int32_t m, int32_t dtype) {
+    if (T < 0 || d < 1 || m < 1 || (dtype != ELB_F32 && dtype != ELB_BF16)) return 0;
+    return align_up((size_t)T * m * esize(dtype));
+}
+
+int elb_ffn_forward(const void* x, const void* W_gate_up, const void* W_down,
+                    const void* residual, int64_t T, int32_t d, int32_t m, int32_t dtype, void* y,
+                    float* gate_up, void* workspace, size_t workspace_bytes, void* stream) {
+    g_err.clear();
+    if (int rc = check_dtype(dtype)) return rc;
+    if (int rc = check_dense(T, d, "d", m, "m")) return rc;
+    if (T == 0) return ELB_OK;
+    if (!x || !W_gate_up || !W_down || !y)
+        return fail(ELB_ERR_INVALID_ARG, "NULL tensor pointer");
+    if (int rc = check_workspace(workspace, workspace_bytes,
+                                 elb_ffn_workspace_bytes(T, d, m, dtype)))
+        return rc;
+    return hip_status(launch_ffn_forward(x, W_gate_up, W_down, residual, T, d, m, dtype, workspace,
+                                         gate_up, y, (hipStream_t)stream),
+                      "ffn_forward");
+}
+
+size_t elb_ffn_backward_workspace_bytes(int64_t T, int32_t d, int32_t m, int32_t dtype) {
+    if (T < 0 || d < 1 || m < 1 || (dtype != ELB_F32 && dtype != ELB_BF16)) return 0;
+    return align_up((size_t)T * m * esize(dtype)) + align_up((size_t)T * 2 * m * esize(dtype));
+}
+
+int elb_ffn_backward(const void* dy, const void* x, const void* W_gate_up, const void* W_down,
+                     const float* gate_up, int64_t T, int32_t d, int32_t m, int32_t dtype,
+                     void* dx, void* dW_gate_up, void* dW_down, void* workspace,
+                     size_t workspace_bytes, void* stream) {
+    g_err.clear();
+    if (int rc = check_dtype(dtype)) return rc;
+    if (int rc = check_dense(T, d, "d", m, "m")) return rc;
+    if (!dx && !dW_gate_up && !dW_down) return ELB_OK;  // nothing asked for
+    if (T > 0 && (!dy || !x || !W_gate_up || !W_down || !gate_up))
+        return fail(ELB_ERR_INVALID_ARG, "NULL tensor pointer");
+    if (T > 0)
+        if (int rc = check_workspace(workspace, workspace_bytes,
+                                     elb_ffn_backward_workspace_bytes(T, d, m, dtype)))
+            return rc;
+    char* const ws = (char*)workspace;
+    return hip_status(launch_ffn_backward(dy, x, W_gate_up, W_down, gate_up, T, d, m, dtype,
+                                          T > 0 ? ws + align_up((size_t)T * m * esize(dtype)) : ws,
+                                          ws, dx, dW_gate_up, dW_down, (hipStream_t)stream),
+                      "ffn_backward");
+}
+
+int elb_quantize_rows(const void* x, int64_t T, int32_t d, int32_t dtype, int8_t* q, float* scale,
+                      void* stream) {
+    g_err.clear();
+    if (int rc = check_dtype(dtype)) return rc;
+    if (int rc = check_dense(T, d, "d", 16, "d")) return rc;
+    if (T == 0) return ELB_OK;
+    if (!x || !q || !scale) return fail(ELB_ERR_INVALID_ARG, "NULL tensor pointer");
+    return hip_status(launch_quantize_rows(x, T, d, dtype, q, scale, (hipStream_t)stream),
+                      "quantize_rows");
+}
+
+int elb_gemm_i8(const int8_t* q, const float* scale, const int8_t* W, const float* W_scale,
+                const void* residual, int64_t T, int32_t n, int32_t k, int32_t dtype, void* y,
+                void* stream) {
+    g_err.clear();
+    if (int rc = check_dtype(dtype)) return rc;
+    if (int rc = check_dense(T, n, "n", k, "k")) return rc;
+    if (int rc = check_i8_k(k, "k")) return rc;
+    if (T == 0) return ELB_OK;
+    if (!q || !scale || !W || !W_scale || !y)
+        return fail(ELB_ERR_INVALID_ARG, "NULL tensor pointer");
+    return hip_status(launch_gemm_i8(q, scale, W, W_scale, residual, T, n, k, dtype, y,
+                                     (hipStream_t)stream),
+                      "gemm_i8");
+}
+
+size_t elb_linear_i8_workspace_bytes(int64_t T, int32_t k) {
+    if (T < 0 || k < 1) return 0;
+    return align_up((size_t)T * k) + align_up((size_t)T * 4);
+}
+
+int elb_linear_i8(const void* x, const int8_t* W, const float* W_scale, const void* residual,
+                  int64_t T, int32_t n, int32_t k, int32_t dtype, void* y, void* workspace,
+                  size_t workspace_bytes, void* stream) {
+    g_err.clear();
+    if (int rc = check_dtype(dtype)) return rc;
+    if (int rc = check_dense(T, n, "n", k, "k")) return rc;
+    if (int rc = check_i8_k(k, "k")) return rc;
+    if (T == 0) return ELB_OK;
+    if (!x || !W || !W_scale || !y) return fail(ELB_ERR_INVALID_ARG, "NULL tensor pointer");
+    if (int rc = check_workspace(workspace, workspace_bytes, elb_linear_i8_workspace_bytes(T, k)))
+        return rc;
+    int8_t* const q = (int8_t*)workspace;
+    float* const scale = (float*)((char*)workspace + align_up((size_t)T * k));
+    hipStream_t s = (hipStream_t)stream;
+    if (int rc = hip_status(launch_quantize_rows(x, T, k, dtype, q, scale, s), "quantize_rows"))
+        return rc;
+    return hip_status(launch_gemm_i8(q, scale, W, W_scale, residual, T, n, k, dtype, y, s),
+                      "gemm_i8");
+}
+
+size_t elb_ffn_i8_workspace_bytes(int64_t T, int32_t d, int32_t m) {
+    if (T < 0 || d < 1 || m < 1) return 0;
+    return i8_layout(T, d, m).total;
+}
+
+int elb_ffn_forward_i8(const void* x, const int8_t* W_gate_up, const float* gate_up_scale,
+                       const int8_t* W_down, const float* down_scale, const void* residual,
+                       int64_t T, int32_t d, int32_t m, int32_t dtype, void* y, void* workspace,
+                       size_t workspace_bytes, void* stream) {
+    g_err.clear();
+    if (int rc = check_dtype(dtype)) return rc;
+    if (int rc = check_dense(T, d, "d", m, "m")) return rc;
+    if (int rc = check_i8_k(d, "d")) return rc;
+    if (int rc = check_i8_k(m, "m")) return rc;
+    if (T == 0) return ELB_OK;
+    if (!x || !W_gate_up || !gate_up_scale || !W_down || !down_scale || !y)
+        return fail(ELB_ERR_INVALID_ARG, "NULL tensor pointer");
+    const I8Layout L = i8_layout(T, d, m);
+    if (int rc = check_workspace(workspace, workspace_bytes, L.total)) return rc;
+    char* const ws = (char*)workspace;
+    int8_t *const xq = (int8_t*)(ws + L.xq), *const hq = (int8_t*)(ws + L.hq);
+    float *const xs = (float*)(ws + L.xs), *const hs = (float*)(ws + L.hs);
+    float* const h = (float*)(ws + L.h);
+    hipStream_t s = (hipStream_t)stream;
+    if (int rc = hip_status(launch_quantize_rows(x, T, d, dtype, xq, xs, s), "quantize_rows"))
+        return rc;
+    if (int rc = hip_status(launch_gate_up_i8(xq, xs, W_gate_up, gate_up_scale, T, d, m, h, s),
+                            "gate_up_i8"))
+        return rc;
+    if (int rc = hip_status(launch_quantize_rows(h, T, m, ELB_F32, hq, hs, s), "quantize_rows"))
+        return rc;
+    return hip_status(launch_gemm_i8(hq, hs, W_down, down_scale, residual, T, d, m, dtype, y, s),
+                      "gemm_i8");
 }
 
 int64_t elb_calibrate_mfma_bf16(int32_t blocks, int32_t iters, float* out, void* stream) {

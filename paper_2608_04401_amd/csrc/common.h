@@ -187,6 +187,23 @@ hipError_t launch_combine(const void* Y, const int* k, const int* inv, const flo
                           const void* residual, int64_t T, int d, int K, int dtype, void* y,
                           hipStream_t s);
 
+// the dense gated feed-forward block (ffn.hip).  Scratch: h [T, m], dgu [T, 2m], both dtype
+hipError_t launch_ffn_forward(const void* x, const void* Wgu, const void* Wd, const void* res,
+                              int64_t T, int d, int m, int dtype, void* h, float* gate_up, void* y,
+                              hipStream_t s);
+hipError_t launch_ffn_backward(const void* dy, const void* x, const void* Wgu, const void* Wd,
+                               const float* gate_up, int64_t T, int d, int m, int dtype, void* dgu,
+                               void* h, void* dx, void* dWgu, void* dWd, hipStream_t s);
+// 8-bit products (ffn_i8.hip)
+hipError_t launch_quantize_rows(const void* x, int64_t rows, int d, int dtype, int8_t* q,
+                                float* scale, hipStream_t s);
+hipError_t launch_gemm_i8(const int8_t* a, const float* a_scale, const int8_t* w,
+                          const float* w_scale, const void* res, int64_t T, int n, int k,
+                          int dtype, void* y, hipStream_t s);
+hipError_t launch_gate_up_i8(const int8_t* a, const float* a_scale, const int8_t* w,
+                             const float* w_scale, int64_t T, int d, int m, float* h,
+                             hipStream_t s);
+
 // calibration: back-to-back bf16 MFMAs, blocks x 4 waves x iters x 8 of them; out [blocks * 4]
 hipError_t launch_calibrate_mfma(int blocks, int iters, float* out, hipStream_t s);
 hipError_t launch_calibrate_read(const void* buf, int64_t bytes, int blocks, uint32_t* out,

@@ -1,0 +1,679 @@
+// Tile products of the dense operators (the gated feed-forward block and the 8-bit products):
+// global -> LDS copies with bounds, MFMA operand reads, and the two block forms built of them.
+//
+//   C[r, c] = sum_k A(r, k) B(c, k),  r < rows, c < cols, k < K
+//
+// An operand is stored either with its contraction contiguous (KC: x W^T has both so) or with
+// the contraction as its row index (KR: the gradients' products dy W and dy^T x read their
+// operands "down" the rows).  A k-tile is 128 bytes of contraction per operand row: 64 bf16, 128
+// int8 or 32 fp32; a unit is one operand's share of a k-tile, TR rows x 128 bytes whatever the
+// layout (KR: 128 / SZ contraction rows of TR elements).
+#pragma once
+
+#include "common.h"
+#include "tilegrid.h"
+
+namespace elb {
+
+namespace {
+
+enum Lay { KC = 0, KR = 1 };
+
+// ---- element types: the MFMA shape and its operand and accumulator registers ----
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
+typedef int32_t i32x4_t __attribute__((ext_vector_type(4)));
+typedef int32_t i32x16_t __attribute__((ext_vector_type(16)));
+typedef short s16x4_t __attribute__((ext_vector_type(4)));
+
+template <class E, int MF>
+struct Mma;
+struct Bf16 {
+    static constexpr int SZ = 2;
+    typedef bf16x8_t frag;
+    typedef float acc1;
+};
+struct I8 {
+    static constexpr int SZ = 1;
+    typedef i32x4_t frag;
+    typedef int32_t acc1;
+};
+struct F32 {
+    static constexpr int SZ = 4;
+    typedef f32x4_t frag;
+    typedef float acc1;
+};
+// The first MFMA operand is the one whose rows become output COLUMNS: a lane then holds four
+// consecutive output columns per group of four accumulators.
+template <>
+struct Mma<Bf16, 32> {
+    typedef f32x16_t acc;
+    static __device__ __forceinline__ acc mma(bf16x8_t b, bf16x8_t a, acc c) {
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(b, a, c, 0, 0, 0);
+    }
+};
+template <>
+struct Mma<Bf16, 16> {
+    typedef f32x4_t acc;
+    static __device__ __forceinline__ acc mma(bf16x8_t b, bf16x8_t a, acc c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(b, a, c, 0, 0, 0);
+    }
+};
+template <>
+struct Mma<I8, 32> {
+    typedef i32x16_t acc;
+    static __device__ __forceinline__ acc mma(i32x4_t b, i32x4_t a, acc c) {
+        return __builtin_amdgcn_mfma_i32_32x32x32_i8(b, a, c, 0, 0, 0);
+    }
+};
+template <>
+struct Mma<I8, 16> {
+    typedef i32x4_t acc;
+    static __device__ __forceinline__ acc mma(i32x4_t b, i32x4_t a, acc c) {
+        return __builtin_amdgcn_mfma_i32_16x16x64_i8(b, a, c, 0, 0, 0);
+    }
+};
+template <>
+struct Mma<F32, 16> {  // four k of one row per operand: a permutation both operands share
+    typedef f32x4_t acc;
+    static __device__ __forceinline__ acc mma(f32x4_t b, f32x4_t a, acc c) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            c = __builtin_amdgcn_mfma_f32_16x16x4f32(b[q], a[q], c, 0, 0, 0);
+        return c;
+    }
+};
+
+// ---- LDS layouts ----
+// KC unit: TR rows of 128 bytes, the eight 16-byte chunks of row r XOR-swizzled so that 16
+// consecutive rows' reads of one logical chunk hit distinct banks.
+__device__ __forceinline__ int kc_swz(int r, int c) {
+    return c ^ (((r >> 1) ^ ((r & 1) << 2)) & 7);
+}
+// KR unit: 128 / SZ rows of TR elements.  bf16: granules of 16 columns (32 bytes), swizzled so
+// that the four rows x two granules that 32 lanes of a transposing read touch lie in distinct
+// banks; fp32: granules of 16 columns (64 bytes), four rows apart in distinct banks.  Returns
+// the XOR on the 16-byte chunk of row k.
+template <int TR, int SZ>
+__device__ __forceinline__ int kr_swz(int k) {
+    if (SZ == 4) return TR >= 64 ? ((k >> 2) & 3) << 2 : 0;
+    return TR >= 128 ? (k & 3) << 2 : TR == 64 ? ((k >> 1) & 1) << 2 : 0;
+}
+
+// ---- global -> LDS copies ----
+// 16 bytes from global memory at any byte boundary
+typedef uint32_t u32x4_byte_t __attribute__((ext_vector_type(4), aligned(1)));
+
+constexpr uint32_t kOutOfBounds = 0x7fffff00u;  // past every buffer: spans stay below 2^31 - 512
+
+// One wave's share of a unit's copies: NW waves copy TR rows, 1 KB per instruction
+// (buffer_load_dwordx4 ... lds).  The buffer's bound is set per unit, so lanes past the operand's
+// last row, column or contraction index write zeros to LDS: tails need no clamping, and nothing
+// they read is out of the tensor.  PAIR (KC): rows [0, TR / 2) and [TR / 2, TR) of the unit come
+// from two places (gate rows and the matching up rows).  DMA = false: ordinary loads, for tensors
+// off a 16-byte boundary.
+template <int LAY, int TR, int SZ, int NW, bool PAIR, bool DMA>
+struct Copier {
+    static constexpr int N = TR / 8 / NW;  // copy instructions per unit
+    static constexpr int NB = (PAIR && NW == 1) ? 2 : 1;
+    static constexpr int KT = 128 / SZ;    // contraction depth of a k-tile
+    static constexpr int P = TR * SZ;      // KR: bytes of a contraction row in LDS
+    static_assert(TR % (8 * NW) == 0 && !(PAIR && LAY == KR) && !(PAIR && NW == 1 && N % 2), "");
+    const char* base[NB];
+    uint32_t off[N];
+    int kchunk[2];   // KC: byte offset in the k-tile of copies i and i + 1 (i even)
+    int64_t ld;      // bytes between the operand's rows
+    int64_t span;    // KC: bytes of the tile's rows; KR: bytes of the tile's columns
+    int64_t klen;    // KC: bytes of contraction; KR: contraction rows
+
+    // p0: the tile's first row (KC) or column (KR) at contraction 0; p1: with PAIR its first row
+    // of the second half; ext: valid rows or columns from there on (of each half with PAIR)
+    __device__ __forceinline__ void init(const void* p0, const void* p1, int64_t ld_, int ext,
+                                         int64_t K, int lane, int w) {
+        ld = ld_;
+        constexpr int HR = PAIR ? TR / 2 : TR;
+        if (LAY == KC) {
+            span = (int64_t)(ext < HR ? ext : HR) * ld_;
+            klen = K * SZ;
+        } else {
+            span = (int64_t)(ext < TR ? ext : TR) * SZ;
+            klen = K;
+        }
+        base[0] = (const char*)(PAIR && NB == 1 && w >= NW / 2 ? p1 : p0);
+        if (NB == 2) base[NB - 1] = (const char*)p1;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            if (LAY == KC) {
+                int r = 8 * (w * N + i) + (lane >> 3);
+                if (i < 2) kchunk[i] = kc_swz(r, lane & 7) * 16;
+                if (PAIR) r = r >= HR ? r - HR : r;
+                off[i] = (uint32_t)(r * ld_) + kchunk[i & 1];
+            } else {
+                constexpr int LPR = P / 16;  // lanes per contraction row
+                const int k = (w * N + i) * (64 / LPR) + lane / LPR;
+                off[i] = (uint32_t)(k * ld_) + ((lane % LPR) ^ kr_swz<TR, SZ>(k)) * 16;
+            }
+        }
+        if (LAY == KC && N == 1) kchunk[1] = kchunk[0];
+    }
+    // copy k-tile t into the unit at LDS byte address lds (ldsp: the same as a pointer); past
+    // tend nothing is read (zeros are written), so that the count of copies in flight is the same
+    __device__ __forceinline__ void issue(int t, int tend, uint32_t lds, char* ldsp, int lane,
+                                          int w) const {
+        int64_t at, rec;
+        if (LAY == KC) {
+            at = (int64_t)t * 128;
+            rec = span - at;
+        } else {
+            at = (int64_t)t * KT * ld;
+            const int64_t left = klen - (int64_t)t * KT;
+            rec = ((left < KT ? left : KT) - 1) * ld + span;
+            if (left <= 0) rec = 0;
+        }
+        if (t >= tend || rec < 0) rec = 0;
+        const bool tail = LAY == KC && klen - at < 128;
+        u32x4_t rs[NB];
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            const uint64_t p = (uint64_t)(base[b] + at);
+            rs[b] = u32x4_t{(uint32_t)p, (uint32_t)(p >> 32) & 0xffffu, (uint32_t)rec,
+                            0x00027000u};
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int b = (NB == 2 && i >= N / 2) ? NB - 1 : 0;
+            uint32_t vo = off[i];
+            if (tail) vo = kchunk[i & 1] < klen - at ? vo : kOutOfBounds;
+            if constexpr (DMA) {
+                const uint32_t la = lds + (uint32_t)(w * N + i) * 1024;
+                // inline assembly: the compiler cannot tell which unit a copy writes, and would
+                // wait for every copy in flight before each LDS read; waits are explicit
+                asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                             :: "s"(la), "v"(vo), "s"(rs[b]) : "memory", "m0");
+            } else {
+                u32x4_t v = {0, 0, 0, 0};
+                if ((int64_t)vo < rec)
+                    v = *reinterpret_cast<const u32x4_byte_t*>(base[b] + at + vo);
+                *reinterpret_cast<u32x4_t*>(ldsp + (w * N + i) * 1024 + lane * 16) = v;
+            }
+        }
+    }
+};
+
+// ---- MFMA operand reads ----
+// Fragment i of MF rows at row0 + MF i of the unit, k-step ks (of 64 / MF) of the k-tile.
+template <class E, int MF, int LAY, int TR>
+struct Reader {
+    static constexpr int P = TR * E::SZ;
+    static constexpr int KS = MF / 8;   // k-steps of a k-tile
+    static constexpr int KD = 512 / MF; // KR, bf16: contraction rows of a k-step
+    int at, ofs[LAY == KC ? KS : 1];
+    int row;
+    __device__ __forceinline__ void init(int row0, int lane) {
+        const int l = lane & (MF - 1), g = lane / MF;
+        row = row0;
+        if (LAY == KC) {
+            at = (row0 + l) * 128;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks)
+                ofs[ks] = kc_swz(l, ks * (64 / MF) + g) * 16;
+        } else if (E::SZ == 2) {
+            // transposing reads: the 16 lanes of a group bring four contraction rows of 16
+            // columns, and lane j of the group receives column j
+            const int p = lane & 15;
+            const int kh = MF == 32 ? (lane >> 5) : (lane >> 4);
+            at = (8 * kh + (p >> 2)) * P + (p & 3) * 8;
+            ofs[0] = (kr_swz<TR, 2>(p >> 2) * 16) ^ (MF == 32 ? ((lane >> 4) & 1) * 32 : 0);
+        } else {
+            at = 4 * g * P + l * 4;
+            ofs[0] = kr_swz<TR, 4>(4 * g) * 16;
+        }
+    }
+    __device__ __forceinline__ typename E::frag load(const char* unit, int i, int ks) const {
+        typename E::frag v;
+        if constexpr (LAY == KC) {
+            v = *reinterpret_cast<const typename E::frag*>(unit + at + i * MF * 128 + ofs[ks]);
+        } else if constexpr (E::SZ == 2) {
+            const int c = ((row + MF * i) * 2) ^ ofs[0];
+            const char* const q = unit + at + c + ks * KD * P;
+            typedef __attribute__((address_space(3))) s16x4_t lds_s16x4;
+            const s16x4_t a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)q);
+            const s16x4_t b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(q + 4 * P));
+            v = __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+        } else {
+            const char* const q = unit + at + (((row + MF * i) * 4) ^ ofs[0]) + ks * 16 * P;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) v[c] = *reinterpret_cast<const float*>(q + c * P);
+        }
+        return v;
+    }
+};
+
+// ---- results: eight consecutive columns of a row at a time ----
+__device__ __forceinline__ void read8(const char* p, float (&v)[8], float) {
+    const f32x4_t a = *reinterpret_cast<const f32x4_t*>(p);
+    const f32x4_t b = *reinterpret_cast<const f32x4_t*>(p + 16);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) v[q] = a[q], v[q + 4] = b[q];
+}
+__device__ __forceinline__ void read8(const char* p, float (&v)[8], int32_t) {
+    const i32x4_t a = *reinterpret_cast<const i32x4_t*>(p);
+    const i32x4_t b = *reinterpret_cast<const i32x4_t*>(p + 16);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) v[q] = (float)a[q], v[q + 4] = (float)b[q];
+}
+
+typedef __bf16 bf16x2_pk_t __attribute__((ext_vector_type(2)));
+typedef float f32x2_pk_t __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+    const f32x2_pk_t v = {lo, hi};
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2_pk_t));
+}
+typedef float f32x4_any_t __attribute__((ext_vector_type(4), aligned(4)));
+// eight values from / to a tensor at any element boundary, rounded once to its type
+__device__ __forceinline__ void load8(const bf16_t* p, float (&v)[8]) {
+    const u32x4_any_t a = *reinterpret_cast<const u32x4_any_t*>(p);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        v[2 * q] = __uint_as_float(a[q] << 16);
+        v[2 * q + 1] = __uint_as_float(a[q] & 0xffff0000u);
+    }
+}
+__device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
+    const f32x4_any_t a = *reinterpret_cast<const f32x4_any_t*>(p);
+    const f32x4_any_t b = *reinterpret_cast<const f32x4_any_t*>(p + 4);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) v[q] = a[q], v[q + 4] = b[q];
+}
+__device__ __forceinline__ void store8(bf16_t* p, const float (&v)[8]) {
+    const u32x4_any_t a = {pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]),
+                           pack2(v[6], v[7])};
+    *reinterpret_cast<u32x4_any_t*>(p) = a;
+}
+__device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
+    *reinterpret_cast<f32x4_any_t*>(p) = f32x4_any_t{v[0], v[1], v[2], v[3]};
+    *reinterpret_cast<f32x4_any_t*>(p + 4) = f32x4_any_t{v[4], v[5], v[6], v[7]};
+}
+
+// One tile's operands: A has the rows, B the columns of the result; b2: the second half's first
+// row with PAIR.  rows, cols: valid ones from the tile's first on (PAIR: output columns, half of
+// the tile's B rows); k-tiles [t0, t1).
+struct TileIn {
+    const char *a, *b, *b2;
+    int64_t lda, ldb;
+    int rows, cols;
+    int64_t K;
+    int t0, t1;
+};
+
+// ------------------------------------------------------------------------------------------
+// Block form 1: a TM x TN tile by four waves (WM x WN), operands in a ring of S k-tiles.  At the
+// barrier that opens k-tile t every wave has read tile t - 1, whose units then receive tile
+// t + S - 1.
+// ------------------------------------------------------------------------------------------
+template <class E, int MF, int TM, int TN, int WM, int LA, int LB, bool PAIR, bool DMA, int S>
+struct TileForm {
+    static constexpr int WN = 4 / WM;
+    static constexpr int WTM = TM / WM, WTN = TN / WN;  // a wave's rows and columns
+    static constexpr int FM = WTM / MF, FN = WTN / MF;
+    static constexpr int HJ = PAIR ? FN / 2 : FN;       // PAIR: the gate rows' fragments
+    static constexpr int AU = TM * 128, BU = TN * 128;  // bytes of a unit
+    static constexpr int RING = S * (AU + BU);
+    static constexpr int PITCH = WTN * 4 + 16;          // bytes per staged row
+    static constexpr int STAGE = MF * PITCH;            // a wave's staging area
+    static constexpr int LDS = RING > 4 * STAGE ? RING : 4 * STAGE;
+    static_assert(WTM % MF == 0 && WTN % MF == 0 && (!PAIR || FN % 2 == 0), "");
+    typedef typename Mma<E, MF>::acc acc_t;
+    typedef Copier<LA, TM, E::SZ, 4, false, DMA> CA;
+    typedef Copier<LB, TN, E::SZ, 4, PAIR, DMA> CB;
+
+    template <class Epi>
+    static __device__ __forceinline__ void run(const TileIn& in, char* sm, const Epi& epi) {
+        const int lane = threadIdx.x & 63;
+        const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const int wm = w / WN, wn = w % WN;
+        CA ca;
+        CB cb;
+        ca.init(in.a, nullptr, in.lda, in.rows, in.K, lane, w);
+        cb.init(in.b, in.b2, in.ldb, in.cols, in.K, lane, w);
+        Reader<E, MF, LA, TM> ra;
+        Reader<E, MF, LB, TN> rb;
+        ra.init(wm * WTM, lane);
+        rb.init(PAIR ? wn * (WTN / 2) : wn * WTN, lane);
+        const uint32_t lds = __builtin_amdgcn_readfirstlane(
+            (uint32_t)(uintptr_t)(lds_void_t*)sm);
+        acc_t acc[FM][FN];
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int j = 0; j < FN; ++j) acc[i][j] = acc_t{};
+        auto issue = [&](int t, int u) {
+            ca.issue(t, in.t1, lds + u * (AU + BU), sm + u * (AU + BU), lane, w);
+            cb.issue(t, in.t1, lds + u * (AU + BU) + AU, sm + u * (AU + BU) + AU, lane, w);
+        };
+#pragma unroll
+        for (int p = 0; p < S - 1; ++p) issue(in.t0 + p, p);
+        int u = 0;
+        for (int t = in.t0; t < in.t1; ++t) {
+            ELB_WAIT_VMCNT((S - 2) * (CA::N + CB::N));
+            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            issue(t + S - 1, u == 0 ? S - 1 : u - 1);
+            const char* const pa = sm + u * (AU + BU);
+            const char* const pb = pa + AU;
+#pragma unroll
+            for (int ks = 0; ks < MF / 8; ++ks) {
+                typename E::frag fa[FM], fb[FN];
+#pragma unroll
+                for (int j = 0; j < FN; ++j)
+                    fb[j] = rb.load(pb + (j >= HJ ? BU / 2 : 0), j % HJ, ks);
+#pragma unroll
+                for (int i = 0; i < FM; ++i) fa[i] = ra.load(pa, i, ks);
+#pragma unroll
+                for (int i = 0; i < FM; ++i)
+#pragma unroll
+                    for (int j = 0; j < FN; ++j)
+                        acc[i][j] = Mma<E, MF>::mma(fb[j], fa[i], acc[i][j]);
+            }
+            u = u + 1 == S ? 0 : u + 1;
+        }
+        // results through LDS, each wave in its own area: MF rows at a time
+        ELB_WAIT_VMCNT(0);
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        results<Epi>(acc, in, sm + w * STAGE, lane, wm, wn, epi);
+    }
+
+    template <class Epi>
+    static __device__ __forceinline__ void results(const acc_t (&acc)[FM][FN], const TileIn& in,
+                                                   char* stg, int lane, int wm, int wn,
+                                                   const Epi& epi) {
+        typedef typename E::acc1 a1;
+        typedef a1 a4 __attribute__((ext_vector_type(4)));
+        constexpr int OC = PAIR ? WTN / 2 : WTN;  // output columns of the wave
+        constexpr int CPR = OC / 8, RPI = 64 / CPR;
+        const int l = lane & (MF - 1), g = lane / MF;
+        const int cc = lane % CPR, r0 = lane / CPR;
+        const int col = wn * OC + cc * 8;
+#pragma unroll
+        for (int i = 0; i < FM; ++i) {
+#pragma unroll
+            for (int j = 0; j < FN; ++j)
+#pragma unroll
+                for (int q = 0; q < MF * MF / 256; ++q) {
+                    const a4 v = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2],
+                                  acc[i][j][4 * q + 3]};
+                    const int c = j * MF + (MF == 32 ? 8 * q + 4 * g : 4 * g);
+                    *reinterpret_cast<a4*>(stg + l * PITCH + c * 4) = v;
+                }
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int p = 0; p < (MF + RPI - 1) / RPI; ++p) {
+                const int r = r0 + p * RPI;
+                if (RPI > MF && r >= MF) break;
+                const int row = wm * WTM + i * MF + r;
+                float v[8];
+                read8(stg + r * PITCH + cc * 32, v, a1{});
+                if constexpr (PAIR) {
+                    float v2[8];
+                    read8(stg + r * PITCH + (OC + cc * 8) * 4, v2, a1{});
+                    if (row < in.rows && col < in.cols) epi.put(row, col, v, v2);
+                } else {
+                    if (row < in.rows && col < in.cols) epi.put(row, col, v);
+                }
+            }
+            __builtin_amdgcn_wave_barrier();
+        }
+    }
+};
+
+// ------------------------------------------------------------------------------------------
+// Block form 2, for few rows: NW waves take a share of the contraction each, every one of them
+// the whole TM x TN tile, with a ring of S k-tiles of its own and no barrier in the loop; their
+// partial tiles are then summed in LDS in the order of the contraction.
+// ------------------------------------------------------------------------------------------
+template <class E, int TM, int TN, int NW, int LB, bool PAIR, bool DMA, int S>
+struct SplitForm {
+    static constexpr int MF = 16;
+    static constexpr int FM = TM / 16, FN = TN / 16;
+    static constexpr int AU = TM * 128, BU = TN * 128;
+    static constexpr int WRING = S * (AU + BU);  // a wave's ring
+    static constexpr int PITCH = TN * 4 + 16;
+    static constexpr int PART = TM * PITCH;      // a wave's partial tile
+    static constexpr int LDS = NW * (WRING > PART ? WRING : PART);
+    typedef typename Mma<E, 16>::acc acc_t;
+    typedef Copier<KC, TM, E::SZ, 1, false, DMA> CA;
+    typedef Copier<LB, TN, E::SZ, 1, PAIR, DMA> CB;
+
+    template <class Epi>
+    static __device__ __forceinline__ void run(const TileIn& in, char* sm, const Epi& epi) {
+        typedef typename E::acc1 a1;
+        typedef a1 a4 __attribute__((ext_vector_type(4)));
+        const int lane = threadIdx.x & 63;
+        const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        CA ca;
+        CB cb;
+        ca.init(in.a, nullptr, in.lda, in.rows, in.K, lane, 0);
+        cb.init(in.b, in.b2, in.ldb, in.cols, in.K, lane, 0);
+        Reader<E, 16, KC, TM> ra;
+        Reader<E, 16, LB, TN> rb;
+        ra.init(0, lane);
+        rb.init(0, lane);
+        char* const ring = sm + w * WRING;
+        const uint32_t lds = __builtin_amdgcn_readfirstlane(
+            (uint32_t)(uintptr_t)(lds_void_t*)sm + (uint32_t)w * WRING);
+        acc_t acc[FM][FN];
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int j = 0; j < FN; ++j) acc[i][j] = acc_t{};
+        const int nt = in.t1 - in.t0;
+        const int t0 = in.t0 + nt * w / NW, t1 = in.t0 + nt * (w + 1) / NW;
+        auto issue = [&](int t, int u) {
+            ca.issue(t, t1, lds + u * (AU + BU), ring + u * (AU + BU), lane, 0);
+            cb.issue(t, t1, lds + u * (AU + BU) + AU, ring + u * (AU + BU) + AU, lane, 0);
+        };
+#pragma unroll
+        for (int p = 0; p < S; ++p) issue(t0 + p, p);
+        int u = 0;
+        for (int t = t0; t < t1; ++t) {
+            ELB_WAIT_VMCNT((S - 1) * (CA::N + CB::N));
+            asm volatile("" ::: "memory");
+            const char* const pa = ring + u * (AU + BU);
+            const char* const pb = pa + AU;
+            typename E::frag fa[2][FM], fb[2][FN];
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks) {
+#pragma unroll
+                for (int j = 0; j < FN; ++j) fb[ks][j] = rb.load(pb, j, ks);
+#pragma unroll
+                for (int i = 0; i < FM; ++i) fa[ks][i] = ra.load(pa, i, ks);
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the units are free again
+            issue(t + S, u);
+#pragma unroll
+            for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+                for (int i = 0; i < FM; ++i)
+#pragma unroll
+                    for (int j = 0; j < FN; ++j)
+                        acc[i][j] = Mma<E, 16>::mma(fb[ks][j], fa[ks][i], acc[i][j]);
+            u = u + 1 == S ? 0 : u + 1;
+        }
+        ELB_WAIT_VMCNT(0);
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        const int l16 = lane & 15, hq = lane >> 4;
+        char* const part = sm + w * PART;
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int j = 0; j < FN; ++j)
+                *reinterpret_cast<a4*>(part + (16 * i + l16) * PITCH + (16 * j + 4 * hq) * 4) =
+                    acc[i][j];
+        __syncthreads();
+        constexpr int OC = PAIR ? TN / 2 : TN;
+        constexpr int CPR = OC / 8, ITEMS = TM * CPR;
+        for (int it = threadIdx.x; it < ITEMS; it += NW * 64) {
+            const int row = it / CPR, cc = it % CPR;
+            if (row >= in.rows || cc * 8 >= in.cols) continue;
+            float v[8], v2[8];
+            sum8<a1>(sm + row * PITCH + cc * 32, v);
+            if constexpr (PAIR) {
+                sum8<a1>(sm + row * PITCH + (OC + cc * 8) * 4, v2);
+                epi.put(row, cc * 8, v, v2);
+            } else {
+                epi.put(row, cc * 8, v);
+            }
+        }
+    }
+    template <class a1>
+    static __device__ __forceinline__ void sum8(const char* p, float (&v)[8]) {
+        typedef a1 a4 __attribute__((ext_vector_type(4)));
+        a4 a = *reinterpret_cast<const a4*>(p), b = *reinterpret_cast<const a4*>(p + 16);
+#pragma unroll
+        for (int w = 1; w < NW; ++w) {
+            a += *reinterpret_cast<const a4*>(p + w * PART);
+            b += *reinterpret_cast<const a4*>(p + w * PART + 16);
+        }
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[q] = (float)a[q], v[q + 4] = (float)b[q];
+    }
+};
+
+// ---- tiles over the chip ----
+// Blocks go round-robin over the 8 XCDs, each with its own L2: XCD x takes a contiguous range of
+// the tiles, which are numbered in groups of GM rows of tiles, down the rows first, so that the
+// blocks resident on an XCD share a patch of rows and columns.
+__device__ __forceinline__ bool dense_tile(int64_t b, int mt, int nt, int& m, int& n) {
+    constexpr int GM = 4;
+    const int64_t total = (int64_t)mt * nt;
+    const int64_t per = (total + 7) >> 3, s = b >> 3, L = (b & 7) * per + s;
+    if (s >= per || L >= total) return false;
+    const int64_t span = (int64_t)GM * nt;
+    const int g = (int)(L / span);
+    const int r = (int)(L - g * span);
+    const int gm = mt - g * GM < GM ? mt - g * GM : GM;
+    m = g * GM + r % gm;
+    n = r / gm;
+    return true;
+}
+
+// A dense product: A [rows, K] (KC) or [K, rows] (KR), B [cols, K] or [K, cols]; PAIR: B is
+// [2 cols, K], output column c of rows c and cols + c.
+struct DenseIn {
+    const char *a, *b;
+    int64_t lda, ldb;  // bytes between rows in memory
+    int64_t rows;
+    int cols;
+    int64_t K;
+};
+
+template <class Form, class E, int TM, int TN, int LA, int LB, bool PAIR, class Epi>
+__device__ __forceinline__ void dense_block(const DenseIn& d, int m, int n, char* sm,
+                                            const Epi& epi) {
+    constexpr int OC = PAIR ? TN / 2 : TN;
+    const int64_t r0 = (int64_t)m * TM;
+    const int c0 = n * OC;
+    TileIn in;
+    in.a = d.a + r0 * (LA == KC ? d.lda : E::SZ);
+    in.b = d.b + (int64_t)c0 * (LB == KC ? d.ldb : E::SZ);
+    in.b2 = PAIR ? d.b + ((int64_t)d.cols + c0) * d.ldb : nullptr;
+    in.lda = d.lda;
+    in.ldb = d.ldb;
+    in.rows = d.rows - r0 < TM ? (int)(d.rows - r0) : TM;
+    in.cols = d.cols - c0;
+    in.K = d.K;
+    in.t0 = 0;
+    in.t1 = (int)((d.K * E::SZ + 127) / 128);
+    Form::run(in, sm, epi.at(r0, c0));
+}
+
+// ---- what becomes of a product: put() takes eight columns of a row ----
+template <class T>
+struct PlainOut {  // y = [res +] v
+    T* y;
+    const T* res;
+    int64_t ld;
+    __device__ __forceinline__ PlainOut at(int64_t r0, int c0) const {
+        const int64_t o = r0 * ld + c0;
+        return {y + o, res ? res + o : nullptr, ld};
+    }
+    __device__ __forceinline__ void put(int row, int col, float (&v)[8]) const {
+        const int64_t o = row * ld + col;
+        if (res) {
+            float r[8];
+            load8(res + o, r);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) v[q] += r[q];
+        }
+        store8(y + o, v);
+    }
+};
+
+// ---- kernels ----
+template <class E, int MF, int TM, int TN, int WM, int LA, int LB, bool PAIR, bool DMA, int S,
+          class Epi>
+__global__ __launch_bounds__(256) void dense_tiles(DenseIn d, int mt, int nt, Epi epi) {
+    typedef TileForm<E, MF, TM, TN, WM, LA, LB, PAIR, DMA, S> Form;
+    __shared__ __attribute__((aligned(1024))) char sm[Form::LDS];
+    int m, n;
+    if (!dense_tile((int64_t)blockIdx.y * kTileGridRow + blockIdx.x, mt, nt, m, n)) return;
+    dense_block<Form, E, TM, TN, LA, LB, PAIR>(d, m, n, sm, epi);
+}
+
+// two products of one kind in one launch: the first mt1 nt1 tiles (rounded up to blocks1 blocks,
+// a multiple of 8), then the second's
+template <class E, int MF, int TM, int TN, int WM, int LA, int LB, bool DMA, int S, class Epi>
+__global__ __launch_bounds__(256) void dense_tiles2(DenseIn d1, DenseIn d2, int mt1, int nt1,
+                                                    int mt2, int nt2, int64_t blocks1, Epi epi1,
+                                                    Epi epi2) {
+    typedef TileForm<E, MF, TM, TN, WM, LA, LB, false, DMA, S> Form;
+    __shared__ __attribute__((aligned(1024))) char sm[Form::LDS];
+    const int64_t b = (int64_t)blockIdx.y * kTileGridRow + blockIdx.x;
+    int m, n;
+    if (b < blocks1) {
+        if (!dense_tile(b, mt1, nt1, m, n)) return;
+        dense_block<Form, E, TM, TN, LA, LB, false>(d1, m, n, sm, epi1);
+    } else {
+        if (!dense_tile(b - blocks1, mt2, nt2, m, n)) return;
+        dense_block<Form, E, TM, TN, LA, LB, false>(d2, m, n, sm, epi2);
+    }
+}
+
+inline int64_t up8(int64_t n) { return (n + 7) / 8 * 8; }
+inline dim3 grid_of(int64_t blocks) {
+    const TileGrid g = tile_grid(blocks);
+    return dim3(g.x, g.y);
+}
+inline int tiles(int64_t n, int t) { return (int)((n + t - 1) / t); }
+
+template <class E, int MF, int TM, int TN, int WM, int LA, int LB, bool PAIR, int S, class Epi>
+void run_tiles(const DenseIn& d, bool dma, const Epi& epi, hipStream_t s) {
+    const int mt = tiles(d.rows, TM), nt = tiles(d.cols, PAIR ? TN / 2 : TN);
+    if (mt == 0 || nt == 0) return;
+    const dim3 grid = grid_of(up8((int64_t)mt * nt));
+    if (dma)
+        ELB_LAUNCH((dense_tiles<E, MF, TM, TN, WM, LA, LB, PAIR, true, S, Epi>), grid, dim3(256),
+                   0, s, d, mt, nt, epi);
+    else
+        ELB_LAUNCH((dense_tiles<E, MF, TM, TN, WM, LA, LB, PAIR, false, S, Epi>), grid,
+                   dim3(256), 0, s, d, mt, nt, epi);
+}
+
+template <class E, int MF, int TM, int TN, int WM, int LA, int LB, int S, class Epi>
+void run_tiles2(const DenseIn& d1, const DenseIn& d2, bool dma, const Epi& e1, const Epi& e2,
+                hipStream_t s) {
+    const int mt1 = tiles(d1.rows, TM), nt1 = tiles(d1.cols, TN);
+    const int mt2 = tiles(d2.rows, TM), nt2 = tiles(d2.cols, TN);
+    const int64_t b1 = up8((int64_t)mt1 * nt1);
+    const int64_t blocks = b1 + up8((int64_t)mt2 * nt2);
+    if (blocks == 0) return;
+    const dim3 grid = grid_of(blocks);
+    if (dma)
+        ELB_LAUNCH((dense_tiles2<E, MF, TM, TN, WM, LA, LB, true, S, Epi>), grid, dim3(256), 0, s,
+                   d1, d2, mt1, nt1, mt2, nt2, b1, e1, e2);
+    else
+        ELB_LAUNCH((dense_tiles2<E, MF, TM, TN, WM, LA, LB, false, S, Epi>), grid, dim3(256), 0,
+                   s, d1, d2, mt1, nt1, mt2, nt2, b1, e1, e2);
+}
+
+}  // namespace
+
+}  // namespace elb

@@ -1,0 +1,151 @@
+// The dense gated feed-forward block, forward and backward (bf16 and fp32).
+//
+//   forward   g = x Wg^T, u = x Wu^T, h = silu(g) * u      one kernel: both projections share the
+//                                                          token tile, SwiGLU on the accumulators
+//             y = [residual +] h Wd^T
+//   backward  dh = dy Wd, s = sigma(g): dg = dh u s (1 + g (1 - s)), du = dh g s, h = g s u
+//             dx = dg Wg + du Wu = [dg du] [Wg; Wu]        one product of contraction 2 m
+//             dWg = dg^T x, dWu = du^T x, dWd = dy^T h     [dg du]^T x, and beside it dy^T h
+//
+// Roundings to bf16: h before the down product, dg, du and h before the gradients' products (they
+// are matrix operands), and every output.  g and u reach the backward in fp32: rounded to
+// bf16, their errors would add to those of dg and du through sigma' in every gradient.
+#include "dense.h"
+
+namespace elb {
+
+namespace {
+
+// e^-g: the hardware exponential where the result is rounded to bf16, the exact one for fp32
+__device__ __forceinline__ float exp_neg(float g, bf16_t) { return __expf(-g); }
+__device__ __forceinline__ float exp_neg(float g, float) { return expf(-g); }
+__device__ __forceinline__ float recip(float v, bf16_t) { return __builtin_amdgcn_rcpf(v); }
+__device__ __forceinline__ float recip(float v, float) { return 1.0f / v; }
+
+// ---- what becomes of the products' results ----
+template <class T>
+struct GateOut {  // h = silu(g) u; keep [T, 2m] fp32: g and u for the backward
+    T* h;
+    float* keep;
+    int64_t m;
+    __device__ __forceinline__ GateOut at(int64_t r0, int c0) const {
+        return {h + r0 * m + c0, keep ? keep + r0 * 2 * m + c0 : nullptr, m};
+    }
+    __device__ __forceinline__ void put(int row, int col, const float (&g)[8],
+                                        const float (&u)[8]) const {
+        float v[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q)
+            v[q] = g[q] * recip(1.0f + exp_neg(g[q], T()), T()) * u[q];
+        store8(h + row * m + col, v);
+        if (keep) {
+            store8(keep + row * 2 * m + col, g);
+            store8(keep + row * 2 * m + m + col, u);
+        }
+    }
+};
+
+template <class T>
+struct GateGradOut {  // from dh, g and u: dg and du [T, 2m], h [T, m]
+    const float* keep;
+    T* dgu;
+    T* h;
+    int64_t m;
+    __device__ __forceinline__ GateGradOut at(int64_t r0, int c0) const {
+        const int64_t o = r0 * 2 * m + c0;
+        return {keep + o, dgu + o, h + r0 * m + c0, m};
+    }
+    __device__ __forceinline__ void put(int row, int col, const float (&dh)[8]) const {
+        const int64_t o = row * 2 * m + col;
+        float g[8], u[8], dg[8], du[8], hh[8];
+        load8(keep + o, g);
+        load8(keep + o + m, u);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            const float s = recip(1.0f + exp_neg(g[q], T()), T());
+            const float gs = g[q] * s;
+            dg[q] = dh[q] * u[q] * (s + gs * (1.0f - s));
+            du[q] = dh[q] * gs;
+            hh[q] = gs * u[q];
+        }
+        store8(dgu + o, dg);
+        store8(dgu + o + m, du);
+        store8(h + row * m + col, hh);
+    }
+};
+
+template <class E, class T>
+struct Block {
+    static constexpr int MF = E::SZ == 2 ? 32 : 16;
+    static constexpr int TT = E::SZ == 2 ? 128 : 64;  // block tile
+    static constexpr int S = E::SZ == 2 ? 2 : 3;
+
+    template <int LA, int LB, bool PAIR, class Epi>
+    static void product(const void* a, int64_t lda, const void* b, int64_t ldb, int64_t rows,
+                        int cols, int64_t K, const Epi& epi, hipStream_t s) {
+        const DenseIn d{(const char*)a, (const char*)b, lda * E::SZ, ldb * E::SZ, rows, cols, K};
+        run_tiles<E, MF, TT, TT, 2, LA, LB, PAIR, S>(d, aligned16(a, b), epi, s);
+    }
+
+    static hipError_t forward(const void* x, const void* Wgu, const void* Wd, const void* res,
+                              int64_t T_, int d, int m, void* h, float* keep, void* y,
+                              hipStream_t s) {
+        {
+            ProfileScope prof("ffn_gate_up", s);
+            product<KC, KC, true>(x, d, Wgu, d, T_, m, d, GateOut<T>{(T*)h, keep, m}, s);
+            if (hipError_t e = hipGetLastError()) return e;
+        }
+        ProfileScope prof("ffn_down", s);
+        product<KC, KC, false>(h, m, Wd, m, T_, d, m, PlainOut<T>{(T*)y, (const T*)res, d}, s);
+        return hipGetLastError();
+    }
+
+    static hipError_t backward(const void* dy, const void* x, const void* Wgu, const void* Wd,
+                               const float* keep, int64_t T_, int d, int m, void* dgu, void* h,
+                               void* dx, void* dWgu, void* dWd, hipStream_t s) {
+        {
+            ProfileScope prof("ffn_dh", s);
+            product<KC, KR, false>(dy, d, Wd, m, T_, m, d,
+                                   GateGradOut<T>{keep, (T*)dgu, (T*)h, m}, s);
+            if (hipError_t e = hipGetLastError()) return e;
+        }
+        if (dx) {
+            ProfileScope prof("ffn_dx", s);
+            product<KC, KR, false>(dgu, 2 * (int64_t)m, Wgu, d, T_, d, 2 * (int64_t)m,
+                                   PlainOut<T>{(T*)dx, nullptr, d}, s);
+            if (hipError_t e = hipGetLastError()) return e;
+        }
+        if (dWgu || dWd) {
+            ProfileScope prof("ffn_dw", s);
+            const DenseIn a{(const char*)dgu, (const char*)x, 2 * (int64_t)m * E::SZ,
+                            (int64_t)d * E::SZ, dWgu ? 2 * (int64_t)m : 0, d, T_};
+            const DenseIn b{(const char*)dy, (const char*)h, (int64_t)d * E::SZ,
+                            (int64_t)m * E::SZ, dWd ? d : 0, m, T_};
+            run_tiles2<E, MF, TT, TT, 2, KR, KR, S>(
+                a, b, aligned16(dy, x), PlainOut<T>{(T*)dWgu, nullptr, d},
+                PlainOut<T>{(T*)dWd, nullptr, m}, s);
+        }
+        return hipGetLastError();
+    }
+};
+
+}  // namespace
+
+hipError_t launch_ffn_forward(const void* x, const void* Wgu, const void* Wd, const void* res,
+                              int64_t T, int d, int m, int dtype, void* h, float* gate_up, void* y,
+                              hipStream_t s) {
+    return dtype == ELB_BF16
+               ? Block<Bf16, bf16_t>::forward(x, Wgu, Wd, res, T, d, m, h, gate_up, y, s)
+               : Block<F32, float>::forward(x, Wgu, Wd, res, T, d, m, h, gate_up, y, s);
+}
+
+hipError_t launch_ffn_backward(const void* dy, const void* x, const void* Wgu, const void* Wd,
+                               const float* gate_up, int64_t T, int d, int m, int dtype, void* dgu,
+                               void* h, void* dx, void* dWgu, void* dWd, hipStream_t s) {
+    return dtype == ELB_BF16 ? Block<Bf16, bf16_t>::backward(dy, x, Wgu, Wd, gate_up, T, d, m, dgu,
+                                                             h, dx, dWgu, dWd, s)
+                             : Block<F32, float>::backward(dy, x, Wgu, Wd, gate_up, T, d, m, dgu,
+                                                           h, dx, dWgu, dWd, s);
+}
+
+}  // namespace elb
