@@ -151,6 +151,9 @@ int check_dense(int64_t T, int a, const char* an, int b, const char* bn) {
         return fail(ELB_ERR_UNSUPPORTED, "%s = %d or %s = %d exceeds %d", an, a, bn, b, kMaxDim);
     if (T >= (int64_t)1 << 31)
         return fail(ELB_ERR_UNSUPPORTED, "T = %lld exceeds 2^31 - 1", (long long)T);
+    // tiles are numbered in 32 bits; 2^38 elements of bf16 are twice the card's memory
+    if (T * (int64_t)std::max(a, b) > (int64_t)1 << 38)
+        return fail(ELB_ERR_UNSUPPORTED, "T x %s or T x %s exceeds 2^38 elements", an, bn);
     return ELB_OK;
 }
 

@@ -11,7 +11,7 @@
 #pragma once
 
 #include "common.h"
-#include "tilegrid.h"
+#include "forms.h"
 
 namespace elb {
 
@@ -103,6 +103,11 @@ __device__ __forceinline__ int kr_swz(int k) {
 // 16 bytes from global memory at any byte boundary
 typedef uint32_t u32x4_byte_t __attribute__((ext_vector_type(4), aligned(1)));
 
+// the same value in every lane, in a scalar register
+__device__ __forceinline__ uint32_t uniform(uint32_t v) {
+    return __builtin_amdgcn_readfirstlane(v);
+}
+
 constexpr uint32_t kOutOfBounds = 0x7fffff00u;  // past every buffer: spans stay below 2^31 - 512
 
 // One wave's share of a unit's copies: NW waves copy TR rows, 1 KB per instruction
@@ -136,7 +141,7 @@ struct Copier {
             klen = K * SZ;
         } else {
             span = (int64_t)(ext < TR ? ext : TR) * SZ;
-            klen = K;
+            klen = ext > 0 ? K : 0;  // a tile past the last column reads nothing
         }
         base[0] = (const char*)(PAIR && NB == 1 && w >= NW / 2 ? p1 : p0);
         if (NB == 2) base[NB - 1] = (const char*)p1;
@@ -146,56 +151,66 @@ struct Copier {
                 int r = 8 * (w * N + i) + (lane >> 3);
                 if (i < 2) kchunk[i] = kc_swz(r, lane & 7) * 16;
                 if (PAIR) r = r >= HR ? r - HR : r;
-                off[i] = (uint32_t)(r * ld_) + kchunk[i & 1];
+                off[i] = (uint32_t)r * (uint32_t)ld_ + kchunk[i & 1];
             } else {
                 constexpr int LPR = P / 16;  // lanes per contraction row
                 const int k = (w * N + i) * (64 / LPR) + lane / LPR;
-                off[i] = (uint32_t)(k * ld_) + ((lane % LPR) ^ kr_swz<TR, SZ>(k)) * 16;
+                off[i] = (uint32_t)k * (uint32_t)ld_ + ((lane % LPR) ^ kr_swz<TR, SZ>(k)) * 16;
             }
         }
         if (LAY == KC && N == 1) kchunk[1] = kchunk[0];
     }
-    // copy k-tile t into the unit at LDS byte address lds (ldsp: the same as a pointer); past
-    // tend nothing is read (zeros are written), so that the count of copies in flight is the same
-    __device__ __forceinline__ void issue(int t, int tend, uint32_t lds, char* ldsp, int lane,
-                                          int w) const {
-        int64_t at, rec;
-        if (LAY == KC) {
-            at = (int64_t)t * 128;
-            rec = span - at;
-        } else {
-            at = (int64_t)t * KT * ld;
-            const int64_t left = klen - (int64_t)t * KT;
-            rec = ((left < KT ? left : KT) - 1) * ld + span;
-            if (left <= 0) rec = 0;
-        }
-        if (t >= tend || rec < 0) rec = 0;
-        const bool tail = LAY == KC && klen - at < 128;
+    // a k-tile's buffer bounds
+    struct Unit {
         u32x4_t rs[NB];
+        int64_t at, rec, left;
+    };
+    // k-tile t; past tend nothing is read (zeros are written), so that the count of copies in
+    // flight is the same
+    __device__ __forceinline__ Unit unit(int t, int tend) const {
+        Unit u;
+        if (LAY == KC) {
+            u.at = (int64_t)t * 128;
+            u.rec = span - u.at;
+            u.left = klen - u.at;
+        } else {
+            u.at = (int64_t)t * KT * ld;
+            u.left = klen - (int64_t)t * KT;
+            u.rec = u.left <= 0 ? 0 : ((u.left < KT ? u.left : KT) - 1) * ld + span;
+        }
+        if (t >= tend || u.rec < 0) u.rec = 0;
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
-            const uint64_t p = (uint64_t)(base[b] + at);
-            rs[b] = u32x4_t{(uint32_t)p, (uint32_t)(p >> 32) & 0xffffu, (uint32_t)rec,
-                            0x00027000u};
+            const uint64_t p = (uint64_t)(base[b] + u.at);
+            u.rs[b] = u32x4_t{uniform((uint32_t)p), uniform((uint32_t)(p >> 32)) & 0xffffu,
+                              uniform((uint32_t)u.rec), 0x00027000u};
         }
+        return u;
+    }
+    // copy instruction i of the unit at LDS byte address lds (ldsp: the same as a pointer)
+    __device__ __forceinline__ void one(const Unit& u, int i, uint32_t lds, char* ldsp, int lane,
+                                        int w) const {
+        const int b = (NB == 2 && i >= N / 2) ? NB - 1 : 0;
+        uint32_t vo = off[i];
+        if (LAY == KC && u.left < 128) vo = kchunk[i & 1] < u.left ? vo : kOutOfBounds;
+        if constexpr (DMA) {
+            const uint32_t la = lds + (uint32_t)(w * N + i) * 1024;
+            // inline assembly: the compiler cannot tell which unit a copy writes, and would wait
+            // for every copy in flight before each LDS read; waits are explicit
+            asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                         :: "s"(la), "v"(vo), "s"(u.rs[b]) : "memory", "m0");
+        } else {
+            u32x4_t v = {0, 0, 0, 0};
+            if ((int64_t)vo < u.rec)
+                v = *reinterpret_cast<const u32x4_byte_t*>(base[b] + u.at + vo);
+            *reinterpret_cast<u32x4_t*>(ldsp + (w * N + i) * 1024 + lane * 16) = v;
+        }
+    }
+    __device__ __forceinline__ void issue(int t, int tend, uint32_t lds, char* ldsp, int lane,
+                                          int w) const {
+        const Unit u = unit(t, tend);
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int b = (NB == 2 && i >= N / 2) ? NB - 1 : 0;
-            uint32_t vo = off[i];
-            if (tail) vo = kchunk[i & 1] < klen - at ? vo : kOutOfBounds;
-            if constexpr (DMA) {
-                const uint32_t la = lds + (uint32_t)(w * N + i) * 1024;
-                // inline assembly: the compiler cannot tell which unit a copy writes, and would
-                // wait for every copy in flight before each LDS read; waits are explicit
-                asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
-                             :: "s"(la), "v"(vo), "s"(rs[b]) : "memory", "m0");
-            } else {
-                u32x4_t v = {0, 0, 0, 0};
-                if ((int64_t)vo < rec)
-                    v = *reinterpret_cast<const u32x4_byte_t*>(base[b] + at + vo);
-                *reinterpret_cast<u32x4_t*>(ldsp + (w * N + i) * 1024 + lane * 16) = v;
-            }
-        }
+        for (int i = 0; i < N; ++i) one(u, i, lds, ldsp, lane, w);
     }
 };
 
@@ -537,21 +552,352 @@ struct SplitForm {
     }
 };
 
+// ------------------------------------------------------------------------------------------
+// Block form 3, for many rows: a TM x TN tile by eight waves, two on each SIMD, that take turns:
+// while the waves 0 .. 3 feed themselves (LDS reads, copies), the waves 4 .. 7 keep the matrix
+// units busy, and the other way round.  The tile is four quadrants (row half x column half) of
+// QM x QN; a wave owns the same QM / WM x QN / WN piece of each.  A k-tile is then four phases, each
+// a quadrant:
+//     phase   LDS reads           copies issued       matrix products
+//       0     A0, B0 (tile t)     A1 (tile t + 1)     A0 B0
+//       1     B1                  A0 (tile t + 2)     A0 B1
+//       2     A1                  B0 (tile t + 2)     A1 B1
+//       3     -                   B1 (tile t + 2)     A1 B0
+// Each half of a phase (reads and copies; products) ends with a barrier of all waves; the second
+// group starts one half later.  A unit is overwritten (by the copies of two k-tiles later, two
+// buffers) at the earliest two halves after its last read by the first group, one after that by
+// the second, whose reads are waited for before its barrier.  Every unit is copied six or seven
+// phases before its first read; the waits leave what is not needed yet in flight: phase 3 needs
+// A0, B0 and B1 of tile t + 1 (issued after them: A1 of it, A0, B0, B1 of t + 2), phase 1 A1 of
+// tile t (after it: A0, B0, B1, A1 of t + 1 and A0 of t + 2).
+// ------------------------------------------------------------------------------------------
+template <class E, int TM, int TN, int WM, int LA, int LB, bool PAIR>
+struct TurnForm {
+    static constexpr int WN = 8 / WM;
+    static constexpr int QM = TM / 2, QN = TN / 2;
+    static constexpr int PM = QM / WM, PN = QN / WN;  // a wave's piece of a quadrant
+    static constexpr int FM = PM / 32, FN = PN / 32;
+    static constexpr int AU = QM * 128, BU = QN * 128, BUF = 2 * (AU + BU);
+    static constexpr int PITCH = 2 * PN * 4 + 16, STAGE = 32 * PITCH;
+    static constexpr int LDS = 2 * BUF > 8 * STAGE ? 2 * BUF : 8 * STAGE;
+    static_assert(FM * 32 * WM == QM && FN * 32 * WN == QN, "");
+    typedef typename Mma<E, 32>::acc acc_t;
+    typedef Copier<LA, QM, E::SZ, 8, false, true> CA;
+    typedef Copier<LB, QN, E::SZ, 8, false, true> CB;
+
+    template <class Epi>
+    static __device__ __forceinline__ void run(const TileIn& in, char* sm, const Epi& epi) {
+        const int lane = threadIdx.x & 63;
+        const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const int wm = w / WN, wn = w % WN;
+        const bool second = w >= 4;
+        CA ca[2];
+        CB cb[2];
+        ca[0].init(in.a, nullptr, in.lda, in.rows, in.K, lane, w);
+        ca[1].init(in.a + QM * (LA == KC ? in.lda : E::SZ), nullptr, in.lda,
+                   in.rows > QM ? in.rows - QM : 0, in.K, lane, w);
+        cb[0].init(in.b, nullptr, in.ldb, in.cols, in.K, lane, w);
+        cb[1].init(PAIR ? in.b2 : in.b + QN * (LB == KC ? in.ldb : E::SZ), nullptr, in.ldb,
+                   PAIR ? in.cols : in.cols > QN ? in.cols - QN : 0, in.K, lane, w);
+        Reader<E, 32, LA, QM> ra;
+        Reader<E, 32, LB, QN> rb;
+        ra.init(wm * PM, lane);
+        rb.init(wn * PN, lane);
+        const uint32_t lds = __builtin_amdgcn_readfirstlane(
+            (uint32_t)(uintptr_t)(lds_void_t*)sm);
+        acc_t acc[2][2][FM][FN];
+#pragma unroll
+        for (int a = 0; a < 2; ++a)
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int i = 0; i < FM; ++i)
+#pragma unroll
+                    for (int j = 0; j < FN; ++j) acc[a][b][i][j] = acc_t{};
+        auto copy_a = [&](int h, int t) {
+            const int at = ((t - in.t0) & 1) * BUF + h * AU;
+            ca[h].issue(t, in.t1, lds + at, sm + at, lane, w);
+        };
+        auto copy_b = [&](int h, int t) {
+            const int at = ((t - in.t0) & 1) * BUF + 2 * AU + h * BU;
+            cb[h].issue(t, in.t1, lds + at, sm + at, lane, w);
+        };
+        typename E::frag fa[FM][4], fb[2][FN][4];
+        auto read_a = [&](const char* unit) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int i = 0; i < FM; ++i) fa[i][k] = ra.load(unit, i, k);
+        };
+        auto read_b = [&](const char* unit, int h) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int j = 0; j < FN; ++j) fb[h][j][k] = rb.load(unit, j, k);
+        };
+        auto half = [&]() {  // the end of a half phase
+            __builtin_amdgcn_sched_barrier(0);
+            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        auto products = [&](int a, int b) {
+            __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int i = 0; i < FM; ++i)
+#pragma unroll
+                    for (int j = 0; j < FN; ++j)
+                        acc[a][b][i][j] =
+                            Mma<E, 32>::mma(fb[b][j][k], fa[i][k], acc[a][b][i][j]);
+            __builtin_amdgcn_s_setprio(0);
+            __builtin_amdgcn_sched_barrier(0);
+            asm volatile("s_barrier" ::: "memory");
+            __builtin_amdgcn_sched_barrier(0);
+        };
+
+        const int t0 = in.t0;
+        copy_a(0, t0);
+        copy_b(0, t0);
+        copy_b(1, t0);
+        copy_a(1, t0);
+        copy_a(0, t0 + 1);
+        copy_b(0, t0 + 1);
+        copy_b(1, t0 + 1);
+        ELB_WAIT_VMCNT(2 * CA::N + 2 * CB::N);
+        half();
+        if (second) asm volatile("s_barrier" ::: "memory");
+        for (int t = t0; t < in.t1; ++t) {
+            const char* const buf = sm + ((t - t0) & 1) * BUF;
+            read_b(buf + 2 * AU, 0);
+            read_a(buf);
+            copy_a(1, t + 1);
+            half();
+            products(0, 0);
+            read_b(buf + 2 * AU + BU, 1);
+            copy_a(0, t + 2);
+            ELB_WAIT_VMCNT(3 * CA::N + 2 * CB::N);
+            half();
+            products(0, 1);
+            read_a(buf + AU);
+            copy_b(0, t + 2);
+            half();
+            products(1, 1);
+            copy_b(1, t + 2);
+            ELB_WAIT_VMCNT(2 * CA::N + 2 * CB::N);
+            half();
+            products(1, 0);
+        }
+        if (!second) asm volatile("s_barrier" ::: "memory");
+        ELB_WAIT_VMCNT(0);
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+
+        // results through LDS, each wave in its own area: 32 rows of a row half at a time
+        typedef typename E::acc1 a1;
+        typedef a1 a4 __attribute__((ext_vector_type(4)));
+        char* const stg = sm + w * STAGE;
+        constexpr int HC = PN / 8;                    // 8-column chunks of a column half
+        constexpr int CPR = PAIR ? HC : 2 * HC, RPI = 64 / CPR;
+        const int l = lane & 31, g = lane >> 5;
+        const int cc = lane % CPR, r0 = lane / CPR;
+        const int col = (cc / HC) * QN + wn * PN + (cc % HC) * 8;
+#pragma unroll
+        for (int a = 0; a < 2; ++a)
+#pragma unroll
+            for (int i = 0; i < FM; ++i) {
+#pragma unroll
+                for (int b = 0; b < 2; ++b)
+#pragma unroll
+                    for (int j = 0; j < FN; ++j)
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            const acc_t& c = acc[a][b][i][j];
+                            const a4 v = {c[4 * q], c[4 * q + 1], c[4 * q + 2], c[4 * q + 3]};
+                            *reinterpret_cast<a4*>(stg + l * PITCH +
+                                                   (b * PN + j * 32 + 8 * q + 4 * g) * 4) = v;
+                        }
+                __builtin_amdgcn_wave_barrier();
+#pragma unroll
+                for (int p = 0; p < 32 / RPI; ++p) {
+                    const int r = r0 + p * RPI;
+                    const int row = a * QM + wm * PM + i * 32 + r;
+                    float v[8];
+                    read8(stg + r * PITCH + cc * 32, v, a1{});
+                    if constexpr (PAIR) {
+                        float v2[8];
+                        read8(stg + r * PITCH + (PN + cc * 8) * 4, v2, a1{});
+                        if (row < in.rows && col < in.cols) epi.put(row, col, v, v2);
+                    } else {
+                        if (row < in.rows && col < in.cols) epi.put(row, col, v);
+                    }
+                }
+                __builtin_amdgcn_wave_barrier();
+            }
+    }
+};
+
+// ------------------------------------------------------------------------------------------
+// Block form 4, for tiles that are few (one round over the chip): a 128 x 128 tile by two groups of
+// four waves (2 x 2 of 64 x 64) that take the k-tiles in turn, one group the even, the other the
+// odd ones, so that a compute unit has two waves per SIMD without a second tile.  A group
+// reads a whole k-tile into registers while the other one multiplies, and the other way round
+// (barriers of all waves between the halves, the second group one half behind).  A group's
+// k-tile i + 2 is copied over k-tile i as soon as its waves have read that.  The two partial tiles
+// are added in LDS, each group finishing one half of every wave's rows.
+// ------------------------------------------------------------------------------------------
+template <class E, int LA, int LB, bool PAIR>
+struct PairForm {
+    static constexpr int TM = 128, TN = 128;
+    static constexpr int AU = TM * 128, BU = TN * 128, BUF = AU + BU;
+    static constexpr int PITCH = 64 * 4 + 16, STAGE = 32 * PITCH;
+    static constexpr int LDS = 16 * STAGE > 4 * BUF ? 16 * STAGE : 4 * BUF;
+    typedef typename Mma<E, 32>::acc acc_t;
+    typedef Copier<LA, TM, E::SZ, 4, false, true> CA;
+    typedef Copier<LB, TN, E::SZ, 4, PAIR, true> CB;
+
+    template <class Epi>
+    static __device__ __forceinline__ void run(const TileIn& in, char* sm, const Epi& epi) {
+        typedef typename E::acc1 a1;
+        typedef a1 a4 __attribute__((ext_vector_type(4)));
+        const int lane = threadIdx.x & 63;
+        const int w8 = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const int grp = w8 >> 2, w = w8 & 3;
+        const int wm = w >> 1, wn = w & 1;
+        CA ca;
+        CB cb;
+        ca.init(in.a, nullptr, in.lda, in.rows, in.K, lane, w);
+        cb.init(in.b, in.b2, in.ldb, in.cols, in.K, lane, w);
+        Reader<E, 32, LA, TM> ra;
+        Reader<E, 32, LB, TN> rb;
+        ra.init(wm * 64, lane);
+        rb.init(PAIR ? wn * 32 : wn * 64, lane);
+        char* const ring = sm + grp * 2 * BUF;
+        const uint32_t lds = __builtin_amdgcn_readfirstlane(
+            (uint32_t)(uintptr_t)(lds_void_t*)sm + (uint32_t)(grp * 2 * BUF));
+        acc_t acc[2][2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) acc[i][j] = acc_t{};
+        auto copy = [&](int i) {  // the group's i-th k-tile
+            const int t = in.t0 + 2 * i + grp, at = (i & 1) * BUF;
+            ca.issue(t, in.t1, lds + at, ring + at, lane, w);
+            cb.issue(t, in.t1, lds + at + AU, ring + at + AU, lane, w);
+        };
+        const int n = (in.t1 - in.t0 + 1) / 2;  // of both groups; past the last one zeros
+        copy(0);
+        copy(1);
+        ELB_WAIT_VMCNT(CA::N + CB::N);
+        asm volatile("s_barrier" ::: "memory");
+        if (grp) asm volatile("s_barrier" ::: "memory");
+        for (int i = 0; i < n; ++i) {
+            const char* const pa = ring + (i & 1) * BUF;
+            const char* const pb = pa + AU;
+            typename E::frag fa[2][4], fb[2][4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    fb[j][k] = PAIR ? rb.load(pb + j * (BU / 2), 0, k) : rb.load(pb, j, k);
+                    fa[j][k] = ra.load(pa, j, k);
+                }
+            __builtin_amdgcn_sched_barrier(0);
+            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            __builtin_amdgcn_sched_barrier(0);
+            const int t2 = in.t0 + 2 * (i + 2) + grp, at2 = (i & 1) * BUF;
+            const auto ua = ca.unit(t2, in.t1);
+            const auto ub = cb.unit(t2, in.t1);
+            // a copy after every other product: one that cannot issue at once then holds up one
+            // product, not all of them
+            __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int a = 0; a < 2; ++a) {
+#pragma unroll
+                    for (int b = 0; b < 2; ++b)
+                        acc[a][b] = Mma<E, 32>::mma(fb[b][k], fa[a][k], acc[a][b]);
+                    __builtin_amdgcn_sched_barrier(0);
+                    if (k < 2) ca.one(ua, 2 * k + a, lds + at2, ring + at2, lane, w);
+                    else cb.one(ub, 2 * k + a - 4, lds + at2 + AU, ring + at2 + AU, lane, w);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            __builtin_amdgcn_s_setprio(0);
+            ELB_WAIT_VMCNT(CA::N + CB::N);
+            __builtin_amdgcn_sched_barrier(0);
+            asm volatile("s_barrier" ::: "memory");
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (!grp) asm volatile("s_barrier" ::: "memory");
+        ELB_WAIT_VMCNT(0);
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+
+        // area a of wave w: its rows 32 a .. 32 a + 31, of group 0 and of group 1
+        const int l = lane & 31, g = lane >> 5;
+#pragma unroll
+        for (int a = 0; a < 2; ++a) {
+            char* const stg = sm + ((w * 2 + a) * 2 + grp) * STAGE + l * PITCH;
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const acc_t& c = acc[a][b];
+                    *reinterpret_cast<a4*>(stg + (b * 32 + 8 * q + 4 * g) * 4) =
+                        a4{c[4 * q], c[4 * q + 1], c[4 * q + 2], c[4 * q + 3]};
+                }
+        }
+        __syncthreads();
+        constexpr int OC = PAIR ? 32 : 64, CPR = OC / 8, RPI = 64 / CPR;
+        const int cc = lane % CPR, r0 = lane / CPR;
+        const int col = wn * OC + cc * 8;
+        const char* const stg = sm + (w * 2 + grp) * 2 * STAGE;
+#pragma unroll
+        for (int p = 0; p < 32 / RPI; ++p) {
+            const int r = r0 + p * RPI, row = wm * 64 + grp * 32 + r;
+            if (row >= in.rows || col >= in.cols) continue;
+            float v[8];
+            sum8<a1>(stg + r * PITCH + cc * 32, v);
+            if constexpr (PAIR) {
+                float v2[8];
+                sum8<a1>(stg + r * PITCH + (32 + cc * 8) * 4, v2);
+                epi.put(row, col, v, v2);
+            } else {
+                epi.put(row, col, v);
+            }
+        }
+    }
+    template <class a1>
+    static __device__ __forceinline__ void sum8(const char* p, float (&v)[8]) {
+        typedef a1 a4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const a4 s = *reinterpret_cast<const a4*>(p + 16 * h) +
+                         *reinterpret_cast<const a4*>(p + STAGE + 16 * h);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) v[4 * h + q] = (float)s[q];
+        }
+    }
+};
+
 // ---- tiles over the chip ----
 // Blocks go round-robin over the 8 XCDs, each with its own L2: XCD x takes a contiguous range of
 // the tiles, which are numbered in groups of GM rows of tiles, down the rows first, so that the
 // blocks resident on an XCD share a patch of rows and columns.
-__device__ __forceinline__ bool dense_tile(int64_t b, int mt, int nt, int& m, int& n) {
-    constexpr int GM = 4;
-    const int64_t total = (int64_t)mt * nt;
-    const int64_t per = (total + 7) >> 3, s = b >> 3, L = (b & 7) * per + s;
+// The block's number; blocks of up to 512 threads in rows of 2^22, so that a launch dimension stays
+// below 2^32 threads.
+constexpr int kDenseRow = 1 << 22;
+__device__ __forceinline__ uint32_t dense_block_number() {
+    return blockIdx.y * (uint32_t)kDenseRow + blockIdx.x;
+}
+__device__ __forceinline__ bool dense_tile(uint32_t b, uint32_t mt, uint32_t nt, int& m, int& n) {
+    constexpr uint32_t GM = 4;
+    const uint32_t total = mt * nt;
+    const uint32_t per = (total + 7) >> 3, s = b >> 3, L = (b & 7) * per + s;
     if (s >= per || L >= total) return false;
-    const int64_t span = (int64_t)GM * nt;
-    const int g = (int)(L / span);
-    const int r = (int)(L - g * span);
-    const int gm = mt - g * GM < GM ? mt - g * GM : GM;
-    m = g * GM + r % gm;
-    n = r / gm;
+    const uint32_t span = GM * nt, g = L / span, r = L - g * span;
+    const uint32_t gm = mt - g * GM < GM ? mt - g * GM : GM;
+    n = (int)(r / gm);
+    m = (int)(g * GM + r - n * gm);
     return true;
 }
 
@@ -614,7 +960,7 @@ __global__ __launch_bounds__(256) void dense_tiles(DenseIn d, int mt, int nt, Ep
     typedef TileForm<E, MF, TM, TN, WM, LA, LB, PAIR, DMA, S> Form;
     __shared__ __attribute__((aligned(1024))) char sm[Form::LDS];
     int m, n;
-    if (!dense_tile((int64_t)blockIdx.y * kTileGridRow + blockIdx.x, mt, nt, m, n)) return;
+    if (!dense_tile(dense_block_number(), mt, nt, m, n)) return;
     dense_block<Form, E, TM, TN, LA, LB, PAIR>(d, m, n, sm, epi);
 }
 
@@ -622,11 +968,11 @@ __global__ __launch_bounds__(256) void dense_tiles(DenseIn d, int mt, int nt, Ep
 // a multiple of 8), then the second's
 template <class E, int MF, int TM, int TN, int WM, int LA, int LB, bool DMA, int S, class Epi>
 __global__ __launch_bounds__(256) void dense_tiles2(DenseIn d1, DenseIn d2, int mt1, int nt1,
-                                                    int mt2, int nt2, int64_t blocks1, Epi epi1,
+                                                    int mt2, int nt2, uint32_t blocks1, Epi epi1,
                                                     Epi epi2) {
     typedef TileForm<E, MF, TM, TN, WM, LA, LB, false, DMA, S> Form;
     __shared__ __attribute__((aligned(1024))) char sm[Form::LDS];
-    const int64_t b = (int64_t)blockIdx.y * kTileGridRow + blockIdx.x;
+    const uint32_t b = dense_block_number();
     int m, n;
     if (b < blocks1) {
         if (!dense_tile(b, mt1, nt1, m, n)) return;
@@ -637,41 +983,169 @@ __global__ __launch_bounds__(256) void dense_tiles2(DenseIn d1, DenseIn d2, int 
     }
 }
 
+template <class E, int TM, int TN, int NW, int LB, bool PAIR, int S, class Epi>
+__global__ __launch_bounds__(NW * 64) void dense_split(DenseIn d, int mt, int nt, Epi epi) {
+    typedef SplitForm<E, TM, TN, NW, LB, PAIR, true, S> Form;
+    __shared__ __attribute__((aligned(1024))) char sm[Form::LDS];
+    int m, n;
+    if (!dense_tile(dense_block_number(), mt, nt, m, n)) return;
+    dense_block<Form, E, TM, TN, KC, LB, PAIR>(d, m, n, sm, epi);
+}
+
+template <class E, int TM, int TN, int WM, int LA, int LB, bool PAIR, class Epi>
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) void dense_turns(
+    DenseIn d, int mt, int nt, Epi epi) {
+    typedef TurnForm<E, TM, TN, WM, LA, LB, PAIR> Form;
+    __shared__ __attribute__((aligned(1024))) char sm[Form::LDS];
+    int m, n;
+    if (!dense_tile(dense_block_number(), mt, nt, m, n)) return;
+    dense_block<Form, E, TM, TN, LA, LB, PAIR>(d, m, n, sm, epi);
+}
+
+template <class E, int TM, int TN, int WM, int LA, int LB, class Epi>
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) void dense_turns2(
+    DenseIn d1, DenseIn d2, int mt1, int nt1, int mt2, int nt2, uint32_t blocks1, Epi epi1,
+    Epi epi2) {
+    typedef TurnForm<E, TM, TN, WM, LA, LB, false> Form;
+    __shared__ __attribute__((aligned(1024))) char sm[Form::LDS];
+    const uint32_t b = dense_block_number();
+    const bool one = b < blocks1;
+    int m, n;
+    if (!dense_tile(one ? b : b - blocks1, one ? mt1 : mt2, one ? nt1 : nt2, m, n)) return;
+    const DenseIn d = one ? d1 : d2;
+    const Epi epi = one ? epi1 : epi2;
+    dense_block<Form, E, TM, TN, LA, LB, false>(d, m, n, sm, epi);
+}
+
+template <class E, int LA, int LB, bool PAIR, class Epi>
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) void dense_pairs(
+    DenseIn d, int mt, int nt, Epi epi) {
+    typedef PairForm<E, LA, LB, PAIR> Form;
+    __shared__ __attribute__((aligned(1024))) char sm[Form::LDS];
+    int m, n;
+    if (!dense_tile(dense_block_number(), mt, nt, m, n)) return;
+    dense_block<Form, E, 128, 128, LA, LB, PAIR>(d, m, n, sm, epi);
+}
+
+template <class E, int LA, int LB, class Epi>
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) void dense_pairs2(
+    DenseIn d1, DenseIn d2, int mt1, int nt1, int mt2, int nt2, uint32_t blocks1, Epi epi1,
+    Epi epi2) {
+    typedef PairForm<E, LA, LB, false> Form;
+    __shared__ __attribute__((aligned(1024))) char sm[Form::LDS];
+    const uint32_t b = dense_block_number();
+    const bool one = b < blocks1;
+    int m, n;
+    if (!dense_tile(one ? b : b - blocks1, one ? mt1 : mt2, one ? nt1 : nt2, m, n)) return;
+    const DenseIn d = one ? d1 : d2;
+    const Epi epi = one ? epi1 : epi2;
+    dense_block<Form, E, 128, 128, LA, LB, false>(d, m, n, sm, epi);
+}
+
 inline int64_t up8(int64_t n) { return (n + 7) / 8 * 8; }
 inline dim3 grid_of(int64_t blocks) {
-    const TileGrid g = tile_grid(blocks);
-    return dim3(g.x, g.y);
+    return blocks <= kDenseRow ? dim3((unsigned)blocks)
+                               : dim3(kDenseRow, (unsigned)((blocks + kDenseRow - 1) / kDenseRow));
 }
 inline int tiles(int64_t n, int t) { return (int)((n + t - 1) / t); }
 
-template <class E, int MF, int TM, int TN, int WM, int LA, int LB, bool PAIR, int S, class Epi>
-void run_tiles(const DenseIn& d, bool dma, const Epi& epi, hipStream_t s) {
+template <class E, int MF, int TM, int TN, int WM, int LA, int LB, bool PAIR, bool DMA, int S,
+          class Epi>
+void run_tiles(const DenseIn& d, const Epi& epi, hipStream_t s) {
     const int mt = tiles(d.rows, TM), nt = tiles(d.cols, PAIR ? TN / 2 : TN);
     if (mt == 0 || nt == 0) return;
-    const dim3 grid = grid_of(up8((int64_t)mt * nt));
-    if (dma)
-        ELB_LAUNCH((dense_tiles<E, MF, TM, TN, WM, LA, LB, PAIR, true, S, Epi>), grid, dim3(256),
-                   0, s, d, mt, nt, epi);
-    else
-        ELB_LAUNCH((dense_tiles<E, MF, TM, TN, WM, LA, LB, PAIR, false, S, Epi>), grid,
-                   dim3(256), 0, s, d, mt, nt, epi);
+    ELB_LAUNCH((dense_tiles<E, MF, TM, TN, WM, LA, LB, PAIR, DMA, S, Epi>),
+               grid_of(up8((int64_t)mt * nt)), dim3(256), 0, s, d, mt, nt, epi);
 }
 
-template <class E, int MF, int TM, int TN, int WM, int LA, int LB, int S, class Epi>
-void run_tiles2(const DenseIn& d1, const DenseIn& d2, bool dma, const Epi& e1, const Epi& e2,
-                hipStream_t s) {
+template <class E, int TM, int TN, int NW, int LB, bool PAIR, int S, class Epi>
+void run_split(const DenseIn& d, const Epi& epi, hipStream_t s) {
+    const int mt = tiles(d.rows, TM), nt = tiles(d.cols, PAIR ? TN / 2 : TN);
+    if (mt == 0 || nt == 0) return;
+    ELB_LAUNCH((dense_split<E, TM, TN, NW, LB, PAIR, S, Epi>), grid_of(up8((int64_t)mt * nt)),
+               dim3(NW * 64), 0, s, d, mt, nt, epi);
+}
+
+template <class E, int TM, int TN, int WM, int LA, int LB, bool PAIR, class Epi>
+void run_turns(const DenseIn& d, const Epi& epi, hipStream_t s) {
+    const int mt = tiles(d.rows, TM), nt = tiles(d.cols, PAIR ? TN / 2 : TN);
+    if (mt == 0 || nt == 0) return;
+    ELB_LAUNCH((dense_turns<E, TM, TN, WM, LA, LB, PAIR, Epi>), grid_of(up8((int64_t)mt * nt)),
+               dim3(512), 0, s, d, mt, nt, epi);
+}
+
+template <class E, int LA, int LB, bool PAIR, class Epi>
+void run_pairs(const DenseIn& d, const Epi& epi, hipStream_t s) {
+    const int mt = tiles(d.rows, 128), nt = tiles(d.cols, PAIR ? 64 : 128);
+    if (mt == 0 || nt == 0) return;
+    ELB_LAUNCH((dense_pairs<E, LA, LB, PAIR, Epi>), grid_of(up8((int64_t)mt * nt)), dim3(512), 0,
+               s, d, mt, nt, epi);
+}
+
+// A product whose first operand has its contraction contiguous, in the form picked for its
+// size.  The forms that copy by 16-byte LDS loads want tensors on 16-byte boundaries (aligned);
+// others take the tile form with ordinary loads.
+template <class E, int LB, bool PAIR, class Epi>
+void run_product(const DenseIn& d, bool aligned, const Epi& epi, hipStream_t s) {
+    constexpr bool F = E::SZ == 4;
+    constexpr int MF = F ? 16 : 32, TT = F ? 64 : 128, S = F ? 3 : 2;
+    const FormId form = !aligned ? kTiles
+                                 : pick_form(d.rows, PAIR ? 2 * (int64_t)d.cols : d.cols,
+                                             (d.K * E::SZ + 127) / 128, F);
+    switch (form) {
+        case kSplit16x16: return run_split<E, 16, 16, 8, LB, PAIR, 4>(d, epi, s);
+        case kSplit16x32: return run_split<E, 16, 32, 8, LB, PAIR, 3>(d, epi, s);
+        case kSplit16x64: return run_split<E, 16, 64, 4, LB, PAIR, 3>(d, epi, s);
+        case kSplit32x32: return run_split<E, 32, 32, 8, LB, PAIR, 2>(d, epi, s);
+        case kSplit32x64: return run_split<E, 32, 64, 4, LB, PAIR, 3>(d, epi, s);
+        case kSplit64x64: return run_split<E, 64, 64, 4, LB, PAIR, 2>(d, epi, s);
+        default: break;
+    }
+    if constexpr (!F) {
+        if (form == kPairs) return run_pairs<E, KC, LB, PAIR>(d, epi, s);
+        if (form == kTurns) return run_turns<E, 256, 256, 2, KC, LB, PAIR>(d, epi, s);
+        run_tiles<E, MF, TT, TT, 2, KC, LB, PAIR, false, S>(d, epi, s);
+    } else {
+        if (aligned) run_tiles<E, MF, TT, TT, 2, KC, LB, PAIR, true, S>(d, epi, s);
+        else run_tiles<E, MF, TT, TT, 2, KC, LB, PAIR, false, S>(d, epi, s);
+    }
+}
+
+// Two products of one kind, both operands down the rows (KR), in one launch.
+template <int TM, int TN, class Kernel, class Epi>
+void launch2(Kernel kernel, int threads, const DenseIn& d1, const DenseIn& d2, const Epi& e1,
+             const Epi& e2, hipStream_t s) {
     const int mt1 = tiles(d1.rows, TM), nt1 = tiles(d1.cols, TN);
     const int mt2 = tiles(d2.rows, TM), nt2 = tiles(d2.cols, TN);
-    const int64_t b1 = up8((int64_t)mt1 * nt1);
-    const int64_t blocks = b1 + up8((int64_t)mt2 * nt2);
+    const int64_t b1 = up8((int64_t)mt1 * nt1), blocks = b1 + up8((int64_t)mt2 * nt2);
     if (blocks == 0) return;
-    const dim3 grid = grid_of(blocks);
-    if (dma)
-        ELB_LAUNCH((dense_tiles2<E, MF, TM, TN, WM, LA, LB, true, S, Epi>), grid, dim3(256), 0, s,
-                   d1, d2, mt1, nt1, mt2, nt2, b1, e1, e2);
-    else
-        ELB_LAUNCH((dense_tiles2<E, MF, TM, TN, WM, LA, LB, false, S, Epi>), grid, dim3(256), 0,
-                   s, d1, d2, mt1, nt1, mt2, nt2, b1, e1, e2);
+    ELB_LAUNCH(kernel, grid_of(blocks), dim3(threads), 0, s, d1, d2, mt1, nt1, mt2, nt2,
+               (uint32_t)b1, e1, e2);
+}
+
+template <class E, class Epi>
+void run_product2(const DenseIn& d1, const DenseIn& d2, bool aligned, const Epi& e1,
+                  const Epi& e2, hipStream_t s) {
+    if constexpr (E::SZ == 4) {
+        if (aligned)
+            launch2<64, 64>(dense_tiles2<E, 16, 64, 64, 2, KR, KR, true, 3, Epi>, 256, d1, d2, e1,
+                            e2, s);
+        else
+            launch2<64, 64>(dense_tiles2<E, 16, 64, 64, 2, KR, KR, false, 3, Epi>, 256, d1, d2,
+                            e1, e2, s);
+    } else {
+        auto time = [&](const FormCost& f) {
+            return form_time(f, form_tiles(f, d1.rows, d1.cols) + form_tiles(f, d2.rows, d2.cols),
+                             (d1.K * E::SZ + 127) / 128, true);
+        };
+        if (!aligned)
+            launch2<128, 128>(dense_tiles2<E, 32, 128, 128, 2, KR, KR, false, 2, Epi>, 256, d1,
+                              d2, e1, e2, s);
+        else if (time(kFormCosts[kPairs]) <= time(kFormCosts[kTurns]))
+            launch2<128, 128>(dense_pairs2<E, KR, KR, Epi>, 512, d1, d2, e1, e2, s);
+        else
+            launch2<256, 256>(dense_turns2<E, 256, 256, 2, KR, KR, Epi>, 512, d1, d2, e1, e2, s);
+    }
 }
 
 }  // namespace

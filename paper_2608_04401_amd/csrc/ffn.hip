@@ -76,15 +76,11 @@ struct GateGradOut {  // from dh, g and u: dg and du [T, 2m], h [T, m]
 
 template <class E, class T>
 struct Block {
-    static constexpr int MF = E::SZ == 2 ? 32 : 16;
-    static constexpr int TT = E::SZ == 2 ? 128 : 64;  // block tile
-    static constexpr int S = E::SZ == 2 ? 2 : 3;
-
-    template <int LA, int LB, bool PAIR, class Epi>
+    template <int LB, bool PAIR, class Epi>
     static void product(const void* a, int64_t lda, const void* b, int64_t ldb, int64_t rows,
                         int cols, int64_t K, const Epi& epi, hipStream_t s) {
         const DenseIn d{(const char*)a, (const char*)b, lda * E::SZ, ldb * E::SZ, rows, cols, K};
-        run_tiles<E, MF, TT, TT, 2, LA, LB, PAIR, S>(d, aligned16(a, b), epi, s);
+        run_product<E, LB, PAIR>(d, aligned16(a, b), epi, s);
     }
 
     static hipError_t forward(const void* x, const void* Wgu, const void* Wd, const void* res,
@@ -92,11 +88,11 @@ struct Block {
                               hipStream_t s) {
         {
             ProfileScope prof("ffn_gate_up", s);
-            product<KC, KC, true>(x, d, Wgu, d, T_, m, d, GateOut<T>{(T*)h, keep, m}, s);
+            product<KC, true>(x, d, Wgu, d, T_, m, d, GateOut<T>{(T*)h, keep, m}, s);
             if (hipError_t e = hipGetLastError()) return e;
         }
         ProfileScope prof("ffn_down", s);
-        product<KC, KC, false>(h, m, Wd, m, T_, d, m, PlainOut<T>{(T*)y, (const T*)res, d}, s);
+        product<KC, false>(h, m, Wd, m, T_, d, m, PlainOut<T>{(T*)y, (const T*)res, d}, s);
         return hipGetLastError();
     }
 
@@ -105,13 +101,13 @@ struct Block {
                                void* dx, void* dWgu, void* dWd, hipStream_t s) {
         {
             ProfileScope prof("ffn_dh", s);
-            product<KC, KR, false>(dy, d, Wd, m, T_, m, d,
+            product<KR, false>(dy, d, Wd, m, T_, m, d,
                                    GateGradOut<T>{keep, (T*)dgu, (T*)h, m}, s);
             if (hipError_t e = hipGetLastError()) return e;
         }
         if (dx) {
             ProfileScope prof("ffn_dx", s);
-            product<KC, KR, false>(dgu, 2 * (int64_t)m, Wgu, d, T_, d, 2 * (int64_t)m,
+            product<KR, false>(dgu, 2 * (int64_t)m, Wgu, d, T_, d, 2 * (int64_t)m,
                                    PlainOut<T>{(T*)dx, nullptr, d}, s);
             if (hipError_t e = hipGetLastError()) return e;
         }
@@ -121,9 +117,8 @@ struct Block {
                             (int64_t)d * E::SZ, dWgu ? 2 * (int64_t)m : 0, d, T_};
             const DenseIn b{(const char*)dy, (const char*)h, (int64_t)d * E::SZ,
                             (int64_t)m * E::SZ, dWd ? d : 0, m, T_};
-            run_tiles2<E, MF, TT, TT, 2, KR, KR, S>(
-                a, b, aligned16(dy, x), PlainOut<T>{(T*)dWgu, nullptr, d},
-                PlainOut<T>{(T*)dWd, nullptr, m}, s);
+            run_product2<E>(a, b, aligned16(dy, x), PlainOut<T>{(T*)dWgu, nullptr, d},
+                            PlainOut<T>{(T*)dWd, nullptr, m}, s);
         }
         return hipGetLastError();
     }

@@ -32,7 +32,7 @@ template <class T>
 __global__ __launch_bounds__(kQuantThreads) void quantize_rows(const T* __restrict__ x, int64_t d,
                                                                int64_t rows, int8_t* __restrict__ q,
                                                                float* __restrict__ scale) {
-    const int64_t row = (int64_t)blockIdx.y * kTileGridRow + blockIdx.x;
+    const int64_t row = dense_block_number();
     if (row >= rows) return;
     const T* const xr = x + row * d;
     const int tid = threadIdx.x;
@@ -144,8 +144,7 @@ struct ScaledGateOut {
 template <class T>
 hipError_t quantize(const void* x, int64_t rows, int d, int8_t* q, float* scale, hipStream_t s) {
     ProfileScope prof("quantize_rows", s);
-    const TileGrid g = tile_grid(rows);
-    ELB_LAUNCH(quantize_rows<T>, dim3(g.x, g.y), dim3(kQuantThreads), 0, s, (const T*)x,
+    ELB_LAUNCH(quantize_rows<T>, grid_of(rows), dim3(kQuantThreads), 0, s, (const T*)x,
                (int64_t)d, rows, q, scale);
     return hipGetLastError();
 }
@@ -154,7 +153,7 @@ template <bool PAIR, class Epi>
 void product(const int8_t* a, const int8_t* w, int64_t rows, int cols, int64_t K, const Epi& epi,
              hipStream_t s) {
     const DenseIn d{(const char*)a, (const char*)w, K, K, rows, cols, K};
-    run_tiles<I8, 32, 128, 128, 2, KC, KC, PAIR, 2>(d, aligned16(a, w), epi, s);
+    run_product<I8, KC, PAIR>(d, aligned16(a, w), epi, s);
 }
 
 }  // namespace
