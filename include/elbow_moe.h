@@ -344,9 +344,9 @@ int elb_gemm_i8(const int8_t *q, const float *scale, const int8_t *W, const floa
 
 /*
  * elb_quantize_rows and elb_gemm_i8 in one call, for activations x [T, k] of dtype.
- *   workspace  at least elb_linear_i8_workspace_bytes(T, k) bytes; y must not alias x
+ *   workspace  at least elb_linear_i8_workspace_bytes(T, n, k) bytes; y must not alias x
  */
-size_t elb_linear_i8_workspace_bytes(int64_t T, int32_t k);
+size_t elb_linear_i8_workspace_bytes(int64_t T, int32_t n, int32_t k);
 int elb_linear_i8(const void *x, const int8_t *W, const float *W_scale, const void *residual,
                   int64_t T, int32_t n, int32_t k, int32_t dtype, void *y, void *workspace,
                   size_t workspace_bytes, void *stream);

@@ -79,7 +79,7 @@ def lib():
         "elb_ffn_backward": ([P, P, P, P, P, I64, I32, I32, I32, P, P, P, P, SZ, P], C.c_int),
         "elb_quantize_rows": ([P, I64, I32, I32, P, P, P], C.c_int),
         "elb_gemm_i8": ([P, P, P, P, P, I64, I32, I32, I32, P, P], C.c_int),
-        "elb_linear_i8_workspace_bytes": ([I64, I32], SZ),
+        "elb_linear_i8_workspace_bytes": ([I64, I32, I32], SZ),
         "elb_linear_i8": ([P, P, P, P, I64, I32, I32, I32, P, P, SZ, P], C.c_int),
         "elb_ffn_i8_workspace_bytes": ([I64, I32, I32], SZ),
         "elb_ffn_forward_i8": ([P, P, P, P, P, P, I64, I32, I32, I32, P, P, SZ, P], C.c_int),
@@ -518,8 +518,8 @@ def elb_gemm_i8(q, scale, W, W_scale, dtype: torch.dtype = torch.bfloat16, resid
 
 
 @functools.lru_cache(maxsize=256)
-def elb_linear_i8_workspace_bytes(T: int, k: int) -> int:
-    return int(lib().elb_linear_i8_workspace_bytes(T, k))
+def elb_linear_i8_workspace_bytes(T: int, n: int, k: int) -> int:
+    return int(lib().elb_linear_i8_workspace_bytes(T, n, k))
 
 
 def elb_linear_i8(x, W, W_scale, residual=None, out=None) -> torch.Tensor:
@@ -534,7 +534,7 @@ def elb_linear_i8(x, W, W_scale, residual=None, out=None) -> torch.Tensor:
     _want("out", out, (T, n), x.dtype)
     y = torch.empty((T, n), dtype=x.dtype, device=x.device) if out is None else out
     stream = _stream()
-    ws = workspace(elb_linear_i8_workspace_bytes(T, k), x.device, stream)
+    ws = workspace(elb_linear_i8_workspace_bytes(T, n, k), x.device, stream)
     _check("elb_linear_i8", lib().elb_linear_i8(
         _ptr(x), _ptr(W), _ptr(W_scale), _ptr(residual), T, n, k, dt, _ptr(y), _ptr(ws),
         ws.numel(), stream))

@@ -174,7 +174,7 @@ int check_i8_k(int k, const char* name) {
 
 // sub-buffers of the int8 block's workspace
 struct I8Layout {
-    size_t xq, xs, h, hq, hs, total;
+    size_t xq, xs, h, hq, hs, part, total;
 };
 I8Layout i8_layout(int64_t T, int d, int m) {
     I8Layout L{};
@@ -189,6 +189,7 @@ I8Layout i8_layout(int64_t T, int d, int m) {
     L.h = take((size_t)T * m * 4);
     L.hq = take((size_t)T * m);
     L.hs = take((size_t)T * 4);
+    L.part = take(i8_halves_bytes(T, d, m));
     L.total = o;
     return L;
 }
@@ -654,7 +655,7 @@ int elb_pack_expert_weights(const void* W_gate_up, const void* W_down, int32_t N
 
 size_t elb_ffn_workspace_bytes(int64_t T, int32_t d, int32_t m, int32_t dtype) {
     if (T < 0 || d < 1 || m < 1 || (dtype != ELB_F32 && dtype != ELB_BF16)) return 0;
-    return align_up((size_t)T * m * esize(dtype));
+    return align_up((size_t)T * m * esize(dtype)) + ffn_halves_bytes(T, d, m, dtype);
 }
 
 int elb_ffn_forward(const void* x, const void* W_gate_up, const void* W_down,
@@ -669,14 +670,16 @@ int elb_ffn_forward(const void* x, const void* W_gate_up, const void* W_down,
     if (int rc = check_workspace(workspace, workspace_bytes,
                                  elb_ffn_workspace_bytes(T, d, m, dtype)))
         return rc;
+    char* const part = (char*)workspace + align_up((size_t)T * m * esize(dtype));
     return hip_status(launch_ffn_forward(x, W_gate_up, W_down, residual, T, d, m, dtype, workspace,
-                                         gate_up, y, (hipStream_t)stream),
+                                         part, gate_up, y, (hipStream_t)stream),
                       "ffn_forward");
 }
 
 size_t elb_ffn_backward_workspace_bytes(int64_t T, int32_t d, int32_t m, int32_t dtype) {
     if (T < 0 || d < 1 || m < 1 || (dtype != ELB_F32 && dtype != ELB_BF16)) return 0;
-    return align_up((size_t)T * m * esize(dtype)) + align_up((size_t)T * 2 * m * esize(dtype));
+    return align_up((size_t)T * m * esize(dtype)) + align_up((size_t)T * 2 * m * esize(dtype)) +
+           ffn_halves_bytes(T, d, 2 * (int64_t)m, dtype);
 }
 
 int elb_ffn_backward(const void* dy, const void* x, const void* W_gate_up, const void* W_down,
@@ -693,10 +696,11 @@ int elb_ffn_backward(const void* dy, const void* x, const void* W_gate_up, const
         if (int rc = check_workspace(workspace, workspace_bytes,
                                      elb_ffn_backward_workspace_bytes(T, d, m, dtype)))
             return rc;
-    char* const ws = (char*)workspace;
-    return hip_status(launch_ffn_backward(dy, x, W_gate_up, W_down, gate_up, T, d, m, dtype,
-                                          T > 0 ? ws + align_up((size_t)T * m * esize(dtype)) : ws,
-                                          ws, dx, dW_gate_up, dW_down, (hipStream_t)stream),
+    char* const h = (char*)workspace;  // (T = 0: not read or written, and may be null)
+    char* const dgu = h ? h + align_up((size_t)T * m * esize(dtype)) : nullptr;
+    char* const part = h ? dgu + align_up((size_t)T * 2 * m * esize(dtype)) : nullptr;
+    return hip_status(launch_ffn_backward(dy, x, W_gate_up, W_down, gate_up, T, d, m, dtype, dgu, h,
+                                          part, dx, dW_gate_up, dW_down, (hipStream_t)stream),
                       "ffn_backward");
 }
 
@@ -726,9 +730,9 @@ int elb_gemm_i8(const int8_t* q, const float* scale, const int8_t* W, const floa
                       "gemm_i8");
 }
 
-size_t elb_linear_i8_workspace_bytes(int64_t T, int32_t k) {
-    if (T < 0 || k < 1) return 0;
-    return align_up((size_t)T * k) + align_up((size_t)T * 4);
+size_t elb_linear_i8_workspace_bytes(int64_t T, int32_t n, int32_t k) {
+    if (T < 0 || n < 1 || k < 1) return 0;
+    return align_up((size_t)T * k) + align_up((size_t)T * 4) + i8_halves_bytes(T, n, k);
 }
 
 int elb_linear_i8(const void* x, const int8_t* W, const float* W_scale, const void* residual,
@@ -740,14 +744,16 @@ int elb_linear_i8(const void* x, const int8_t* W, const float* W_scale, const vo
     if (int rc = check_i8_k(k, "k")) return rc;
     if (T == 0) return ELB_OK;
     if (!x || !W || !W_scale || !y) return fail(ELB_ERR_INVALID_ARG, "NULL tensor pointer");
-    if (int rc = check_workspace(workspace, workspace_bytes, elb_linear_i8_workspace_bytes(T, k)))
+    if (int rc = check_workspace(workspace, workspace_bytes, elb_linear_i8_workspace_bytes(T, n, k)))
         return rc;
     int8_t* const q = (int8_t*)workspace;
     float* const scale = (float*)((char*)workspace + align_up((size_t)T * k));
+    char* const part = (char*)scale + align_up((size_t)T * 4);
     hipStream_t s = (hipStream_t)stream;
-    if (int rc = hip_status(launch_quantize_rows(x, T, k, dtype, q, scale, s), "quantize_rows"))
+    if (int rc = hip_status(launch_quantize_rows(x, T, k, dtype, q, scale, s, part, n),
+                            "quantize_rows"))
         return rc;
-    return hip_status(launch_gemm_i8(q, scale, W, W_scale, residual, T, n, k, dtype, y, s),
+    return hip_status(launch_gemm_i8(q, scale, W, W_scale, residual, T, n, k, dtype, y, s, part),
                       "gemm_i8");
 }
 
@@ -780,9 +786,12 @@ int elb_ffn_forward_i8(const void* x, const int8_t* W_gate_up, const float* gate
     if (int rc = hip_status(launch_gate_up_i8(xq, xs, W_gate_up, gate_up_scale, T, d, m, h, s),
                             "gate_up_i8"))
         return rc;
-    if (int rc = hip_status(launch_quantize_rows(h, T, m, ELB_F32, hq, hs, s), "quantize_rows"))
+    char* const part = ws + L.part;
+    if (int rc = hip_status(launch_quantize_rows(h, T, m, ELB_F32, hq, hs, s, part, d),
+                            "quantize_rows"))
         return rc;
-    return hip_status(launch_gemm_i8(hq, hs, W_down, down_scale, residual, T, d, m, dtype, y, s),
+    return hip_status(launch_gemm_i8(hq, hs, W_down, down_scale, residual, T, d, m, dtype, y, s,
+                                     part),
                       "gemm_i8");
 }
 

@@ -187,19 +187,24 @@ hipError_t launch_combine(const void* Y, const int* k, const int* inv, const flo
                           const void* residual, int64_t T, int d, int K, int dtype, void* y,
                           hipStream_t s);
 
-// the dense gated feed-forward block (ffn.hip).  Scratch: h [T, m], dgu [T, 2m], both dtype
+// the dense gated feed-forward block (ffn.hip).  Scratch: h [T, m], dgu [T, 2m], both dtype; part
+// of ffn_halves_bytes for the product with the down weights (K = m), backward that for dx (K = 2m)
+size_t ffn_halves_bytes(int64_t T, int d, int64_t K, int dtype);
 hipError_t launch_ffn_forward(const void* x, const void* Wgu, const void* Wd, const void* res,
-                              int64_t T, int d, int m, int dtype, void* h, float* gate_up, void* y,
-                              hipStream_t s);
+                              int64_t T, int d, int m, int dtype, void* h, void* part,
+                              float* gate_up, void* y, hipStream_t s);
 hipError_t launch_ffn_backward(const void* dy, const void* x, const void* Wgu, const void* Wd,
                                const float* gate_up, int64_t T, int d, int m, int dtype, void* dgu,
-                               void* h, void* dx, void* dWgu, void* dWd, hipStream_t s);
-// 8-bit products (ffn_i8.hip)
+                               void* h, void* part, void* dx, void* dWgu, void* dWd,
+                               hipStream_t s);
+// 8-bit products (ffn_i8.hip).  part: scratch of i8_halves_bytes for the product [T, k] x [n, k],
+// whose counters the quantisation of its tokens clears; or null
+size_t i8_halves_bytes(int64_t T, int n, int k);
 hipError_t launch_quantize_rows(const void* x, int64_t rows, int d, int dtype, int8_t* q,
-                                float* scale, hipStream_t s);
+                                float* scale, hipStream_t s, void* part = nullptr, int n = 0);
 hipError_t launch_gemm_i8(const int8_t* a, const float* a_scale, const int8_t* w,
                           const float* w_scale, const void* res, int64_t T, int n, int k,
-                          int dtype, void* y, hipStream_t s);
+                          int dtype, void* y, hipStream_t s, void* part = nullptr);
 hipError_t launch_gate_up_i8(const int8_t* a, const float* a_scale, const int8_t* w,
                              const float* w_scale, int64_t T, int d, int m, float* h,
                              hipStream_t s);

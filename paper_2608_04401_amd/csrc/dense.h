@@ -318,6 +318,9 @@ struct TileIn {
     int rows, cols;
     int64_t K;
     int t0, t1;
+    char* part;       // TurnForm with HALVES: the tile's two partial results,
+    uint32_t* count;  // the number of them that are written,
+    int half;         // and the one that is this block's
 };
 
 // ------------------------------------------------------------------------------------------
@@ -407,8 +410,16 @@ struct TileForm {
         const int l = lane & (MF - 1), g = lane / MF;
         const int cc = lane % CPR, r0 = lane / CPR;
         const int col = wn * OC + cc * 8;
+        constexpr int NP = (MF + RPI - 1) / RPI;
 #pragma unroll
         for (int i = 0; i < FM; ++i) {
+            typename Epi::Extra extra[NP];
+#pragma unroll
+            for (int p = 0; p < NP; ++p) {
+                const int r = r0 + p * RPI, row = wm * WTM + i * MF + r;
+                if ((RPI <= MF || r < MF) && row < in.rows && col < in.cols)
+                    epi.fetch(row, col, extra[p]);
+            }
 #pragma unroll
             for (int j = 0; j < FN; ++j)
 #pragma unroll
@@ -420,18 +431,17 @@ struct TileForm {
                 }
             __builtin_amdgcn_wave_barrier();
 #pragma unroll
-            for (int p = 0; p < (MF + RPI - 1) / RPI; ++p) {
-                const int r = r0 + p * RPI;
-                if (RPI > MF && r >= MF) break;
-                const int row = wm * WTM + i * MF + r;
+            for (int p = 0; p < NP; ++p) {
+                const int r = r0 + p * RPI, row = wm * WTM + i * MF + r;
+                if ((RPI > MF && r >= MF) || row >= in.rows || col >= in.cols) continue;
                 float v[8];
                 read8(stg + r * PITCH + cc * 32, v, a1{});
                 if constexpr (PAIR) {
                     float v2[8];
                     read8(stg + r * PITCH + (OC + cc * 8) * 4, v2, a1{});
-                    if (row < in.rows && col < in.cols) epi.put(row, col, v, v2);
+                    epi.put(row, col, v, v2, extra[p]);
                 } else {
-                    if (row < in.rows && col < in.cols) epi.put(row, col, v);
+                    epi.put(row, col, v, extra[p]);
                 }
             }
             __builtin_amdgcn_wave_barrier();
@@ -528,13 +538,15 @@ struct SplitForm {
         for (int it = threadIdx.x; it < ITEMS; it += NW * 64) {
             const int row = it / CPR, cc = it % CPR;
             if (row >= in.rows || cc * 8 >= in.cols) continue;
+            typename Epi::Extra extra;
+            epi.fetch(row, cc * 8, extra);
             float v[8], v2[8];
             sum8<a1>(sm + row * PITCH + cc * 32, v);
             if constexpr (PAIR) {
                 sum8<a1>(sm + row * PITCH + (OC + cc * 8) * 4, v2);
-                epi.put(row, cc * 8, v, v2);
+                epi.put(row, cc * 8, v, v2, extra);
             } else {
-                epi.put(row, cc * 8, v);
+                epi.put(row, cc * 8, v, extra);
             }
         }
     }
@@ -570,8 +582,13 @@ struct SplitForm {
 // phases before its first read; the waits leave what is not needed yet in flight: phase 3 needs
 // A0, B0 and B1 of tile t + 1 (issued after them: A1 of it, A0, B0, B1 of t + 2), phase 1 A1 of
 // tile t (after it: A0, B0, B1, A1 of t + 1 and A0 of t + 2).
+// HALVES: two blocks share a tile, each with half of the contraction (two halves of 128 tiles fill the
+// chip where one block each would leave half of it idle).  The block that finds its partner's
+// partial result written adds it to its own and finishes the tile; one that does not writes its
+// own.  Neither waits: where both come at once both write, and the second one to count goes on.  A sum
+// of two does not depend on its order.
 // ------------------------------------------------------------------------------------------
-template <class E, int TM, int TN, int WM, int LA, int LB, bool PAIR>
+template <class E, int TM, int TN, int WM, int LA, int LB, bool PAIR, bool HALVES = false>
 struct TurnForm {
     static constexpr int WN = 8 / WM;
     static constexpr int QM = TM / 2, QN = TN / 2;
@@ -692,19 +709,62 @@ struct TurnForm {
         ELB_WAIT_VMCNT(0);
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 
-        // results through LDS, each wave in its own area: 32 rows of a row half at a time
         typedef typename E::acc1 a1;
         typedef a1 a4 __attribute__((ext_vector_type(4)));
+        if constexpr (HALVES) {
+            static_assert(8 * STAGE + 4 <= LDS, "the flag beside the staging areas");
+            constexpr int NV = 4 * FM * FN * 4;  // 16-byte pieces of a lane's results
+            uint32_t* const flag = reinterpret_cast<uint32_t*>(sm + LDS - 4);
+            auto piece = [&](int half, int i) {
+                return reinterpret_cast<a4*>(in.part + half * (TM * TN * 4)) +
+                       ((w * NV + i) * 64 + lane);
+            };
+            if (threadIdx.x == 0)
+                *flag = __hip_atomic_load(in.count, __ATOMIC_ACQUIRE, __HIP_MEMORY_SCOPE_AGENT);
+            __syncthreads();
+            if (*flag == 0) {
+#pragma unroll
+                for (int i = 0; i < NV; ++i) {
+                    const acc_t& c = acc[i / (8 * FM * FN)][i / (4 * FM * FN) % 2]
+                                        [i / (4 * FN) % FM][i / 4 % FN];
+                    *piece(in.half, i) = a4{c[4 * (i % 4)], c[4 * (i % 4) + 1],
+                                            c[4 * (i % 4) + 2], c[4 * (i % 4) + 3]};
+                }
+                __syncthreads();
+                if (threadIdx.x == 0)  // one wave's release covers the block's stores
+                    *flag = __hip_atomic_fetch_add(in.count, 1u, __ATOMIC_ACQ_REL,
+                                                   __HIP_MEMORY_SCOPE_AGENT);
+                __syncthreads();
+                if (*flag == 0) return;
+            }
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                acc_t& c = acc[i / (8 * FM * FN)][i / (4 * FM * FN) % 2][i / (4 * FN) % FM]
+                              [i / 4 % FN];
+                const a4 v = *piece(1 - in.half, i);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) c[4 * (i % 4) + q] += v[q];
+            }
+        }
+
+        // results through LDS, each wave in its own area: 32 rows of a row half at a time
         char* const stg = sm + w * STAGE;
         constexpr int HC = PN / 8;                    // 8-column chunks of a column half
         constexpr int CPR = PAIR ? HC : 2 * HC, RPI = 64 / CPR;
         const int l = lane & 31, g = lane >> 5;
         const int cc = lane % CPR, r0 = lane / CPR;
         const int col = (cc / HC) * QN + wn * PN + (cc % HC) * 8;
+        constexpr int NP = 32 / RPI;
 #pragma unroll
         for (int a = 0; a < 2; ++a)
 #pragma unroll
             for (int i = 0; i < FM; ++i) {
+                typename Epi::Extra extra[NP];
+#pragma unroll
+                for (int p = 0; p < NP; ++p) {
+                    const int row = a * QM + wm * PM + i * 32 + r0 + p * RPI;
+                    if (row < in.rows && col < in.cols) epi.fetch(row, col, extra[p]);
+                }
 #pragma unroll
                 for (int b = 0; b < 2; ++b)
 #pragma unroll
@@ -718,17 +778,17 @@ struct TurnForm {
                         }
                 __builtin_amdgcn_wave_barrier();
 #pragma unroll
-                for (int p = 0; p < 32 / RPI; ++p) {
-                    const int r = r0 + p * RPI;
-                    const int row = a * QM + wm * PM + i * 32 + r;
+                for (int p = 0; p < NP; ++p) {
+                    const int r = r0 + p * RPI, row = a * QM + wm * PM + i * 32 + r;
+                    if (row >= in.rows || col >= in.cols) continue;
                     float v[8];
                     read8(stg + r * PITCH + cc * 32, v, a1{});
                     if constexpr (PAIR) {
                         float v2[8];
                         read8(stg + r * PITCH + (PN + cc * 8) * 4, v2, a1{});
-                        if (row < in.rows && col < in.cols) epi.put(row, col, v, v2);
+                        epi.put(row, col, v, v2, extra[p]);
                     } else {
-                        if (row < in.rows && col < in.cols) epi.put(row, col, v);
+                        epi.put(row, col, v, extra[p]);
                     }
                 }
                 __builtin_amdgcn_wave_barrier();
@@ -851,6 +911,12 @@ struct PairForm {
         const int cc = lane % CPR, r0 = lane / CPR;
         const int col = wn * OC + cc * 8;
         const char* const stg = sm + (w * 2 + grp) * 2 * STAGE;
+        typename Epi::Extra extra[32 / RPI];
+#pragma unroll
+        for (int p = 0; p < 32 / RPI; ++p) {
+            const int row = wm * 64 + grp * 32 + r0 + p * RPI;
+            if (row < in.rows && col < in.cols) epi.fetch(row, col, extra[p]);
+        }
 #pragma unroll
         for (int p = 0; p < 32 / RPI; ++p) {
             const int r = r0 + p * RPI, row = wm * 64 + grp * 32 + r;
@@ -860,9 +926,9 @@ struct PairForm {
             if constexpr (PAIR) {
                 float v2[8];
                 sum8<a1>(stg + r * PITCH + (32 + cc * 8) * 4, v2);
-                epi.put(row, col, v, v2);
+                epi.put(row, col, v, v2, extra[p]);
             } else {
-                epi.put(row, col, v);
+                epi.put(row, col, v, extra[p]);
             }
         }
     }
@@ -909,11 +975,20 @@ struct DenseIn {
     int64_t rows;
     int cols;
     int64_t K;
+    char* part;       // scratch for kHalves (halves_bytes), or null
+    uint32_t* clear;  // counters of a later product in this call, set to zero here
+    int nclear;
 };
+
+__device__ __forceinline__ void clear_counters(uint32_t* c, int n) {
+    if (c && dense_block_number() == 0)
+        for (int i = threadIdx.x; i < n; i += blockDim.x) c[i] = 0;
+}
 
 template <class Form, class E, int TM, int TN, int LA, int LB, bool PAIR, class Epi>
 __device__ __forceinline__ void dense_block(const DenseIn& d, int m, int n, char* sm,
-                                            const Epi& epi) {
+                                            const Epi& epi, int half = -1, int tile = 0,
+                                            int tiles = 0) {
     constexpr int OC = PAIR ? TN / 2 : TN;
     const int64_t r0 = (int64_t)m * TM;
     const int c0 = n * OC;
@@ -926,30 +1001,57 @@ __device__ __forceinline__ void dense_block(const DenseIn& d, int m, int n, char
     in.rows = d.rows - r0 < TM ? (int)(d.rows - r0) : TM;
     in.cols = d.cols - c0;
     in.K = d.K;
-    in.t0 = 0;
-    in.t1 = (int)((d.K * E::SZ + 127) / 128);
+    const int nk = (int)((d.K * E::SZ + 127) / 128);
+    // with halves the first block takes 8 k-tiles less, so that it has written its partial result
+    // when the second one is done (down product of 4096 tokens, m = 8192: 135 -> 126 us)
+    const int first = nk / 2 - 4 < 0 ? 0 : nk / 2 - 4;
+    in.t0 = half > 0 ? first : 0;
+    in.t1 = half == 0 ? first : nk;
+    in.half = half;
+    in.part = d.part + (int64_t)tile * (2 * kPartialBytes);
+    in.count = reinterpret_cast<uint32_t*>(d.part + (int64_t)tiles * (2 * kPartialBytes)) + tile;
     Form::run(in, sm, epi.at(r0, c0));
 }
 
-// ---- what becomes of a product: put() takes eight columns of a row ----
+// ---- what becomes of a product ----
+// An Epi's fetch(row, col) loads what eight columns of a row need beside the product, and put()
+// computes and stores them.  Block forms fetch for several rows before they put the first: loads
+// do not pass the stores before them, and one at a time each would wait out the memory's latency
+// (dh of 4096 tokens, m = 8192, whose rows need 64 bytes per eight columns: 220 us one at a time).
+struct Nothing {};
+
+template <class T>
+struct Eight {  // eight values of a tensor, as loaded
+    T v[8];
+    __device__ __forceinline__ void load(const T* p) {
+        typedef uint32_t raw_t __attribute__((ext_vector_type(2 * sizeof(T)), aligned(2)));
+        *reinterpret_cast<raw_t*>(v) = *reinterpret_cast<const raw_t*>(p);
+    }
+    __device__ __forceinline__ float operator[](int i) const {
+        if constexpr (sizeof(T) == 2) return bf16_to_f32(v[i]);
+        else return v[i];
+    }
+};
+
 template <class T>
 struct PlainOut {  // y = [res +] v
     T* y;
     const T* res;
     int64_t ld;
+    typedef Eight<T> Extra;
     __device__ __forceinline__ PlainOut at(int64_t r0, int c0) const {
         const int64_t o = r0 * ld + c0;
         return {y + o, res ? res + o : nullptr, ld};
     }
-    __device__ __forceinline__ void put(int row, int col, float (&v)[8]) const {
-        const int64_t o = row * ld + col;
+    __device__ __forceinline__ void fetch(int row, int col, Extra& e) const {
+        if (res) e.load(res + row * ld + col);
+    }
+    __device__ __forceinline__ void put(int row, int col, float (&v)[8], const Extra& e) const {
         if (res) {
-            float r[8];
-            load8(res + o, r);
 #pragma unroll
-            for (int q = 0; q < 8; ++q) v[q] += r[q];
+            for (int q = 0; q < 8; ++q) v[q] += e[q];
         }
-        store8(y + o, v);
+        store8(y + row * ld + col, v);
     }
 };
 
@@ -959,6 +1061,7 @@ template <class E, int MF, int TM, int TN, int WM, int LA, int LB, bool PAIR, bo
 __global__ __launch_bounds__(256) void dense_tiles(DenseIn d, int mt, int nt, Epi epi) {
     typedef TileForm<E, MF, TM, TN, WM, LA, LB, PAIR, DMA, S> Form;
     __shared__ __attribute__((aligned(1024))) char sm[Form::LDS];
+    clear_counters(d.clear, d.nclear);
     int m, n;
     if (!dense_tile(dense_block_number(), mt, nt, m, n)) return;
     dense_block<Form, E, TM, TN, LA, LB, PAIR>(d, m, n, sm, epi);
@@ -987,6 +1090,7 @@ template <class E, int TM, int TN, int NW, int LB, bool PAIR, int S, class Epi>
 __global__ __launch_bounds__(NW * 64) void dense_split(DenseIn d, int mt, int nt, Epi epi) {
     typedef SplitForm<E, TM, TN, NW, LB, PAIR, true, S> Form;
     __shared__ __attribute__((aligned(1024))) char sm[Form::LDS];
+    clear_counters(d.clear, d.nclear);
     int m, n;
     if (!dense_tile(dense_block_number(), mt, nt, m, n)) return;
     dense_block<Form, E, TM, TN, KC, LB, PAIR>(d, m, n, sm, epi);
@@ -997,9 +1101,23 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     DenseIn d, int mt, int nt, Epi epi) {
     typedef TurnForm<E, TM, TN, WM, LA, LB, PAIR> Form;
     __shared__ __attribute__((aligned(1024))) char sm[Form::LDS];
+    clear_counters(d.clear, d.nclear);
     int m, n;
     if (!dense_tile(dense_block_number(), mt, nt, m, n)) return;
     dense_block<Form, E, TM, TN, LA, LB, PAIR>(d, m, n, sm, epi);
+}
+
+// two blocks per tile: tile b / 2 of a numbering in which an XCD's tiles follow each other
+template <class E, int TM, int TN, int WM, int LA, int LB, class Epi>
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) void dense_halves(
+    DenseIn d, int mt, int nt, Epi epi) {
+    typedef TurnForm<E, TM, TN, WM, LA, LB, false, true> Form;
+    __shared__ __attribute__((aligned(1024))) char sm[Form::LDS];
+    const uint32_t b = dense_block_number();
+    const uint32_t half = b >> 3 & 1, b2 = (b >> 4 << 3) + (b & 7);  // both on one XCD
+    int m, n;
+    if (!dense_tile(b2, mt, nt, m, n)) return;
+    dense_block<Form, E, TM, TN, LA, LB, false>(d, m, n, sm, epi, half, m * nt + n, mt * nt);
 }
 
 template <class E, int TM, int TN, int WM, int LA, int LB, class Epi>
@@ -1022,6 +1140,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     DenseIn d, int mt, int nt, Epi epi) {
     typedef PairForm<E, LA, LB, PAIR> Form;
     __shared__ __attribute__((aligned(1024))) char sm[Form::LDS];
+    clear_counters(d.clear, d.nclear);
     int m, n;
     if (!dense_tile(dense_block_number(), mt, nt, m, n)) return;
     dense_block<Form, E, 128, 128, LA, LB, PAIR>(d, m, n, sm, epi);
@@ -1074,6 +1193,26 @@ void run_turns(const DenseIn& d, const Epi& epi, hipStream_t s) {
                dim3(512), 0, s, d, mt, nt, epi);
 }
 
+template <class E, int TM, int TN, int WM, int LA, int LB, class Epi>
+void run_halves(const DenseIn& d, const Epi& epi, hipStream_t s) {
+    const int mt = tiles(d.rows, TM), nt = tiles(d.cols, TN);
+    if (mt == 0 || nt == 0) return;
+    ELB_LAUNCH((dense_halves<E, TM, TN, WM, LA, LB, Epi>),
+               grid_of(2 * up8((int64_t)mt * nt)), dim3(512), 0, s, d, mt, nt, epi);
+}
+
+// the counters of a product's kHalves scratch, or none where another form is picked
+struct Counters {
+    uint32_t* p;
+    int n;
+};
+inline Counters halves_counters(char* part, int64_t rows, int64_t cols, int64_t ktiles,
+                                bool fp32) {
+    if (!part || pick_form(rows, cols, ktiles, fp32, true) != kHalves) return {nullptr, 0};
+    const int64_t n = form_tiles(kFormCosts[kHalves], rows, cols);
+    return {reinterpret_cast<uint32_t*>(part + n * 2 * kPartialBytes), (int)n};
+}
+
 template <class E, int LA, int LB, bool PAIR, class Epi>
 void run_pairs(const DenseIn& d, const Epi& epi, hipStream_t s) {
     const int mt = tiles(d.rows, 128), nt = tiles(d.cols, PAIR ? 64 : 128);
@@ -1091,7 +1230,8 @@ void run_product(const DenseIn& d, bool aligned, const Epi& epi, hipStream_t s) 
     constexpr int MF = F ? 16 : 32, TT = F ? 64 : 128, S = F ? 3 : 2;
     const FormId form = !aligned ? kTiles
                                  : pick_form(d.rows, PAIR ? 2 * (int64_t)d.cols : d.cols,
-                                             (d.K * E::SZ + 127) / 128, F);
+                                             (d.K * E::SZ + 127) / 128, F,
+                                             !PAIR && d.part);
     switch (form) {
         case kSplit16x16: return run_split<E, 16, 16, 8, LB, PAIR, 4>(d, epi, s);
         case kSplit16x32: return run_split<E, 16, 32, 8, LB, PAIR, 3>(d, epi, s);
@@ -1104,6 +1244,8 @@ void run_product(const DenseIn& d, bool aligned, const Epi& epi, hipStream_t s) 
     if constexpr (!F) {
         if (form == kPairs) return run_pairs<E, KC, LB, PAIR>(d, epi, s);
         if (form == kTurns) return run_turns<E, 256, 256, 2, KC, LB, PAIR>(d, epi, s);
+        if constexpr (!PAIR)
+            if (form == kHalves) return run_halves<E, 256, 256, 2, KC, LB>(d, epi, s);
         run_tiles<E, MF, TT, TT, 2, KC, LB, PAIR, false, S>(d, epi, s);
     } else {
         if (aligned) run_tiles<E, MF, TT, TT, 2, KC, LB, PAIR, true, S>(d, epi, s);

@@ -31,7 +31,9 @@ constexpr int kQuantKeep = 4;  // groups of 8 elements that a thread keeps in re
 template <class T>
 __global__ __launch_bounds__(kQuantThreads) void quantize_rows(const T* __restrict__ x, int64_t d,
                                                                int64_t rows, int8_t* __restrict__ q,
-                                                               float* __restrict__ scale) {
+                                                               float* __restrict__ scale,
+                                                               Counters clear) {
+    clear_counters(clear.p, clear.n);
     const int64_t row = dense_block_number();
     if (row >= rows) return;
     const T* const xr = x + row * d;
@@ -98,21 +100,25 @@ struct ScaledOut {  // y = [res +] v s_row c_col
         const int64_t o = r0 * ld + c0;
         return {y + o, res ? res + o : nullptr, s + r0, c + c0, ld};
     }
-    __device__ __forceinline__ void put(int row, int col, float (&v)[8]) const {
+    struct Extra {
+        Eight<float> c;
+        float s;
+        Eight<T> r;
+    };
+    __device__ __forceinline__ void fetch(int row, int col, Extra& e) const {
+        e.c.load(c + col);
+        e.s = s[row];
+        if (res) e.r.load(res + row * ld + col);
+    }
+    __device__ __forceinline__ void put(int row, int col, float (&v)[8], const Extra& e) const {
 #pragma clang fp contract(off)  // the same roundings in every kernel
-        const int64_t o = row * ld + col;
-        float cs[8];
-        load8(c + col, cs);
-        const float sr = s[row];
 #pragma unroll
-        for (int q = 0; q < 8; ++q) v[q] = v[q] * sr * cs[q];
+        for (int q = 0; q < 8; ++q) v[q] = v[q] * e.s * e.c[q];
         if (res) {
-            float r[8];
-            load8(res + o, r);
 #pragma unroll
-            for (int q = 0; q < 8; ++q) v[q] += r[q];
+            for (int q = 0; q < 8; ++q) v[q] += e.r[q];
         }
-        store8(y + o, v);
+        store8(y + row * ld + col, v);
     }
 };
 
@@ -125,55 +131,65 @@ struct ScaledGateOut {
     __device__ __forceinline__ ScaledGateOut at(int64_t r0, int c0) const {
         return {h + r0 * m + c0, s + r0, c + c0, m};
     }
+    struct Extra {
+        Eight<float> g, u;
+        float s;
+    };
+    __device__ __forceinline__ void fetch(int row, int col, Extra& e) const {
+        e.g.load(c + col);
+        e.u.load(c + m + col);
+        e.s = s[row];
+    }
     __device__ __forceinline__ void put(int row, int col, const float (&g)[8],
-                                        const float (&u)[8]) const {
+                                        const float (&u)[8], const Extra& e) const {
 #pragma clang fp contract(off)
-        float cg[8], cu[8], v[8];
-        load8(c + col, cg);
-        load8(c + m + col, cu);
-        const float sr = s[row];
+        float v[8];
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
-            const float gg = g[q] * sr * cg[q];
-            v[q] = gg / (1.0f + expf(-gg)) * (u[q] * sr * cu[q]);
+            const float gg = g[q] * e.s * e.g[q];
+            v[q] = gg / (1.0f + expf(-gg)) * (u[q] * e.s * e.u[q]);
         }
         store8(h + row * m + col, v);
     }
 };
 
 template <class T>
-hipError_t quantize(const void* x, int64_t rows, int d, int8_t* q, float* scale, hipStream_t s) {
+hipError_t quantize(const void* x, int64_t rows, int d, int8_t* q, float* scale, Counters clear,
+                    hipStream_t s) {
     ProfileScope prof("quantize_rows", s);
     ELB_LAUNCH(quantize_rows<T>, grid_of(rows), dim3(kQuantThreads), 0, s, (const T*)x,
-               (int64_t)d, rows, q, scale);
+               (int64_t)d, rows, q, scale, clear);
     return hipGetLastError();
 }
 
 template <bool PAIR, class Epi>
 void product(const int8_t* a, const int8_t* w, int64_t rows, int cols, int64_t K, const Epi& epi,
-             hipStream_t s) {
-    const DenseIn d{(const char*)a, (const char*)w, K, K, rows, cols, K};
+             hipStream_t s, void* part = nullptr) {
+    const DenseIn d{(const char*)a, (const char*)w, K, K, rows, cols, K, (char*)part, nullptr, 0};
     run_product<I8, KC, PAIR>(d, aligned16(a, w), epi, s);
 }
 
 }  // namespace
 
+size_t i8_halves_bytes(int64_t T, int n, int k) { return halves_bytes(T, n, (k + 127) / 128, false); }
+
 hipError_t launch_quantize_rows(const void* x, int64_t rows, int d, int dtype, int8_t* q,
-                                float* scale, hipStream_t s) {
-    return dtype == ELB_BF16 ? quantize<bf16_t>(x, rows, d, q, scale, s)
-                             : quantize<float>(x, rows, d, q, scale, s);
+                                float* scale, hipStream_t s, void* part, int n) {
+    const Counters c = halves_counters((char*)part, rows, n, (d + 127) / 128, false);
+    return dtype == ELB_BF16 ? quantize<bf16_t>(x, rows, d, q, scale, c, s)
+                             : quantize<float>(x, rows, d, q, scale, c, s);
 }
 
 hipError_t launch_gemm_i8(const int8_t* a, const float* a_scale, const int8_t* w,
                           const float* w_scale, const void* res, int64_t T, int n, int k,
-                          int dtype, void* y, hipStream_t s) {
+                          int dtype, void* y, hipStream_t s, void* part) {
     ProfileScope prof("gemm_i8", s);
     if (dtype == ELB_BF16)
         product<false>(a, w, T, n, k, ScaledOut<bf16_t>{(bf16_t*)y, (const bf16_t*)res, a_scale,
-                                                        w_scale, n}, s);
+                                                        w_scale, n}, s, part);
     else
         product<false>(a, w, T, n, k, ScaledOut<float>{(float*)y, (const float*)res, a_scale,
-                                                       w_scale, n}, s);
+                                                       w_scale, n}, s, part);
     return hipGetLastError();
 }
 

@@ -7,11 +7,14 @@
 //   512 rows, 2048 columns, int8 k = 2048:  64 x 64 split 7.5, pairs 11.5, turns 26.3;
 //   2048 rows: 24.8, 14.1, 28.3;  2048 rows, 8192 columns: 89.8, 52.9, 38.2;
 //   64 rows, 2048 columns: 32 x 32 split 4.9, 32 x 64 5.9, 64 x 64 6.8, 16 x 16 (two rounds) 7.6.
-// Over 144 such products the choice is 0.3 % slower than the best form on average, 13 % at worst
+//   4096 rows, 2048 columns (128 turns tiles, 512 pairs tiles): bf16 of 128 k-tiles pairs 146,
+//   halves 126, of 256 k-tiles 303 and 228; int8 of 64 k-tiles pairs 72, halves 85.
+// Over 144 such products the choice (without halves) is 0.3 % slower than the best form on average, 13 % at worst
 // (fp32, 128 products: 0.4 % and 10 %).
 // Usable from host code without HIP (for tests).
 #pragma once
 
+#include <stddef.h>
 #include <stdint.h>
 
 namespace elb {
@@ -20,6 +23,7 @@ enum FormId {
     kSplit16x16, kSplit16x32, kSplit16x64, kSplit32x32, kSplit32x64, kSplit64x64,
     kPairs,  // 128 x 128, two groups of waves taking the k-tiles in turn (bf16, int8)
     kTurns,  // 256 x 256, two groups of waves taking turns at the units (bf16, int8)
+    kHalves, // the same, two blocks per tile, half of the contraction each (bf16, int8)
     kTiles,  // 64 x 64 (fp32); 128 x 128 for tensors off a 16-byte boundary (bf16, int8)
     kForms
 };
@@ -27,6 +31,7 @@ enum FormId {
 struct FormCost {
     int tm, tn, ways;  // ways: k-tiles in work at a time
     float start, round, iter;
+    int blocks = 1;    // per tile
 };
 
 // bf16 and int8: a k-tile's copies, LDS reads and matrix cycles are the same
@@ -34,36 +39,45 @@ constexpr FormCost kFormCosts[kForms] = {
     {16, 16, 8, 1.7f, 2.5f, 0.32f},  {16, 32, 8, 1.55f, 2.5f, 0.46f},
     {16, 64, 4, 1.4f, 2.45f, 0.37f}, {32, 32, 8, 1.4f, 2.4f, 0.60f},
     {32, 64, 4, 1.35f, 2.8f, 0.45f}, {64, 64, 4, 1.25f, 3.3f, 0.59f},
-    {128, 128, 2, 0.0f, 5.4f, 0.76f}, {256, 256, 1, 0.0f, 7.7f, 1.10f}, {0, 0, 0, 0, 0, 0}};
+    {128, 128, 2, 0.0f, 5.4f, 0.76f}, {256, 256, 1, 0.0f, 7.7f, 1.10f},
+    {256, 256, 2, 0.0f, 30.f, 1.10f, 2}, {0, 0, 0, 0, 0, 0}};
 constexpr FormCost kFormCostsF32[kForms] = {
     {16, 16, 8, 1.75f, 2.95f, 0.38f}, {16, 32, 8, 1.7f, 2.95f, 0.65f},
     {16, 64, 4, 1.5f, 2.8f, 0.66f},   {32, 32, 8, 1.55f, 2.85f, 1.17f},
     {32, 64, 4, 1.35f, 3.25f, 1.14f}, {64, 64, 4, 1.15f, 3.65f, 2.09f},
     {0, 0, 0, 0, 0, 0},               {0, 0, 0, 0, 0, 0},
-    {64, 64, 1, 2.6f, 1.15f, 0.52f}};
+    {0, 0, 0, 0, 0, 0},               {64, 64, 1, 2.6f, 1.15f, 0.52f}};
 
 inline int64_t form_tiles(const FormCost& f, int64_t rows, int64_t cols) {
     return ((rows + f.tm - 1) / f.tm) * ((cols + f.tn - 1) / f.tn);
 }
 
 inline float form_time(const FormCost& f, int64_t tiles, int64_t ktiles, bool whole_rounds) {
-    const float r = tiles <= 256 ? 1.0f
-                    : whole_rounds ? (float)((tiles + 255) / 256) : (float)tiles / 256.0f;
+    const int64_t n = tiles * f.blocks;
+    const float r = n <= 256 ? 1.0f : whole_rounds ? (float)((n + 255) / 256) : (float)n / 256.0f;
     return f.start + r * (f.round + f.iter * (float)((ktiles + f.ways - 1) / f.ways));
 }
 
 // the form for a rows x cols product (cols: rows of the second operand) of that many k-tiles;
-// with fp32 set, of fp32
-inline FormId pick_form(int64_t rows, int64_t cols, int64_t ktiles, bool fp32) {
+// with fp32 set, of fp32; halves: whether there is scratch for kHalves (halves_bytes)
+inline FormId pick_form(int64_t rows, int64_t cols, int64_t ktiles, bool fp32, bool halves) {
     int best = -1;
     float least = 0;
     for (int i = 0; i < kForms; ++i) {
         const FormCost& f = (fp32 ? kFormCostsF32 : kFormCosts)[i];
-        if (!f.ways) continue;
+        if (!f.ways || (i == kHalves && !halves)) continue;
         const float t = form_time(f, form_tiles(f, rows, cols), ktiles, i != kTiles);
         if (best < 0 || t < least) best = i, least = t;
     }
     return (FormId)best;
+}
+
+// scratch of a product that may take kHalves: per tile the two blocks' fp32 (int32) partial tiles,
+// then a counter; 0 where another form is picked
+constexpr int64_t kPartialBytes = 256 * 256 * 4;
+inline size_t halves_bytes(int64_t rows, int64_t cols, int64_t ktiles, bool fp32) {
+    if (pick_form(rows, cols, ktiles, fp32, true) != kHalves) return 0;
+    return (size_t)form_tiles(kFormCosts[kHalves], rows, cols) * (2 * kPartialBytes + 4);
 }
 
 }  // namespace elb

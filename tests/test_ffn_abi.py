@@ -96,12 +96,12 @@ def test_workspace_sizes():
     assert L.elb_ffn_workspace_bytes(100, 64, 48, 1) >= 100 * 48 * 2
     assert L.elb_ffn_workspace_bytes(100, 64, 48, 0) >= 100 * 48 * 4
     assert L.elb_ffn_backward_workspace_bytes(100, 64, 48, 1) >= 100 * 48 * 3 * 2
-    assert L.elb_linear_i8_workspace_bytes(100, 64) >= 100 * 64 + 400
+    assert L.elb_linear_i8_workspace_bytes(100, 48, 64) >= 100 * 64 + 400
     assert L.elb_ffn_i8_workspace_bytes(100, 64, 48) >= 100 * (64 + 48 * 5 + 8)
     for f, args in ((L.elb_ffn_workspace_bytes, (-1, 64, 48, 1)),
                     (L.elb_ffn_workspace_bytes, (1, 64, 48, 9)),
                     (L.elb_ffn_backward_workspace_bytes, (1, 0, 48, 1)),
-                    (L.elb_linear_i8_workspace_bytes, (-1, 48)),
+                    (L.elb_linear_i8_workspace_bytes, (-1, 48, 48)),
                     (L.elb_ffn_i8_workspace_bytes, (1, 64, 0))):
         assert f(*args) == 0
 
