@@ -414,18 +414,26 @@ def elb_moe_forward_prepared(x, W_router, W_gate_up, W_down, K: int = 8, eps: fl
     return call, y
 
 
-def _want(name: str, t: Optional[torch.Tensor], shape, dtype: torch.dtype):
-    """t: None, or a contiguous tensor of that shape and type on the current device."""
-    if t is None:
+def _want(name: str, t: Optional[torch.Tensor], shape, dtype: torch.dtype, device: int):
+    """t: None, or a contiguous tensor of that shape and type on the current device (_device())."""
+    if t is None or (t.dtype is dtype and t.shape == shape and t.is_contiguous()
+                     and t.get_device() == device):
         return
-    if not t.is_cuda or t.get_device() != torch._C._cuda_getDevice():
+    if t.get_device() != device:
         raise ValueError("%s must be on the current GPU" % name)
     if t.dtype != dtype:
         raise TypeError("%s must be %s, not %s" % (name, dtype, t.dtype))
     if t.shape != shape:
         raise ValueError("%s must have shape %s, not %s" % (name, tuple(shape), tuple(t.shape)))
-    if not t.is_contiguous():
-        raise ValueError("%s must be contiguous" % name)
+    raise ValueError("%s must be contiguous" % name)
+
+
+def _device(*ts) -> int:
+    """The current device's index (tensors on the CPU are refused before it is asked for)."""
+    for t in ts:
+        if not t.is_cuda:
+            raise ValueError("tensors must be on the GPU")
+    return torch._C._cuda_getDevice()
 
 
 def _matrix(name: str, t: torch.Tensor):
@@ -435,14 +443,15 @@ def _matrix(name: str, t: torch.Tensor):
 
 
 def _ffn_dims(x, W_gate_up, W_down):
-    """(T, d, m, dtype code) of the dense block; its operands checked."""
+    """(T, d, m, dtype code, device) of the dense block; its operands checked."""
     T, d = _matrix("x", x)
     m = _matrix("W_down", W_down)[1]
     dt = _dtype_code(x)
-    _want("x", x, (T, d), x.dtype)
-    _want("W_gate_up", W_gate_up, (2 * m, d), x.dtype)
-    _want("W_down", W_down, (d, m), x.dtype)
-    return T, d, m, dt
+    dev = _device(x)
+    _want("x", x, (T, d), x.dtype, dev)
+    _want("W_gate_up", W_gate_up, (2 * m, d), x.dtype, dev)
+    _want("W_down", W_down, (d, m), x.dtype, dev)
+    return T, d, m, dt, dev
 
 
 @functools.lru_cache(maxsize=256)
@@ -453,9 +462,9 @@ def elb_ffn_workspace_bytes(T: int, d: int, m: int, dtype: int) -> int:
 def elb_ffn_forward(x, W_gate_up, W_down, residual=None, out=None, keep: bool = False):
     """The dense gated feed-forward block.  -> y, or with keep=True (y, gate_up): gate_up
     [T, 2m] float32 is what elb_ffn_backward needs of the forward pass."""
-    T, d, m, dt = _ffn_dims(x, W_gate_up, W_down)
-    _want("residual", residual, (T, d), x.dtype)
-    _want("out", out, (T, d), x.dtype)
+    T, d, m, dt, dev = _ffn_dims(x, W_gate_up, W_down)
+    _want("residual", residual, (T, d), x.dtype, dev)
+    _want("out", out, (T, d), x.dtype, dev)
     y = torch.empty_like(x) if out is None else out
     gate_up = torch.empty((T, 2 * m), dtype=torch.float32, device=x.device) if keep else None
     stream = _stream()
@@ -474,9 +483,9 @@ def elb_ffn_backward_workspace_bytes(T: int, d: int, m: int, dtype: int) -> int:
 def elb_ffn_backward(dy, x, W_gate_up, W_down, gate_up, need=(True, True, True)):
     """-> (dx, dW_gate_up, dW_down), None where need is false; gate_up from
     elb_ffn_forward(..., keep=True)."""
-    T, d, m, dt = _ffn_dims(x, W_gate_up, W_down)
-    _want("dy", dy, (T, d), x.dtype)
-    _want("gate_up", gate_up, (T, 2 * m), torch.float32)
+    T, d, m, dt, dev = _ffn_dims(x, W_gate_up, W_down)
+    _want("dy", dy, (T, d), x.dtype, dev)
+    _want("gate_up", gate_up, (T, 2 * m), torch.float32, dev)
     dx, dWgu, dWd = (torch.empty_like(t) if n else None
                      for t, n in zip((x, W_gate_up, W_down), need))
     stream = _stream()
@@ -491,7 +500,7 @@ def elb_quantize_rows(x: torch.Tensor):
     """-> (q [T, d] int8, scale [T] float32): q scale[:, None] stands for x"""
     T, d = _matrix("x", x)
     dt = _dtype_code(x)
-    _want("x", x, (T, d), x.dtype)
+    _want("x", x, (T, d), x.dtype, _device(x))
     q = torch.empty((T, d), dtype=torch.int8, device=x.device)
     scale = torch.empty(T, dtype=torch.float32, device=x.device)
     _check("elb_quantize_rows", lib().elb_quantize_rows(_ptr(x), T, d, dt, _ptr(q), _ptr(scale),
@@ -504,12 +513,13 @@ def elb_gemm_i8(q, scale, W, W_scale, dtype: torch.dtype = torch.bfloat16, resid
     """y [T, n] of dtype (bfloat16 or float32) from q [T, k] int8 and W [n, k] int8."""
     T, k = _matrix("q", q)
     n = _matrix("W", W)[0]
-    _want("q", q, (T, k), torch.int8)
-    _want("scale", scale, (T,), torch.float32)
-    _want("W", W, (n, k), torch.int8)
-    _want("W_scale", W_scale, (n,), torch.float32)
-    _want("residual", residual, (T, n), dtype)
-    _want("out", out, (T, n), dtype)
+    dev = _device(q)
+    _want("q", q, (T, k), torch.int8, dev)
+    _want("scale", scale, (T,), torch.float32, dev)
+    _want("W", W, (n, k), torch.int8, dev)
+    _want("W_scale", W_scale, (n,), torch.float32, dev)
+    _want("residual", residual, (T, n), dtype, dev)
+    _want("out", out, (T, n), dtype, dev)
     y = torch.empty((T, n), dtype=dtype, device=q.device) if out is None else out
     _check("elb_gemm_i8", lib().elb_gemm_i8(
         _ptr(q), _ptr(scale), _ptr(W), _ptr(W_scale), _ptr(residual), T, n, k, _dtype_code(y),
@@ -527,11 +537,12 @@ def elb_linear_i8(x, W, W_scale, residual=None, out=None) -> torch.Tensor:
     T, k = _matrix("x", x)
     n = _matrix("W", W)[0]
     dt = _dtype_code(x)
-    _want("x", x, (T, k), x.dtype)
-    _want("W", W, (n, k), torch.int8)
-    _want("W_scale", W_scale, (n,), torch.float32)
-    _want("residual", residual, (T, n), x.dtype)
-    _want("out", out, (T, n), x.dtype)
+    dev = _device(x)
+    _want("x", x, (T, k), x.dtype, dev)
+    _want("W", W, (n, k), torch.int8, dev)
+    _want("W_scale", W_scale, (n,), torch.float32, dev)
+    _want("residual", residual, (T, n), x.dtype, dev)
+    _want("out", out, (T, n), x.dtype, dev)
     y = torch.empty((T, n), dtype=x.dtype, device=x.device) if out is None else out
     stream = _stream()
     ws = workspace(elb_linear_i8_workspace_bytes(T, n, k), x.device, stream)
@@ -553,13 +564,14 @@ def elb_ffn_forward_i8(x, W_gate_up, gate_up_scale, W_down, down_scale, residual
     T, d = _matrix("x", x)
     m = _matrix("W_down", W_down)[1]
     dt = _dtype_code(x)
-    _want("x", x, (T, d), x.dtype)
-    _want("W_gate_up", W_gate_up, (2 * m, d), torch.int8)
-    _want("gate_up_scale", gate_up_scale, (2 * m,), torch.float32)
-    _want("W_down", W_down, (d, m), torch.int8)
-    _want("down_scale", down_scale, (d,), torch.float32)
-    _want("residual", residual, (T, d), x.dtype)
-    _want("out", out, (T, d), x.dtype)
+    dev = _device(x)
+    _want("x", x, (T, d), x.dtype, dev)
+    _want("W_gate_up", W_gate_up, (2 * m, d), torch.int8, dev)
+    _want("gate_up_scale", gate_up_scale, (2 * m,), torch.float32, dev)
+    _want("W_down", W_down, (d, m), torch.int8, dev)
+    _want("down_scale", down_scale, (d,), torch.float32, dev)
+    _want("residual", residual, (T, d), x.dtype, dev)
+    _want("out", out, (T, d), x.dtype, dev)
     y = torch.empty_like(x) if out is None else out
     stream = _stream()
     ws = workspace(elb_ffn_i8_workspace_bytes(T, d, m), x.device, stream)

@@ -749,12 +749,9 @@ int elb_linear_i8(const void* x, const int8_t* W, const float* W_scale, const vo
     int8_t* const q = (int8_t*)workspace;
     float* const scale = (float*)((char*)workspace + align_up((size_t)T * k));
     char* const part = (char*)scale + align_up((size_t)T * 4);
-    hipStream_t s = (hipStream_t)stream;
-    if (int rc = hip_status(launch_quantize_rows(x, T, k, dtype, q, scale, s, part, n),
-                            "quantize_rows"))
-        return rc;
-    return hip_status(launch_gemm_i8(q, scale, W, W_scale, residual, T, n, k, dtype, y, s, part),
-                      "gemm_i8");
+    return hip_status(launch_linear_i8(x, dtype, W, W_scale, residual, T, n, k, dtype, y, q, scale,
+                                       part, (hipStream_t)stream),
+                      "linear_i8");
 }
 
 size_t elb_ffn_i8_workspace_bytes(int64_t T, int32_t d, int32_t m) {
@@ -781,18 +778,13 @@ int elb_ffn_forward_i8(const void* x, const int8_t* W_gate_up, const float* gate
     float *const xs = (float*)(ws + L.xs), *const hs = (float*)(ws + L.hs);
     float* const h = (float*)(ws + L.h);
     hipStream_t s = (hipStream_t)stream;
-    if (int rc = hip_status(launch_quantize_rows(x, T, d, dtype, xq, xs, s), "quantize_rows"))
-        return rc;
-    if (int rc = hip_status(launch_gate_up_i8(xq, xs, W_gate_up, gate_up_scale, T, d, m, h, s),
+    if (int rc = hip_status(launch_gate_up_i8(x, dtype, W_gate_up, gate_up_scale, T, d, m, h, xq,
+                                              xs, s),
                             "gate_up_i8"))
         return rc;
-    char* const part = ws + L.part;
-    if (int rc = hip_status(launch_quantize_rows(h, T, m, ELB_F32, hq, hs, s, part, d),
-                            "quantize_rows"))
-        return rc;
-    return hip_status(launch_gemm_i8(hq, hs, W_down, down_scale, residual, T, d, m, dtype, y, s,
-                                     part),
-                      "gemm_i8");
+    return hip_status(launch_linear_i8(h, ELB_F32, W_down, down_scale, residual, T, d, m, dtype, y,
+                                       hq, hs, ws + L.part, s),
+                      "linear_i8");
 }
 
 int64_t elb_calibrate_mfma_bf16(int32_t blocks, int32_t iters, float* out, void* stream) {

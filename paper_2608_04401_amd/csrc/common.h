@@ -205,8 +205,14 @@ hipError_t launch_quantize_rows(const void* x, int64_t rows, int d, int dtype, i
 hipError_t launch_gemm_i8(const int8_t* a, const float* a_scale, const int8_t* w,
                           const float* w_scale, const void* res, int64_t T, int n, int k,
                           int dtype, void* y, hipStream_t s, void* part = nullptr);
-hipError_t launch_gate_up_i8(const int8_t* a, const float* a_scale, const int8_t* w,
-                             const float* w_scale, int64_t T, int d, int m, float* h,
+// float rows x [T, k] of type `in`, quantised on the way (scratch q [T, k], scale [T], part), times
+// w [n, k], to type `out`
+hipError_t launch_linear_i8(const void* x, int in, const int8_t* w, const float* w_scale,
+                            const void* res, int64_t T, int n, int k, int out, void* y, int8_t* q,
+                            float* scale, void* part, hipStream_t s);
+// h = silu(gate) up, fp32, of x [T, d] quantised on the way (scratch q [T, d], scale [T])
+hipError_t launch_gate_up_i8(const void* x, int dtype, const int8_t* w, const float* w_scale,
+                             int64_t T, int d, int m, float* h, int8_t* q, float* scale,
                              hipStream_t s);
 
 // calibration: back-to-back bf16 MFMAs, blocks x 4 waves x iters x 8 of them; out [blocks * 4]

@@ -449,6 +449,62 @@ struct TileForm {
     }
 };
 
+// The end of a split form: the waves' partial TM x TN tiles, summed in LDS in the order of the
+// contraction.
+template <class E, int TM, int TN, int NW, bool PAIR>
+struct SplitJoin {
+    static constexpr int FM = TM / 16, FN = TN / 16;
+    static constexpr int PITCH = TN * 4 + 16;
+    static constexpr int PART = TM * PITCH;  // a wave's partial tile
+    typedef typename Mma<E, 16>::acc acc_t;
+
+    template <class Epi>
+    static __device__ __forceinline__ void run(const acc_t (&acc)[FM][FN], const TileIn& in,
+                                               char* sm, int lane, int w, const Epi& epi) {
+        typedef typename E::acc1 a1;
+        typedef a1 a4 __attribute__((ext_vector_type(4)));
+        ELB_WAIT_VMCNT(0);
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        const int l16 = lane & 15, hq = lane >> 4;
+        char* const part = sm + w * PART;
+#pragma unroll
+        for (int i = 0; i < FM; ++i)
+#pragma unroll
+            for (int j = 0; j < FN; ++j)
+                *reinterpret_cast<a4*>(part + (16 * i + l16) * PITCH + (16 * j + 4 * hq) * 4) =
+                    acc[i][j];
+        __syncthreads();
+        constexpr int OC = PAIR ? TN / 2 : TN;
+        constexpr int CPR = OC / 8, ITEMS = TM * CPR;
+        for (int it = threadIdx.x; it < ITEMS; it += NW * 64) {
+            const int row = it / CPR, cc = it % CPR;
+            if (row >= in.rows || cc * 8 >= in.cols) continue;
+            typename Epi::Extra extra;
+            epi.fetch(row, cc * 8, extra);
+            float v[8], v2[8];
+            sum8<a1>(sm + row * PITCH + cc * 32, v);
+            if constexpr (PAIR) {
+                sum8<a1>(sm + row * PITCH + (OC + cc * 8) * 4, v2);
+                epi.put(row, cc * 8, v, v2, extra);
+            } else {
+                epi.put(row, cc * 8, v, extra);
+            }
+        }
+    }
+    template <class a1>
+    static __device__ __forceinline__ void sum8(const char* p, float (&v)[8]) {
+        typedef a1 a4 __attribute__((ext_vector_type(4)));
+        a4 a = *reinterpret_cast<const a4*>(p), b = *reinterpret_cast<const a4*>(p + 16);
+#pragma unroll
+        for (int w = 1; w < NW; ++w) {
+            a += *reinterpret_cast<const a4*>(p + w * PART);
+            b += *reinterpret_cast<const a4*>(p + w * PART + 16);
+        }
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[q] = (float)a[q], v[q + 4] = (float)b[q];
+    }
+};
+
 // ------------------------------------------------------------------------------------------
 // Block form 2, for few rows: NW waves take a share of the contraction each, every one of them
 // the whole TM x TN tile, with a ring of S k-tiles of its own and no barrier in the loop; their
@@ -460,8 +516,7 @@ struct SplitForm {
     static constexpr int FM = TM / 16, FN = TN / 16;
     static constexpr int AU = TM * 128, BU = TN * 128;
     static constexpr int WRING = S * (AU + BU);  // a wave's ring
-    static constexpr int PITCH = TN * 4 + 16;
-    static constexpr int PART = TM * PITCH;      // a wave's partial tile
+    static constexpr int PART = SplitJoin<E, TM, TN, NW, PAIR>::PART;
     static constexpr int LDS = NW * (WRING > PART ? WRING : PART);
     typedef typename Mma<E, 16>::acc acc_t;
     typedef Copier<KC, TM, E::SZ, 1, false, DMA> CA;
@@ -469,8 +524,6 @@ struct SplitForm {
 
     template <class Epi>
     static __device__ __forceinline__ void run(const TileIn& in, char* sm, const Epi& epi) {
-        typedef typename E::acc1 a1;
-        typedef a1 a4 __attribute__((ext_vector_type(4)));
         const int lane = threadIdx.x & 63;
         const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         CA ca;
@@ -522,45 +575,7 @@ struct SplitForm {
                         acc[i][j] = Mma<E, 16>::mma(fb[ks][j], fa[ks][i], acc[i][j]);
             u = u + 1 == S ? 0 : u + 1;
         }
-        ELB_WAIT_VMCNT(0);
-        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-        const int l16 = lane & 15, hq = lane >> 4;
-        char* const part = sm + w * PART;
-#pragma unroll
-        for (int i = 0; i < FM; ++i)
-#pragma unroll
-            for (int j = 0; j < FN; ++j)
-                *reinterpret_cast<a4*>(part + (16 * i + l16) * PITCH + (16 * j + 4 * hq) * 4) =
-                    acc[i][j];
-        __syncthreads();
-        constexpr int OC = PAIR ? TN / 2 : TN;
-        constexpr int CPR = OC / 8, ITEMS = TM * CPR;
-        for (int it = threadIdx.x; it < ITEMS; it += NW * 64) {
-            const int row = it / CPR, cc = it % CPR;
-            if (row >= in.rows || cc * 8 >= in.cols) continue;
-            typename Epi::Extra extra;
-            epi.fetch(row, cc * 8, extra);
-            float v[8], v2[8];
-            sum8<a1>(sm + row * PITCH + cc * 32, v);
-            if constexpr (PAIR) {
-                sum8<a1>(sm + row * PITCH + (OC + cc * 8) * 4, v2);
-                epi.put(row, cc * 8, v, v2, extra);
-            } else {
-                epi.put(row, cc * 8, v, extra);
-            }
-        }
-    }
-    template <class a1>
-    static __device__ __forceinline__ void sum8(const char* p, float (&v)[8]) {
-        typedef a1 a4 __attribute__((ext_vector_type(4)));
-        a4 a = *reinterpret_cast<const a4*>(p), b = *reinterpret_cast<const a4*>(p + 16);
-#pragma unroll
-        for (int w = 1; w < NW; ++w) {
-            a += *reinterpret_cast<const a4*>(p + w * PART);
-            b += *reinterpret_cast<const a4*>(p + w * PART + 16);
-        }
-#pragma unroll
-        for (int q = 0; q < 4; ++q) v[q] = (float)a[q], v[q + 4] = (float)b[q];
+        SplitJoin<E, TM, TN, NW, PAIR>::run(acc, in, sm, lane, w, epi);
     }
 };
 
@@ -1011,6 +1026,22 @@ __device__ __forceinline__ void dense_block(const DenseIn& d, int m, int n, char
     in.part = d.part + (int64_t)tile * (2 * kPartialBytes);
     in.count = reinterpret_cast<uint32_t*>(d.part + (int64_t)tiles * (2 * kPartialBytes)) + tile;
     Form::run(in, sm, epi.at(r0, c0));
+}
+
+// sigma(g) = 1 / (1 + e^-g) to about two units in the last place of fp32: e^-g = 2^t 2^r with t the
+// rounded product -g log2 e and r what its rounding left off (below 2^-17 for |g| < 2^7), 2^r =
+// 1 + r ln 2.  A g below -88 makes 2^t infinite and sigma zero.  (The library's exponential and
+// division take five times the instructions: gate/up of 4096 tokens, m = 8192, int8, 162 us with
+// them.)
+__device__ __forceinline__ float sigma_f32(float g) {
+    constexpr float kLog2e = 1.44269504f, kLog2eRest = 1.92596299e-8f, kLn2 = 0.69314718f;
+    const float t = -g * kLog2e;
+    const float r = fmaf(-g, kLog2eRest, fmaf(-g, kLog2e, -t));
+    return __builtin_amdgcn_rcpf(fmaf(__builtin_amdgcn_exp2f(t), fmaf(r, kLn2, 1.0f), 1.0f));
+}
+// where the result is rounded to bf16: the hardware's exponential as it is
+__device__ __forceinline__ float sigma_bf16(float g) {
+    return __builtin_amdgcn_rcpf(1.0f + __expf(-g));
 }
 
 // ---- what becomes of a product ----

@@ -16,11 +16,8 @@ namespace elb {
 
 namespace {
 
-// e^-g: the hardware exponential where the result is rounded to bf16, the exact one for fp32
-__device__ __forceinline__ float exp_neg(float g, bf16_t) { return __expf(-g); }
-__device__ __forceinline__ float exp_neg(float g, float) { return expf(-g); }
-__device__ __forceinline__ float recip(float v, bf16_t) { return __builtin_amdgcn_rcpf(v); }
-__device__ __forceinline__ float recip(float v, float) { return 1.0f / v; }
+__device__ __forceinline__ float sigma(float g, bf16_t) { return sigma_bf16(g); }
+__device__ __forceinline__ float sigma(float g, float) { return sigma_f32(g); }
 
 // ---- what becomes of the products' results ----
 template <class T>
@@ -38,7 +35,7 @@ struct GateOut {  // h = silu(g) u; keep [T, 2m] fp32: g and u for the backward
         float v[8];
 #pragma unroll
         for (int q = 0; q < 8; ++q)
-            v[q] = g[q] * recip(1.0f + exp_neg(g[q], T()), T()) * u[q];
+            v[q] = g[q] * sigma(g[q], T()) * u[q];
         store8(h + row * m + col, v);
         if (keep) {
             store8(keep + row * 2 * m + col, g);
@@ -71,7 +68,7 @@ struct GateGradOut {  // from dh, g and u: dg and du [T, 2m], h [T, m]
         float dg[8], du[8], hh[8];
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
-            const float s = recip(1.0f + exp_neg(g[q], T()), T());
+            const float s = sigma(g[q], T());
             const float gs = g[q] * s;
             dg[q] = dh[q] * u[q] * (s + gs * (1.0f - s));
             du[q] = dh[q] * gs;

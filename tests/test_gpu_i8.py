@@ -125,6 +125,8 @@ def test_gemm_i8_unaligned(T, which):
 @pytest.mark.parametrize("T,n,k", [(1, 528, 1040), (5, 2048, 2048), (16, 512, 2048),
                                    (17, 64, 512), (40, 2048, 2048), (200, 272, 2064),
                                    (3, 64, 20000), (1030, 512, 8208),
+                                   (2, 512, 2048), (2, 512, 2064), (64, 1040, 2048),
+                                   (64, 1040, 2064), (100, 512, 1040), (20, 8208, 1040),
                                    (2500, 2064, 12304)])
 def test_linear_i8(T, n, k, dtype):
     """The two steps in one call: their bits, and the definition's values."""
