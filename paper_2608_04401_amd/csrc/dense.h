@@ -677,7 +677,6 @@ struct TurnForm {
             __builtin_amdgcn_sched_barrier(0);
         };
         auto products = [&](int a, int b) {
-            __builtin_amdgcn_s_setprio(1);
 #pragma unroll
             for (int k = 0; k < KS; ++k)
 #pragma unroll
@@ -686,7 +685,6 @@ struct TurnForm {
                     for (int j = 0; j < FN; ++j)
                         acc[a][b][i][j] =
                             Mma<E, MF>::mma(fb[b][j][k], fa[i][k], acc[a][b][i][j]);
-            __builtin_amdgcn_s_setprio(0);
             __builtin_amdgcn_sched_barrier(0);
             asm volatile("s_barrier" ::: "memory");
             __builtin_amdgcn_sched_barrier(0);
@@ -747,8 +745,11 @@ struct TurnForm {
                     const acc_t& c = acc[i / (2 * FM * FN)][i / (FM * FN) % 2][i / FN % FM][i % FN];
                     *piece(in.half, i) = c;
                 }
+                // every wave's stores have reached L2 before the barrier; then one wave's release
+                // (which writes L2 back) covers them all (by all eight waves: 35 us more)
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
                 __syncthreads();
-                if (threadIdx.x == 0)  // one wave's release covers the block's stores
+                if (threadIdx.x == 0)
                     *flag = __hip_atomic_fetch_add(in.count, 1u, __ATOMIC_ACQ_REL,
                                                    __HIP_MEMORY_SCOPE_AGENT);
                 __syncthreads();
@@ -1063,6 +1064,7 @@ struct Eight {  // eight values of a tensor, as loaded
 
 template <class T>
 struct PlainOut {  // y = [res +] v
+    static constexpr bool kMayHalve = true;  // its products may take kHalves
     T* y;
     const T* res;
     int64_t ld;
@@ -1259,7 +1261,7 @@ void run_product(const DenseIn& d, bool aligned, const Epi& epi, hipStream_t s) 
     const FormId form = !aligned ? kTiles
                                  : pick_form(d.rows, PAIR ? 2 * (int64_t)d.cols : d.cols,
                                              (d.K * E::SZ + 127) / 128, F,
-                                             !PAIR && d.part);
+                                             Epi::kMayHalve && d.part);
     switch (form) {
         case kSplit16x16: return run_split<E, 16, 16, 8, LB, PAIR, 4>(d, epi, s);
         case kSplit16x32: return run_split<E, 16, 32, 8, LB, PAIR, 3>(d, epi, s);
@@ -1272,7 +1274,7 @@ void run_product(const DenseIn& d, bool aligned, const Epi& epi, hipStream_t s) 
     if constexpr (!F) {
         if (form == kPairs) return run_pairs<E, KC, LB, PAIR>(d, epi, s);
         if (form == kTurns) return run_turns<E, 256, 256, 2, KC, LB, PAIR>(d, epi, s);
-        if constexpr (!PAIR)
+        if constexpr (Epi::kMayHalve)
             if (form == kHalves) return run_halves<E, 256, 256, 2, KC, LB>(d, epi, s);
         run_tiles<E, MF, TT, TT, 2, KC, LB, PAIR, false, S>(d, epi, s);
     } else {

@@ -22,6 +22,7 @@ __device__ __forceinline__ float sigma(float g, float) { return sigma_f32(g); }
 // ---- what becomes of the products' results ----
 template <class T>
 struct GateOut {  // h = silu(g) u; keep [T, 2m] fp32: g and u for the backward
+    static constexpr bool kMayHalve = false;
     T* h;
     float* keep;
     int64_t m;
@@ -46,6 +47,7 @@ struct GateOut {  // h = silu(g) u; keep [T, 2m] fp32: g and u for the backward
 
 template <class T>
 struct GateGradOut {  // from dh, g and u: dg and du [T, 2m], h [T, m]
+    static constexpr bool kMayHalve = false;
     const float* keep;
     T* dgu;
     T* h;

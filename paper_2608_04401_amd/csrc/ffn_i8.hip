@@ -262,6 +262,7 @@ __global__ __launch_bounds__(NW * 64) void dense_quant(DenseIn d, int mt, int nt
 
 template <class T>
 struct ScaledOut {  // y = [res +] v s_row c_col
+    static constexpr bool kMayHalve = true;
     T* y;
     const T* res;
     const float *s, *c;
@@ -295,6 +296,7 @@ struct ScaledOut {  // y = [res +] v s_row c_col
 // h = silu(g) u in fp32: rounded to bf16 first, one h in eight would move to the next whole number
 // when it is quantised (2^-9 of a value is up to a quarter of a step)
 struct ScaledGateOut {
+    static constexpr bool kMayHalve = false;
     float* h;
     const float *s, *c;  // c: m scales of the gate rows, then m of the up rows
     int64_t m;
@@ -328,8 +330,9 @@ hipError_t quantize(const void* x, int64_t rows, int d, int8_t* q, float* scale,
                     hipStream_t s) {
     ProfileScope prof("quantize_rows", s);
     // a wave per row where its lanes can keep it and the rows fill the chip (us, wave / block a row:
-    // 65536 x 512 24.5 / 60.9, 16384 x 2048 23.0 / 24.8, 8192 x 1024 9.6 / 11.8, 300 x 2048 8.7 / 4.1)
-    if (d <= 2048 && rows >= 4096)
+    // 65536 x 512 24.5 / 60.9, 16384 x 2048 23.0 / 24.8, 8192 x 1024 9.6 / 11.8, 4096 x 2048 12.4 /
+    // 10.2, 300 x 2048 8.7 / 4.1)
+    if (d <= 2048 && rows >= 8192)
         ELB_LAUNCH((quantize_rows<T, 64>), grid_of((rows + 3) / 4), dim3(256), 0, s, (const T*)x,
                    (int64_t)d, rows, q, scale, clear);
     else
@@ -425,7 +428,7 @@ hipError_t launch_quantize_rows(const void* x, int64_t rows, int d, int dtype, i
 hipError_t launch_gemm_i8(const int8_t* a, const float* a_scale, const int8_t* w,
                           const float* w_scale, const void* res, int64_t T, int n, int k,
                           int dtype, void* y, hipStream_t s, void* part) {
-    ProfileScope prof("gemm_i8", s);
+    ProfileScope prof("product_i8", s);
     if (dtype == ELB_BF16)
         product<false>(a, w, T, n, k, ScaledOut<bf16_t>{(bf16_t*)y, (const bf16_t*)res, a_scale,
                                                         w_scale, n}, s, part);

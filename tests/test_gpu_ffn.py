@@ -231,6 +231,36 @@ def test_two_streams_at_once():
             assert all(torch.equal(a, b) for a, b in zip(g, want[i]))
 
 
+def test_tiles_of_two_blocks():
+    """Products whose tiles two blocks share, whichever ends first: the same bits call after call,
+    alone and beside the same product on another stream, and as captured."""
+    T, d, m = 2500, 2064, 6160
+    x, Wgu, Wd, res, dy = _inputs(T, d, m, "bf16", 11)
+
+    def step():
+        y, keep = B.elb_ffn_forward(x, Wgu, Wd, residual=res, keep=True)
+        return y, B.elb_ffn_backward(dy, x, Wgu, Wd, keep, need=(True, False, False))[0]
+    want = step()
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = []
+    for _ in range(6):
+        for s in streams:
+            with torch.cuda.stream(s):
+                got.append(step())
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step()
+    for _ in range(3):
+        graph.replay()
+        got.append(step())
+        torch.cuda.synchronize()
+        got.append([t.clone() for t in out])
+    for g in got:
+        assert all(torch.equal(a, b) for a, b in zip(g, want))
+
+
 def test_beside_the_routed_experts():
     """A layer with a shared expert: the routed experts' output is the block's residual."""
     T, d, N, m = 300, 256, 16, 128
