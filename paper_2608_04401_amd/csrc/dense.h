@@ -586,17 +586,24 @@ struct SplitForm {
 // QM x QN; a wave owns the same QM / WM x QN / WN piece of each.  A k-tile is then four phases, each
 // a quadrant:
 //     phase   LDS reads           copies issued       matrix products
-//       0     A0, B0 (tile t)     A1 (tile t + 1)     A0 B0
-//       1     B1                  A0 (tile t + 2)     A0 B1
-//       2     A1                  B0 (tile t + 2)     A1 B1
-//       3     -                   B1 (tile t + 2)     A1 B0
+//       0     A0 (tile t)         A1 (tile t + 1)     A0 BF
+//       1     BG                  A0 (tile t + 2)     A0 BG
+//       2     A1                  BF (tile t + 2)     A1 BG
+//       3     BG (tile t + 1)     BG (tile t + 2)     A1 BF
+// AHEAD, where A's contraction is contiguous: F is 0 in even k-tiles and 1 in odd ones, G = 1 - F, so
+// that the half of B that a k-tile starts with is read in phase 3 before, where its registers
+// have just become free.  Otherwise F is always 0, and phase 0 reads BF too, phase 3 nothing (us,
+// otherwise / AHEAD: gate and up of 4096 tokens, m = 8192 250 / 244, their down product 127 / 121;
+// both weight gradients, which read A and B down the rows with twice the instructions, 332 / 357).
 // Each half of a phase (reads and copies; products) ends with a barrier of all waves; the second
 // group starts one half later.  A unit is overwritten (by the copies of two k-tiles later, two
 // buffers) at the earliest two halves after its last read by the first group, one after that by
-// the second, whose reads are waited for before its barrier.  Every unit is copied six or seven
-// phases before its first read; the waits leave what is not needed yet in flight: phase 3 needs
-// A0, B0 and B1 of tile t + 1 (issued after them: A1 of it, A0, B0, B1 of t + 2), phase 1 A1 of
-// tile t (after it: A0, B0, B1, A1 of t + 1 and A0 of t + 2).
+// the second, whose reads are waited for before its barrier.  Every unit is copied five to seven
+// phases before its first read; the waits leave what is not needed yet in flight.  Copies are
+// issued, and arrive, in the order ... A0, BF, BG (tile t + 1; phases 1, 2, 3 of tile t - 1), A1
+// (phase 0 of tile t), A0, BF, BG (t + 2) ...  Phase 1 waits for A1 of tile t (five units are later);
+// AHEAD, phase 0 for BG of tile t (five), phase 2 for the first half of B of tile t + 1, and with
+// it its A0 (four); otherwise phase 3 for A0, BF and BG of tile t + 1 (four).
 // HALVES: two blocks share a tile, each with half of the contraction (two halves of 128 tiles fill the
 // chip where one block each would leave half of it idle).  The block that finds its partner's
 // partial result written adds it to its own and finishes the tile; one that does not writes its
@@ -606,9 +613,14 @@ struct SplitForm {
 // The 16 x 16 MFMAs run it faster than the 32 x 32 ones of the same rate (us, 32 / 16: 4096 x 16384 x
 // 2048 with SwiGLU 227 / 211, 8192 x 4096 x 8192 442 / 403, int8 of twice the depth 456 / 410).
 // ------------------------------------------------------------------------------------------
+template <int V>
+struct Half {
+    static constexpr int value = V;
+};
 template <class E, int TM, int TN, int WM, int LA, int LB, bool PAIR, bool HALVES = false>
 struct TurnForm {
     static constexpr int MF = 16, KS = 2;  // MFMA rows and columns, k-steps of a k-tile
+    static constexpr bool AHEAD = LA == KC;
     static constexpr int WN = 8 / WM;
     static constexpr int QM = TM / 2, QN = TN / 2;
     static constexpr int PM = QM / WM, PN = QN / WN;  // a wave's piece of a quadrant
@@ -691,36 +703,46 @@ struct TurnForm {
         };
 
         const int t0 = in.t0;
+        auto buffer = [&](int t) { return sm + ((t - t0) & 1) * BUF; };
+        auto tile = [&](int t, auto first) {
+            constexpr int F = decltype(first)::value, G = 1 - F;
+            const char* const buf = buffer(t);
+            if (!AHEAD) read_b(buf + 2 * AU, F);
+            read_a(buf);
+            copy_a(1, t + 1);
+            if (AHEAD) ELB_WAIT_VMCNT(3 * CA::N + 2 * CB::N);
+            half();
+            products(0, F);
+            read_b(buf + 2 * AU + G * BU, G);
+            copy_a(0, t + 2);
+            ELB_WAIT_VMCNT(3 * CA::N + 2 * CB::N);
+            half();
+            products(0, G);
+            read_a(buf + AU);
+            copy_b(F, t + 2);
+            if (AHEAD) ELB_WAIT_VMCNT(2 * CA::N + 2 * CB::N);
+            half();
+            products(1, G);
+            if (AHEAD) read_b(buffer(t + 1) + 2 * AU + G * BU, G);
+            copy_b(G, t + 2);
+            if (!AHEAD) ELB_WAIT_VMCNT(2 * CA::N + 2 * CB::N);
+            half();
+            products(1, F);
+        };
         copy_a(0, t0);
         copy_b(0, t0);
         copy_b(1, t0);
         copy_a(1, t0);
         copy_a(0, t0 + 1);
-        copy_b(0, t0 + 1);
-        copy_b(1, t0 + 1);
+        copy_b(AHEAD, t0 + 1);
+        copy_b(!AHEAD, t0 + 1);
         ELB_WAIT_VMCNT(2 * CA::N + 2 * CB::N);
         half();
+        if (AHEAD) read_b(buffer(t0) + 2 * AU, 0);
         if (second) asm volatile("s_barrier" ::: "memory");
-        for (int t = t0; t < in.t1; ++t) {
-            const char* const buf = sm + ((t - t0) & 1) * BUF;
-            read_b(buf + 2 * AU, 0);
-            read_a(buf);
-            copy_a(1, t + 1);
-            half();
-            products(0, 0);
-            read_b(buf + 2 * AU + BU, 1);
-            copy_a(0, t + 2);
-            ELB_WAIT_VMCNT(3 * CA::N + 2 * CB::N);
-            half();
-            products(0, 1);
-            read_a(buf + AU);
-            copy_b(0, t + 2);
-            half();
-            products(1, 1);
-            copy_b(1, t + 2);
-            ELB_WAIT_VMCNT(2 * CA::N + 2 * CB::N);
-            half();
-            products(1, 0);
+        for (int t = t0; t < in.t1; t += 2) {
+            tile(t, Half<0>());
+            if (t + 1 < in.t1) tile(t + 1, Half<AHEAD ? 1 : 0>());
         }
         if (!second) asm volatile("s_barrier" ::: "memory");
         ELB_WAIT_VMCNT(0);
@@ -744,6 +766,7 @@ struct TurnForm {
                 for (int i = 0; i < NV; ++i) {
                     const acc_t& c = acc[i / (2 * FM * FN)][i / (FM * FN) % 2][i / FN % FM][i % FN];
                     *piece(in.half, i) = c;
+                    if (i % 8 == 7) __builtin_amdgcn_sched_barrier(0);
                 }
                 // every wave's stores have reached L2 before the barrier; then one wave's release
                 // (which writes L2 back) covers them all (by all eight waves: 35 us more)
@@ -759,6 +782,8 @@ struct TurnForm {
             for (int i = 0; i < NV; ++i) {
                 acc[i / (2 * FM * FN)][i / (FM * FN) % 2][i / FN % FM][i % FN] +=
                     *piece(1 - in.half, i);
+                // eight loads at a time: all of them at once have no registers
+                if (i % 8 == 7) __builtin_amdgcn_sched_barrier(0);
             }
         }
 
