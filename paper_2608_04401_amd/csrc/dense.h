@@ -510,7 +510,7 @@ struct SplitJoin {
 // the whole TM x TN tile, with a ring of S k-tiles of its own and no barrier in the loop; their
 // partial tiles are then summed in LDS in the order of the contraction.
 // ------------------------------------------------------------------------------------------
-template <class E, int TM, int TN, int NW, int LB, bool PAIR, bool DMA, int S>
+template <class E, int TM, int TN, int NW, int LA, int LB, bool PAIR, int S>
 struct SplitForm {
     static constexpr int MF = 16;
     static constexpr int FM = TM / 16, FN = TN / 16;
@@ -519,8 +519,8 @@ struct SplitForm {
     static constexpr int PART = SplitJoin<E, TM, TN, NW, PAIR>::PART;
     static constexpr int LDS = NW * (WRING > PART ? WRING : PART);
     typedef typename Mma<E, 16>::acc acc_t;
-    typedef Copier<KC, TM, E::SZ, 1, false, DMA> CA;
-    typedef Copier<LB, TN, E::SZ, 1, PAIR, DMA> CB;
+    typedef Copier<LA, TM, E::SZ, 1, false, true> CA;
+    typedef Copier<LB, TN, E::SZ, 1, PAIR, true> CB;
 
     template <class Epi>
     static __device__ __forceinline__ void run(const TileIn& in, char* sm, const Epi& epi) {
@@ -530,7 +530,7 @@ struct SplitForm {
         CB cb;
         ca.init(in.a, nullptr, in.lda, in.rows, in.K, lane, 0);
         cb.init(in.b, in.b2, in.ldb, in.cols, in.K, lane, 0);
-        Reader<E, 16, KC, TM> ra;
+        Reader<E, 16, LA, TM> ra;
         Reader<E, 16, LB, TN> rb;
         ra.init(0, lane);
         rb.init(0, lane);
@@ -1143,7 +1143,7 @@ __global__ __launch_bounds__(256) void dense_tiles2(DenseIn d1, DenseIn d2, int 
 
 template <class E, int TM, int TN, int NW, int LB, bool PAIR, int S, class Epi>
 __global__ __launch_bounds__(NW * 64) void dense_split(DenseIn d, int mt, int nt, Epi epi) {
-    typedef SplitForm<E, TM, TN, NW, LB, PAIR, true, S> Form;
+    typedef SplitForm<E, TM, TN, NW, KC, LB, PAIR, S> Form;
     __shared__ __attribute__((aligned(1024))) char sm[Form::LDS];
     clear_counters(d.clear, d.nclear);
     int m, n;
@@ -1214,6 +1214,21 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     const DenseIn d = one ? d1 : d2;
     const Epi epi = one ? epi1 : epi2;
     dense_block<Form, E, 128, 128, LA, LB, false>(d, m, n, sm, epi);
+}
+
+template <class E, int TM, int TN, int NW, int S, class Epi>
+__global__ __launch_bounds__(NW * 64) void dense_split2(DenseIn d1, DenseIn d2, int mt1, int nt1,
+                                                        int mt2, int nt2, uint32_t blocks1,
+                                                        Epi epi1, Epi epi2) {
+    typedef SplitForm<E, TM, TN, NW, KR, KR, false, S> Form;
+    __shared__ __attribute__((aligned(1024))) char sm[Form::LDS];
+    const uint32_t b = dense_block_number();
+    const bool one = b < blocks1;
+    int m, n;
+    if (!dense_tile(one ? b : b - blocks1, one ? mt1 : mt2, one ? nt1 : nt2, m, n)) return;
+    const DenseIn d = one ? d1 : d2;
+    const Epi epi = one ? epi1 : epi2;
+    dense_block<Form, E, TM, TN, KR, KR, false>(d, m, n, sm, epi);
 }
 
 inline int64_t up8(int64_t n) { return (n + 7) / 8 * 8; }
@@ -1323,7 +1338,28 @@ void launch2(Kernel kernel, int threads, const DenseIn& d1, const DenseIn& d2, c
 template <class E, class Epi>
 void run_product2(const DenseIn& d1, const DenseIn& d2, bool aligned, const Epi& e1,
                   const Epi& e2, hipStream_t s) {
-    if constexpr (E::SZ == 4) {
+    constexpr bool F = E::SZ == 4;
+    auto time = [&](FormId i) {
+        const FormCost& f = (F ? kFormCostsF32 : kFormCosts)[i];
+        return form_time(f, form_tiles(f, d1.rows, d1.cols) + form_tiles(f, d2.rows, d2.cols),
+                         (d1.K * E::SZ + 127) / 128, i != kTiles);
+    };
+    // The split forms are for small layers (tiles few, contraction long): us, large tiles / split:
+    // fp32 256 tokens, d = 128, m = 256 8.4 / 5.2, 2000 tokens, d = 128, m = 64 61 / 14, bf16 16384
+    // tokens, d = m = 256 114 / 41.
+    auto split = [&](float than) {
+        const float t32 = time(kSplit32x32), t64 = time(kSplit64x64);
+        if (t32 >= than && t64 >= than) return false;
+        if (t32 <= t64)
+            launch2<32, 32>(dense_split2<E, 32, 32, 8, 2, Epi>, 512, d1, d2, e1, e2, s);
+        else
+            launch2<64, 64>(dense_split2<E, 64, 64, 4, 2, Epi>, 256, d1, d2, e1, e2, s);
+        return true;
+    };
+    if constexpr (F) {
+        // (read down the rows, the tiles take 1.35 times their estimate: 512 tokens, d = m = 512,
+        // 18.4 us, split 14.0)
+        if (aligned && split(1.35f * time(kTiles))) return;
         if (aligned)
             launch2<64, 64>(dense_tiles2<E, 16, 64, 64, 2, KR, KR, true, 3, Epi>, 256, d1, d2, e1,
                             e2, s);
@@ -1331,14 +1367,12 @@ void run_product2(const DenseIn& d1, const DenseIn& d2, bool aligned, const Epi&
             launch2<64, 64>(dense_tiles2<E, 16, 64, 64, 2, KR, KR, false, 3, Epi>, 256, d1, d2,
                             e1, e2, s);
     } else {
-        auto time = [&](const FormCost& f) {
-            return form_time(f, form_tiles(f, d1.rows, d1.cols) + form_tiles(f, d2.rows, d2.cols),
-                             (d1.K * E::SZ + 127) / 128, true);
-        };
+        const float pairs = time(kPairs), turns = time(kTurns);
+        if (aligned && split(pairs < turns ? pairs : turns)) return;
         if (!aligned)
             launch2<128, 128>(dense_tiles2<E, 32, 128, 128, 2, KR, KR, false, 2, Epi>, 256, d1,
                               d2, e1, e2, s);
-        else if (time(kFormCosts[kPairs]) <= time(kFormCosts[kTurns]))
+        else if (pairs <= turns)
             launch2<128, 128>(dense_pairs2<E, KR, KR, Epi>, 512, d1, d2, e1, e2, s);
         else
             launch2<256, 256>(dense_turns2<E, 256, 256, 2, KR, KR, Epi>, 512, d1, d2, e1, e2, s);

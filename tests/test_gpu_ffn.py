@@ -51,7 +51,9 @@ def test_block_edges(T, d, m, dtype):
                                          (40, 2048, 1024, "bf16"), (100, 1024, 4112, "bf16"),
                                          (513, 2048, 1024, "bf16"), (1777, 2048, 1024, "bf16"),
                                          (2500, 1040, 2064, "bf16"), (1500, 1024, 528, "f32"),
-                                         (4096, 2048, 2048, "bf16"), (2500, 2064, 6160, "bf16")])
+                                         (4096, 2048, 2048, "bf16"), (2500, 2064, 6160, "bf16"),
+                                         (5000, 144, 80, "bf16"), (3000, 144, 80, "f32"),
+                                         (515, 512, 528, "f32"), (2100, 528, 272, "bf16")])
 def test_block_sizes(T, d, m, dtype):
     _check(T, d, m, dtype)
 
