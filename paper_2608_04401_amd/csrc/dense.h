@@ -90,13 +90,16 @@ __device__ __forceinline__ int kc_swz(int r, int c) {
     return c ^ (((r >> 1) ^ ((r & 1) << 2)) & 7);
 }
 // KR unit: 128 / SZ rows of TR elements.  bf16: granules of 16 columns (32 bytes), swizzled so
-// that the four rows x two granules that 32 lanes of a transposing read touch lie in distinct
-// banks; fp32: granules of 16 columns (64 bytes), four rows apart in distinct banks.  Returns
-// the XOR on the 16-byte chunk of row k.
+// that what 32 lanes of a transposing read touch lies in distinct banks, four rows x two granules
+// (MFMAs of 32) or two times four rows, eight apart, of one granule (of 16); fp32: granules of 16
+// columns (64 bytes), four rows apart in distinct banks.  Returns the XOR on the 16-byte chunk of
+// row k.
 template <int TR, int SZ>
 __device__ __forceinline__ int kr_swz(int k) {
     if (SZ == 4) return TR >= 64 ? ((k >> 2) & 3) << 2 : 0;
-    return TR >= 128 ? (k & 3) << 2 : TR == 64 ? ((k >> 1) & 1) << 2 : 0;
+    const int far = ((k >> 3) & 1) << 1;
+    return TR >= 128 ? (k & 3) << 2 | far : TR == 64 ? ((k >> 1) & 1) << 2 | far
+           : TR == 32 ? far : 0;
 }
 
 // ---- global -> LDS copies ----
@@ -237,7 +240,7 @@ struct Reader {
             const int p = lane & 15;
             const int kh = MF == 32 ? (lane >> 5) : (lane >> 4);
             at = (8 * kh + (p >> 2)) * P + (p & 3) * 8;
-            ofs[0] = (kr_swz<TR, 2>(p >> 2) * 16) ^ (MF == 32 ? ((lane >> 4) & 1) * 32 : 0);
+            ofs[0] = (kr_swz<TR, 2>(8 * kh + (p >> 2)) * 16) ^ (MF == 32 ? ((lane >> 4) & 1) * 32 : 0);
         } else {
             at = 4 * g * P + l * 4;
             ofs[0] = kr_swz<TR, 4>(4 * g) * 16;
