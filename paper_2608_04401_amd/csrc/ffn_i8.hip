@@ -293,8 +293,9 @@ struct ScaledOut {  // y = [res +] v s_row c_col
     }
 };
 
-// h = silu(g) u in fp32: rounded to bf16 first, one h in eight would move to the next whole number
-// when it is quantised (2^-9 of a value is up to a quarter of a step)
+// h = silu(g) u in fp32: rounded to bf16 first (2^-9 of a value, up to a quarter of a step), one h
+// in eight of those at 64 steps or more would move to the next whole number when it is quantised
+// (8192 columns, gaussian g and u: 13.7 %; of all h 1.1 %)
 struct ScaledGateOut {
     static constexpr bool kMayHalve = false;
     float* h;
