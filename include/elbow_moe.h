@@ -319,6 +319,8 @@ int elb_ffn_backward(const void *dy, const void *x, const void *W_gate_up, const
  * Rows to 8-bit integers with one scale per row (symmetric):
  *   scale_t = fl32(max_i |x_ti| / 127),  q_ti = the whole number nearest to x_ti / scale_t (of the
  *   exact quotient; ties to even), at most 127 in magnitude; 0 where scale_t = 0
+ *   A row that holds a NaN has scale NaN, one that holds an infinity (and no NaN) an infinite
+ *   scale; the products of both are NaN.
  *   x     [T, d]  dtype
  *   q     [T, d]  int8 output
  *   scale [T]     float output: q_ti scale_t stands for x_ti

@@ -66,17 +66,22 @@ __device__ __forceinline__ u32x2_t quantize8(const X& x, const RowScale& r) {
     return w;
 }
 
+// maxima in which NaN is the largest (fmaxf drops it): a row that holds one has a scale of NaN, and
+// so have its products
+__device__ __forceinline__ float max_nan(float a, float b) {
+    return __builtin_elementwise_maximum(a, b);
+}
 template <class X>
 __device__ __forceinline__ float max8(const X& x, float m) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) m = fmaxf(m, fabsf(x[e]));
+    for (int e = 0; e < 8; ++e) m = max_nan(m, fabsf(x[e]));
     return m;
 }
 // the largest over a wave of values of at least zero (lanes without a source get zero)
 __device__ __forceinline__ float wave_max(float m) {
 #define ELB_MAX_STEP(ctrl, rows)                                                             \
-    m = fmaxf(m, __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(m), ctrl, rows, \
-                                                             0xf, false)))
+    m = max_nan(m, __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(m), ctrl,  \
+                                                               rows, 0xf, false)))
     ELB_MAX_STEP(0x111, 0xf);  // row_shr:1, 2, 4, 8: lane 15 of each row of 16 has the row's
     ELB_MAX_STEP(0x112, 0xf);
     ELB_MAX_STEP(0x114, 0xf);
@@ -122,7 +127,7 @@ __global__ __launch_bounds__(256) void quantize_rows(const T* __restrict__ x, in
         __shared__ float part[4];
         if ((tid & 63) == 0) part[tid >> 6] = mx;
         __syncthreads();
-        mx = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
+        mx = max_nan(max_nan(part[0], part[1]), max_nan(part[2], part[3]));
     }
     const RowScale r(mx);
     if (tid == 0) scale[row] = r.s;

@@ -250,3 +250,37 @@ def test_quantised_layer_beside_the_float_one():
     assert torch.equal(one, y)
     ref = R.ffn_forward(x, fgu, fd)[0]
     assert float((y.double() - res.double() - ref).norm() / ref.norm()) < 0.06
+
+
+@pytest.mark.parametrize("bad", ["nan", "inf", "-inf"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,k,n,m", [(1, 16, 16, 16), (3, 2048, 64, 48), (40, 512, 256, 64),
+                                     (300, 2064, 128, 80), (9, 8208, 32, 16), (8200, 64, 32, 32)])
+def test_a_value_that_is_not_finite_reaches_its_row(T, k, n, m, dtype, bad):
+    """One NaN or infinity makes its row's scale and products so, and no other row's: where the
+    product quantises, where quantisation is its own launch (a wave, a block a row; rows kept in
+    registers and longer ones), and through the block, whose h is quantised again."""
+    x = _rand((T, k), T + k, 1.0, dtype)
+    W, c = B.elb_quantize_rows(_rand((n, k), 1, 0.1))
+    Wgu, cgu = B.elb_quantize_rows(_rand((2 * m, k), 2, 0.1))
+    Wd, cd = B.elb_quantize_rows(_rand((k, m), 3, 0.1))
+    res = _rand((T, k), 4, 1.0, dtype)
+
+    def run(v):
+        q, s = B.elb_quantize_rows(v)
+        return (s[:, None], B.elb_linear_i8(v, W, c), B.elb_gemm_i8(q, s, W, c, dtype=v.dtype),
+                B.elb_ffn_forward_i8(v, Wgu, cgu, Wd, cd, residual=res))
+
+    clean = run(x)
+    for row, col in {(0, k - 1), (T // 2, k // 2), (T - 1, 0)}:
+        y = x.clone()
+        y[row, col] = float(bad)
+        got = run(y)
+        torch.cuda.synchronize()
+        others = torch.arange(T, device="cuda") != row
+        scale = float(got[0][row])
+        assert scale != scale if bad == "nan" else scale == float("inf")
+        for a, b in zip(got, clean):
+            assert torch.equal(a[others], b[others])
+        for a in got[1:]:
+            assert bool(a[row].isnan().all())
