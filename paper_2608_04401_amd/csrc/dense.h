@@ -1,5 +1,5 @@
 // Tile products of the dense operators (the gated feed-forward block and the 8-bit products):
-// global -> LDS copies with bounds, MFMA operand reads, and the two block forms built of them.
+// global -> LDS copies with bounds, MFMA operand reads, and the block forms built of them.
 //
 //   C[r, c] = sum_k A(r, k) B(c, k),  r < rows, c < cols, k < K
 //
@@ -1056,10 +1056,13 @@ __device__ __forceinline__ void dense_block(const DenseIn& d, int m, int n, char
 
 // sigma(g) = 1 / (1 + e^-g) to about two units in the last place of fp32: e^-g = 2^t 2^r with t the
 // rounded product -g log2 e and r what its rounding left off (below 2^-17 for |g| < 2^7), 2^r =
-// 1 + r ln 2.  A g below -88 makes 2^t infinite and sigma zero.  (The library's exponential and
+// 1 + r ln 2.  A g below -88 makes 2^t infinite and sigma zero.  g is held to +-128, where sigma is
+// 1 and 0 already: beyond 2^127 / log2 e, t and r would be infinite and their product no number. A
+// NaN becomes -128, and still NaN in every product with g itself.  (The library's exponential and
 // division take five times the instructions: gate/up of 4096 tokens, m = 8192, int8, 162 us with
 // them.)
 __device__ __forceinline__ float sigma_f32(float g) {
+    g = __builtin_amdgcn_fmed3f(g, -128.0f, 128.0f);
     constexpr float kLog2e = 1.44269504f, kLog2eRest = 1.92596299e-8f, kLn2 = 0.69314718f;
     const float t = -g * kLog2e;
     const float r = fmaf(-g, kLog2eRest, fmaf(-g, kLog2e, -t));

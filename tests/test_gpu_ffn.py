@@ -275,3 +275,40 @@ def test_beside_the_routed_experts():
     torch.cuda.synchronize()
     ry, ey, _, _ = R.ffn_forward(x, Wgu, Wd, routed)
     R.within(y, ry, ey)
+
+
+@pytest.mark.parametrize("T", [1, 40, 300])
+@pytest.mark.parametrize("g", [100.0, 2.5e38, 3.4e38, float("inf")])
+def test_gates_up_to_the_largest(g, T):
+    """fp32 gates where sigma is 1 (or 0, negative): h = g u, dg = dh u, du = dh g, and the zeros."""
+    d = m = 16
+    g, u = float(torch.tensor(g)), 2.0 ** -80
+    x = torch.zeros(T, d, device="cuda")
+    x[:, 0] = 1
+    Wgu = torch.zeros(2 * m, d, device="cuda")
+    Wgu[:m, 0], Wgu[m:, 0] = g, u
+    Wgu[1:m:2, 0] = -min(g, 3.4e38)   # (minus infinity times zero is no number)
+    if g == float("inf"):             # an infinite weight would meet the zeros of x
+        x = torch.full((T, d), 1.0, device="cuda")
+        Wgu[:, 1:] = 0
+    Wd = torch.ones(d, m, device="cuda")
+    y, kept = B.elb_ffn_forward(x, Wgu, Wd, keep=True)
+    # sigma 2 units in the last place, two products, a sum of 16
+    tol = 2 * 2.0 ** -23 + 2 * 2.0 ** -24 + 16 * 2.0 ** -24
+    torch.cuda.synchronize()
+    want = 8 * g * u
+    assert bool((kept[:, 0] == g).all())
+    if g == float("inf"):
+        assert bool((y == want).all())
+        return
+    assert bool(((y.double() - want).abs() <= tol * want).all())
+    dy = torch.zeros(T, d, device="cuda")
+    dy[:, 0] = 2.0 ** -20
+    dx, dWgu, dWd = B.elb_ffn_backward(dy, x, Wgu, Wd, kept)
+    torch.cuda.synchronize()
+    tol += T * 2.0 ** -24
+    dg, du, h = dWgu[0, 0], dWgu[m, 0], dWd[0, 0]
+    for got, ref in ((dg, T * u * 2.0 ** -20), (du, T * g * 2.0 ** -20), (h, T * g * u * 2.0 ** -20)):
+        assert abs(float(got) - ref) <= tol * ref
+    assert float(dWgu[1, 0]) == 0 and float(dWgu[m + 1, 0]) == 0 and float(dWd[0, 1]) == 0
+    assert bool(dx.isfinite().all())
