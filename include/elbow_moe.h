@@ -287,6 +287,8 @@ int elb_moe_forward_packed(const void *x, const void *W_router, const void *W_ga
  * Sums are fp32; for ELB_BF16 h is rounded to bf16 before the second product and y at the end.
  * Requirements: d and m positive multiples of 16, at most 2^20; T < 2^31, T d and T m at most 2^38
  * (as for the entry points below).
+ * The workspace sizes of this and the entry points below never fall as T grows: a workspace for
+ * a batch serves every smaller one too.
  */
 size_t elb_ffn_workspace_bytes(int64_t T, int32_t d, int32_t m, int32_t dtype);
 int elb_ffn_forward(const void *x, const void *W_gate_up, const void *W_down,

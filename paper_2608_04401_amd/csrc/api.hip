@@ -172,11 +172,25 @@ int check_i8_k(int k, const char* name) {
     return ELB_OK;
 }
 
+// Workspaces of the dense operators.  `most`: with the scratch that any batch of up to T tokens needs
+// for products whose tiles two blocks share (what the size queries answer: it never falls as T
+// grows); otherwise what this T needs.
+size_t ffn_bytes(int64_t T, int d, int m, int dtype, bool most) {
+    return align_up((size_t)T * m * esize(dtype)) + ffn_halves_bytes(T, d, m, dtype, most);
+}
+size_t ffn_backward_bytes(int64_t T, int d, int m, int dtype, bool most) {
+    return align_up((size_t)T * m * esize(dtype)) + align_up((size_t)T * 2 * m * esize(dtype)) +
+           ffn_halves_bytes(T, d, 2 * (int64_t)m, dtype, most);
+}
+size_t linear_i8_bytes(int64_t T, int n, int k, bool most) {
+    return align_up((size_t)T * k) + align_up((size_t)T * 4) + i8_halves_bytes(T, n, k, most);
+}
+
 // sub-buffers of the int8 block's workspace
 struct I8Layout {
     size_t xq, xs, h, hq, hs, part, total;
 };
-I8Layout i8_layout(int64_t T, int d, int m) {
+I8Layout i8_layout(int64_t T, int d, int m, bool most) {
     I8Layout L{};
     size_t o = 0;
     auto take = [&](size_t bytes) {
@@ -189,7 +203,7 @@ I8Layout i8_layout(int64_t T, int d, int m) {
     L.h = take((size_t)T * m * 4);
     L.hq = take((size_t)T * m);
     L.hs = take((size_t)T * 4);
-    L.part = take(i8_halves_bytes(T, d, m));
+    L.part = take(i8_halves_bytes(T, d, m, most));
     L.total = o;
     return L;
 }
@@ -655,7 +669,7 @@ int elb_pack_expert_weights(const void* W_gate_up, const void* W_down, int32_t N
 
 size_t elb_ffn_workspace_bytes(int64_t T, int32_t d, int32_t m, int32_t dtype) {
     if (T < 0 || d < 1 || m < 1 || (dtype != ELB_F32 && dtype != ELB_BF16)) return 0;
-    return align_up((size_t)T * m * esize(dtype)) + ffn_halves_bytes(T, d, m, dtype);
+    return ffn_bytes(T, d, m, dtype, true);
 }
 
 int elb_ffn_forward(const void* x, const void* W_gate_up, const void* W_down,
@@ -667,8 +681,7 @@ int elb_ffn_forward(const void* x, const void* W_gate_up, const void* W_down,
     if (T == 0) return ELB_OK;
     if (!x || !W_gate_up || !W_down || !y)
         return fail(ELB_ERR_INVALID_ARG, "NULL tensor pointer");
-    if (int rc = check_workspace(workspace, workspace_bytes,
-                                 elb_ffn_workspace_bytes(T, d, m, dtype)))
+    if (int rc = check_workspace(workspace, workspace_bytes, ffn_bytes(T, d, m, dtype, false)))
         return rc;
     char* const part = (char*)workspace + align_up((size_t)T * m * esize(dtype));
     return hip_status(launch_ffn_forward(x, W_gate_up, W_down, residual, T, d, m, dtype, workspace,
@@ -678,8 +691,7 @@ int elb_ffn_forward(const void* x, const void* W_gate_up, const void* W_down,
 
 size_t elb_ffn_backward_workspace_bytes(int64_t T, int32_t d, int32_t m, int32_t dtype) {
     if (T < 0 || d < 1 || m < 1 || (dtype != ELB_F32 && dtype != ELB_BF16)) return 0;
-    return align_up((size_t)T * m * esize(dtype)) + align_up((size_t)T * 2 * m * esize(dtype)) +
-           ffn_halves_bytes(T, d, 2 * (int64_t)m, dtype);
+    return ffn_backward_bytes(T, d, m, dtype, true);
 }
 
 int elb_ffn_backward(const void* dy, const void* x, const void* W_gate_up, const void* W_down,
@@ -694,7 +706,7 @@ int elb_ffn_backward(const void* dy, const void* x, const void* W_gate_up, const
         return fail(ELB_ERR_INVALID_ARG, "NULL tensor pointer");
     if (T > 0)
         if (int rc = check_workspace(workspace, workspace_bytes,
-                                     elb_ffn_backward_workspace_bytes(T, d, m, dtype)))
+                                     ffn_backward_bytes(T, d, m, dtype, false)))
             return rc;
     char* const h = (char*)workspace;  // (T = 0: not read or written, and may be null)
     char* const dgu = h ? h + align_up((size_t)T * m * esize(dtype)) : nullptr;
@@ -732,7 +744,7 @@ int elb_gemm_i8(const int8_t* q, const float* scale, const int8_t* W, const floa
 
 size_t elb_linear_i8_workspace_bytes(int64_t T, int32_t n, int32_t k) {
     if (T < 0 || n < 1 || k < 1) return 0;
-    return align_up((size_t)T * k) + align_up((size_t)T * 4) + i8_halves_bytes(T, n, k);
+    return linear_i8_bytes(T, n, k, true);
 }
 
 int elb_linear_i8(const void* x, const int8_t* W, const float* W_scale, const void* residual,
@@ -744,7 +756,7 @@ int elb_linear_i8(const void* x, const int8_t* W, const float* W_scale, const vo
     if (int rc = check_i8_k(k, "k")) return rc;
     if (T == 0) return ELB_OK;
     if (!x || !W || !W_scale || !y) return fail(ELB_ERR_INVALID_ARG, "NULL tensor pointer");
-    if (int rc = check_workspace(workspace, workspace_bytes, elb_linear_i8_workspace_bytes(T, n, k)))
+    if (int rc = check_workspace(workspace, workspace_bytes, linear_i8_bytes(T, n, k, false)))
         return rc;
     int8_t* const q = (int8_t*)workspace;
     float* const scale = (float*)((char*)workspace + align_up((size_t)T * k));
@@ -756,7 +768,7 @@ int elb_linear_i8(const void* x, const int8_t* W, const float* W_scale, const vo
 
 size_t elb_ffn_i8_workspace_bytes(int64_t T, int32_t d, int32_t m) {
     if (T < 0 || d < 1 || m < 1) return 0;
-    return i8_layout(T, d, m).total;
+    return i8_layout(T, d, m, true).total;
 }
 
 int elb_ffn_forward_i8(const void* x, const int8_t* W_gate_up, const float* gate_up_scale,
@@ -771,7 +783,7 @@ int elb_ffn_forward_i8(const void* x, const int8_t* W_gate_up, const float* gate
     if (T == 0) return ELB_OK;
     if (!x || !W_gate_up || !gate_up_scale || !W_down || !down_scale || !y)
         return fail(ELB_ERR_INVALID_ARG, "NULL tensor pointer");
-    const I8Layout L = i8_layout(T, d, m);
+    const I8Layout L = i8_layout(T, d, m, false);
     if (int rc = check_workspace(workspace, workspace_bytes, L.total)) return rc;
     char* const ws = (char*)workspace;
     int8_t *const xq = (int8_t*)(ws + L.xq), *const hq = (int8_t*)(ws + L.hq);

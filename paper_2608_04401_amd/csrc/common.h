@@ -188,8 +188,9 @@ hipError_t launch_combine(const void* Y, const int* k, const int* inv, const flo
                           hipStream_t s);
 
 // the dense gated feed-forward block (ffn.hip).  Scratch: h [T, m], dgu [T, 2m], both dtype; part
-// of ffn_halves_bytes for the product with the down weights (K = m), backward that for dx (K = 2m)
-size_t ffn_halves_bytes(int64_t T, int d, int64_t K, int dtype);
+// of ffn_halves_bytes for the product with the down weights (K = m), backward that for dx (K = 2m);
+// most: the most that any batch of up to T tokens needs
+size_t ffn_halves_bytes(int64_t T, int d, int64_t K, int dtype, bool most);
 hipError_t launch_ffn_forward(const void* x, const void* Wgu, const void* Wd, const void* res,
                               int64_t T, int d, int m, int dtype, void* h, void* part,
                               float* gate_up, void* y, hipStream_t s);
@@ -199,7 +200,7 @@ hipError_t launch_ffn_backward(const void* dy, const void* x, const void* Wgu, c
                                hipStream_t s);
 // 8-bit products (ffn_i8.hip).  part: scratch of i8_halves_bytes for the product [T, k] x [n, k],
 // whose counters the quantisation of its tokens clears; or null
-size_t i8_halves_bytes(int64_t T, int n, int k);
+size_t i8_halves_bytes(int64_t T, int n, int k, bool most);
 hipError_t launch_quantize_rows(const void* x, int64_t rows, int d, int dtype, int8_t* q,
                                 float* scale, hipStream_t s, void* part = nullptr, int n = 0);
 hipError_t launch_gemm_i8(const int8_t* a, const float* a_scale, const int8_t* w,

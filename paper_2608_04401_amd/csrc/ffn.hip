@@ -143,9 +143,9 @@ struct Block {
 
 }  // namespace
 
-size_t ffn_halves_bytes(int64_t T, int d, int64_t K, int dtype) {
-    const int size = dtype == ELB_BF16 ? 2 : 4;
-    return halves_bytes(T, d, (K * size + 127) / 128, dtype != ELB_BF16);
+size_t ffn_halves_bytes(int64_t T, int d, int64_t K, int dtype, bool most) {
+    const int64_t kt = (K * (dtype == ELB_BF16 ? 2 : 4) + 127) / 128;
+    return (most ? halves_reserve : halves_bytes)(T, d, kt, dtype != ELB_BF16);
 }
 
 hipError_t launch_ffn_forward(const void* x, const void* Wgu, const void* Wd, const void* res,

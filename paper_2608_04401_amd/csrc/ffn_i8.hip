@@ -422,7 +422,9 @@ hipError_t gate_up(const void* x, const int8_t* w, const float* c, int64_t rows,
 
 }  // namespace
 
-size_t i8_halves_bytes(int64_t T, int n, int k) { return halves_bytes(T, n, (k + 127) / 128, false); }
+size_t i8_halves_bytes(int64_t T, int n, int k, bool most) {
+    return (most ? halves_reserve : halves_bytes)(T, n, ((int64_t)k + 127) / 128, false);
+}
 
 hipError_t launch_quantize_rows(const void* x, int64_t rows, int d, int dtype, int8_t* q,
                                 float* scale, hipStream_t s, void* part, int n) {

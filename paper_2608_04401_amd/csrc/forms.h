@@ -81,4 +81,24 @@ inline size_t halves_bytes(int64_t rows, int64_t cols, int64_t ktiles, bool fp32
     return (size_t)form_tiles(kFormCosts[kHalves], rows, cols) * (2 * kPartialBytes + 4);
 }
 
+// More tiles than this never take kHalves: over q whole rounds of 256 turns tiles and up to half of
+// another, 2 q + 1 half rounds of halves cost less only from (50.8 q + 20.8) / (0.5 - 0.05 q) k-tiles
+// on, 42 for q = 0, 159 for 1, 9560 for 9 and nowhere for 10.
+constexpr int64_t kHalvesMost = 9 * 256 + 128;
+
+// The most that halves_bytes is for any number of rows up to this one: what a caller reserves for
+// batches of up to that size.  Within 256 rows the halves' time stays and the others' do not fall, so
+// that the last of them tells.
+inline size_t halves_reserve(int64_t rows, int64_t cols, int64_t ktiles, bool fp32) {
+    // where one tile is no faster, no number of them is: their rounds are no fewer
+    if (fp32 || form_time(kFormCosts[kHalves], 1, ktiles, true) >=
+                    form_time(kFormCosts[kTurns], 1, ktiles, true))
+        return 0;
+    const int64_t nt = (cols + 255) / 256, most = kHalvesMost / nt;
+    for (int64_t mt = (rows + 255) / 256 < most ? (rows + 255) / 256 : most; mt > 0; --mt)
+        if (size_t n = halves_bytes(rows < 256 * mt ? rows : 256 * mt, cols, ktiles, false))
+            return n;
+    return 0;
+}
+
 }  // namespace elb
