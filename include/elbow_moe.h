@@ -280,13 +280,15 @@ int elb_moe_forward_packed(const void *x, const void *W_router, const void *W_ga
  *   W_gate_up [2m, d]  dtype   rows [0, m) = W_gate, rows [m, 2m) = W_up
  *   W_down    [d, m]   dtype
  *   residual  [T, d]   dtype   optional (NULL: none)
- *   y         [T, d]   dtype   output; may alias residual, must not alias another input
+ *   y         [T, d]   dtype   output; may be residual, and may share memory with x (which is read
+ *                              before y is written), with no other tensor of the call
  *   gate_up   [T, 2m]  float   optional output (NULL: not written): W_gate x_t and W_up x_t, for
- *                              elb_ffn_backward
+ *                              elb_ffn_backward; shares memory with no other tensor
  *   workspace          at least elb_ffn_workspace_bytes(T, d, m, dtype) bytes
  * Sums are fp32; for ELB_BF16 h is rounded to bf16 before the second product and y at the end.
  * Requirements: d and m positive multiples of 16, at most 2^20; T < 2^31, T d and T m at most 2^38
  * (as for the entry points below).
+ * An output that shares memory where it may not is refused with ELB_ERR_INVALID_ARG, here and below.
  * The workspace sizes of this and the entry points below never fall as T grows: a workspace for
  * a batch serves every smaller one too.
  */
@@ -306,7 +308,7 @@ int elb_ffn_forward(const void *x, const void *W_gate_up, const void *W_down,
  *   dW_gate_up [2m, d]  dtype   output, or NULL: not computed
  *   dW_down    [d, m]   dtype   output, or NULL: not computed
  *   workspace           at least elb_ffn_backward_workspace_bytes(T, d, m, dtype) bytes
- * Outputs are overwritten, not added to, and must not alias an input.  Sums are fp32 in a fixed
+ * Outputs are overwritten, not added to, and share memory with no other tensor of the call.  Sums are fp32 in a fixed
  * order (the same bits on every call); for ELB_BF16 dg, du and h are rounded to bf16 before the
  * products they enter.  With T = 0 the weight gradients are sums over no token: they are
  * written as zeros (the one case in which T = 0 enqueues work).  Requirements as elb_ffn_forward.
@@ -325,7 +327,7 @@ int elb_ffn_backward(const void *dy, const void *x, const void *W_gate_up, const
  *   scale; the products of both are NaN.
  *   x     [T, d]  dtype
  *   q     [T, d]  int8 output
- *   scale [T]     float output: q_ti scale_t stands for x_ti
+ *   scale [T]     float output: q_ti scale_t stands for x_ti; x, q and scale share no memory
  * Quantises tokens for elb_gemm_i8, and weights too (rows = output channels).
  * Requirements: d a positive multiple of 16, at most 2^20; T < 2^31.
  */
@@ -338,7 +340,7 @@ int elb_quantize_rows(const void *x, int64_t T, int32_t d, int32_t dtype, int8_t
  *   q        [T, k]  int8, scale [T] float     tokens (elb_quantize_rows)
  *   W        [n, k]  int8, W_scale [n] float   weights
  *   residual [T, n]  dtype   optional (NULL: none)
- *   y        [T, n]  dtype   output; may alias residual
+ *   y        [T, n]  dtype   output; may be residual, shares memory with no other input
  * The sum is exact (int32); its scaling and the residual are fp32, rounded to dtype once.
  * Requirements: n and k positive multiples of 16, n at most 2^20, k at most 131071; T < 2^31.
  */
@@ -348,7 +350,8 @@ int elb_gemm_i8(const int8_t *q, const float *scale, const int8_t *W, const floa
 
 /*
  * elb_quantize_rows and elb_gemm_i8 in one call, for activations x [T, k] of dtype.
- *   workspace  at least elb_linear_i8_workspace_bytes(T, n, k) bytes; y must not alias x
+ *   workspace  at least elb_linear_i8_workspace_bytes(T, n, k) bytes
+ *   y may be residual and shares memory with no other input (x is read while y is written)
  */
 size_t elb_linear_i8_workspace_bytes(int64_t T, int32_t n, int32_t k);
 int elb_linear_i8(const void *x, const int8_t *W, const float *W_scale, const void *residual,
@@ -359,7 +362,8 @@ int elb_linear_i8(const void *x, const int8_t *W, const float *W_scale, const vo
  * The dense gated feed-forward block with 8-bit weights (and activations quantised on the way):
  * x is quantised by rows, g and u are its 8-bit products with W_gate_up, h = silu(g) u is kept in
  * fp32 and quantised by rows, and y = [residual +] the 8-bit product of that with W_down.
- *   x [T, d], residual [T, d] (or NULL), y [T, d]   dtype; y may alias residual, not x
+ *   x [T, d], residual [T, d] (or NULL), y [T, d]   dtype; y may be residual, and may share memory
+ *                                                   with x, with no other input
  *   W_gate_up [2m, d] int8, gate_up_scale [2m] float; W_down [d, m] int8, down_scale [d] float
  *   workspace  at least elb_ffn_i8_workspace_bytes(T, d, m) bytes
  * Requirements: d and m positive multiples of 16, at most 131071; T < 2^31.

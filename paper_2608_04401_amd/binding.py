@@ -461,7 +461,7 @@ def elb_ffn_workspace_bytes(T: int, d: int, m: int, dtype: int) -> int:
 
 def elb_ffn_forward(x, W_gate_up, W_down, residual=None, out=None, keep: bool = False):
     """The dense gated feed-forward block.  -> y, or with keep=True (y, gate_up): gate_up
-    [T, 2m] float32 is what elb_ffn_backward needs of the forward pass."""
+    [T, 2m] float32 is what elb_ffn_backward needs of the forward pass.  out may be residual or x."""
     T, d, m, dt, dev = _ffn_dims(x, W_gate_up, W_down)
     _want("residual", residual, (T, d), x.dtype, dev)
     _want("out", out, (T, d), x.dtype, dev)
@@ -510,7 +510,8 @@ def elb_quantize_rows(x: torch.Tensor):
 
 def elb_gemm_i8(q, scale, W, W_scale, dtype: torch.dtype = torch.bfloat16, residual=None,
                 out=None) -> torch.Tensor:
-    """y [T, n] of dtype (bfloat16 or float32) from q [T, k] int8 and W [n, k] int8."""
+    """y [T, n] of dtype (bfloat16 or float32) from q [T, k] int8 and W [n, k] int8.  out may be
+    residual."""
     T, k = _matrix("q", q)
     n = _matrix("W", W)[0]
     dev = _device(q)
@@ -533,7 +534,8 @@ def elb_linear_i8_workspace_bytes(T: int, n: int, k: int) -> int:
 
 
 def elb_linear_i8(x, W, W_scale, residual=None, out=None) -> torch.Tensor:
-    """y [T, n] = x [T, k], quantised by rows on the way, times W [n, k] int8."""
+    """y [T, n] = x [T, k], quantised by rows on the way, times W [n, k] int8.  out may be residual,
+    not x."""
     T, k = _matrix("x", x)
     n = _matrix("W", W)[0]
     dt = _dtype_code(x)
@@ -560,7 +562,8 @@ def elb_ffn_i8_workspace_bytes(T: int, d: int, m: int) -> int:
 def elb_ffn_forward_i8(x, W_gate_up, gate_up_scale, W_down, down_scale, residual=None,
                        out=None) -> torch.Tensor:
     """The dense gated feed-forward block with int8 weights (elb_quantize_rows of the float
-    ones): W_gate_up [2m, d], gate_up_scale [2m], W_down [d, m], down_scale [d]."""
+    ones): W_gate_up [2m, d], gate_up_scale [2m], W_down [d, m], down_scale [d].  out may be
+    residual or x."""
     T, d = _matrix("x", x)
     m = _matrix("W_down", W_down)[1]
     dt = _dtype_code(x)

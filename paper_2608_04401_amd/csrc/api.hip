@@ -5,6 +5,7 @@
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
+#include <initializer_list>
 #include <map>
 #include <mutex>
 #include <string>
@@ -170,6 +171,31 @@ int check_i8_k(int k, const char* name) {
         return fail(ELB_ERR_UNSUPPORTED, "%s = %d: int32 sums hold a contraction of %d", name, k,
                     kMaxI8K);
     return ELB_OK;
+}
+
+// A tensor of a call, and whether two of them share memory.  Null: one that the call has not.
+struct Span {
+    const char* name;
+    const void* p;
+    int64_t bytes;
+    bool meets(const Span& o) const {
+        const uintptr_t a = (uintptr_t)p, b = (uintptr_t)o.p;
+        return p && o.p && bytes > 0 && o.bytes > 0 && a < b + (uint64_t)o.bytes &&
+               b < a + (uint64_t)bytes;
+    }
+};
+
+// An output may share no memory with what a launch reads while another of its blocks writes.
+int check_apart(const Span& out, std::initializer_list<Span> others) {
+    for (const Span& o : others)
+        if (out.meets(o))
+            return fail(ELB_ERR_INVALID_ARG, "%s overlaps %s", out.name, o.name);
+    return ELB_OK;
+}
+
+// residual and y of one size: the same tensor, or apart (each value is read by the lane that writes it)
+int check_residual(const Span& y, const void* residual) {
+    return residual == y.p ? ELB_OK : check_apart(y, {{"residual", residual, y.bytes}});
 }
 
 // Workspaces of the dense operators.  `most`: with the scratch that any batch of up to T tokens needs
@@ -683,6 +709,13 @@ int elb_ffn_forward(const void* x, const void* W_gate_up, const void* W_down,
         return fail(ELB_ERR_INVALID_ARG, "NULL tensor pointer");
     if (int rc = check_workspace(workspace, workspace_bytes, ffn_bytes(T, d, m, dtype, false)))
         return rc;
+    const int64_t e = esize(dtype);
+    const Span out{"y", y, T * d * e}, in{"x", x, T * d * e},
+        gu{"W_gate_up", W_gate_up, (int64_t)2 * m * d * e},
+        down{"W_down", W_down, (int64_t)d * m * e}, kept{"gate_up", gate_up, T * 2 * m * 4};
+    if (int rc = check_apart(out, {gu, down, kept})) return rc;
+    if (int rc = check_residual(out, residual)) return rc;
+    if (int rc = check_apart(kept, {in, gu, down, {"residual", residual, out.bytes}})) return rc;
     char* const part = (char*)workspace + align_up((size_t)T * m * esize(dtype));
     return hip_status(launch_ffn_forward(x, W_gate_up, W_down, residual, T, d, m, dtype, workspace,
                                          part, gate_up, y, (hipStream_t)stream),
@@ -708,6 +741,16 @@ int elb_ffn_backward(const void* dy, const void* x, const void* W_gate_up, const
         if (int rc = check_workspace(workspace, workspace_bytes,
                                      ffn_backward_bytes(T, d, m, dtype, false)))
             return rc;
+    const int64_t e = esize(dtype);
+    const Span in[] = {{"dy", dy, T * d * e}, {"x", x, T * d * e},
+                       {"W_gate_up", W_gate_up, (int64_t)2 * m * d * e},
+                       {"W_down", W_down, (int64_t)d * m * e}, {"gate_up", gate_up, T * 2 * m * 4}};
+    const Span out[] = {{"dx", dx, in[1].bytes}, {"dW_gate_up", dW_gate_up, in[2].bytes},
+                        {"dW_down", dW_down, in[3].bytes}};
+    for (int i = 0; i < 3; ++i) {
+        if (int rc = check_apart(out[i], {in[0], in[1], in[2], in[3], in[4]})) return rc;
+        if (int rc = check_apart(out[i], {out[(i + 1) % 3]})) return rc;
+    }
     char* const h = (char*)workspace;  // (T = 0: not read or written, and may be null)
     char* const dgu = h ? h + align_up((size_t)T * m * esize(dtype)) : nullptr;
     char* const part = h ? dgu + align_up((size_t)T * 2 * m * esize(dtype)) : nullptr;
@@ -723,6 +766,9 @@ int elb_quantize_rows(const void* x, int64_t T, int32_t d, int32_t dtype, int8_t
     if (int rc = check_dense(T, d, "d", 16, "d")) return rc;
     if (T == 0) return ELB_OK;
     if (!x || !q || !scale) return fail(ELB_ERR_INVALID_ARG, "NULL tensor pointer");
+    const Span in{"x", x, T * d * (int64_t)esize(dtype)}, scales{"scale", scale, T * 4};
+    if (int rc = check_apart({"q", q, T * d}, {in, scales})) return rc;
+    if (int rc = check_apart(scales, {in})) return rc;
     return hip_status(launch_quantize_rows(x, T, d, dtype, q, scale, (hipStream_t)stream),
                       "quantize_rows");
 }
@@ -737,6 +783,11 @@ int elb_gemm_i8(const int8_t* q, const float* scale, const int8_t* W, const floa
     if (T == 0) return ELB_OK;
     if (!q || !scale || !W || !W_scale || !y)
         return fail(ELB_ERR_INVALID_ARG, "NULL tensor pointer");
+    const Span out{"y", y, T * n * (int64_t)esize(dtype)};
+    if (int rc = check_apart(out, {{"q", q, T * k}, {"scale", scale, T * 4},
+                                   {"W", W, (int64_t)n * k}, {"W_scale", W_scale, (int64_t)n * 4}}))
+        return rc;
+    if (int rc = check_residual(out, residual)) return rc;
     return hip_status(launch_gemm_i8(q, scale, W, W_scale, residual, T, n, k, dtype, y,
                                      (hipStream_t)stream),
                       "gemm_i8");
@@ -758,6 +809,12 @@ int elb_linear_i8(const void* x, const int8_t* W, const float* W_scale, const vo
     if (!x || !W || !W_scale || !y) return fail(ELB_ERR_INVALID_ARG, "NULL tensor pointer");
     if (int rc = check_workspace(workspace, workspace_bytes, linear_i8_bytes(T, n, k, false)))
         return rc;
+    const int64_t e = esize(dtype);
+    const Span out{"y", y, T * n * e};
+    if (int rc = check_apart(out, {{"x", x, T * k * e}, {"W", W, (int64_t)n * k},
+                                   {"W_scale", W_scale, (int64_t)n * 4}}))
+        return rc;
+    if (int rc = check_residual(out, residual)) return rc;
     int8_t* const q = (int8_t*)workspace;
     float* const scale = (float*)((char*)workspace + align_up((size_t)T * k));
     char* const part = (char*)scale + align_up((size_t)T * 4);
@@ -785,6 +842,13 @@ int elb_ffn_forward_i8(const void* x, const int8_t* W_gate_up, const float* gate
         return fail(ELB_ERR_INVALID_ARG, "NULL tensor pointer");
     const I8Layout L = i8_layout(T, d, m, false);
     if (int rc = check_workspace(workspace, workspace_bytes, L.total)) return rc;
+    const Span out{"y", y, T * d * (int64_t)esize(dtype)};
+    if (int rc = check_apart(out, {{"W_gate_up", W_gate_up, (int64_t)2 * m * d},
+                                   {"gate_up_scale", gate_up_scale, (int64_t)2 * m * 4},
+                                   {"W_down", W_down, (int64_t)d * m},
+                                   {"down_scale", down_scale, (int64_t)d * 4}}))
+        return rc;
+    if (int rc = check_residual(out, residual)) return rc;
     char* const ws = (char*)workspace;
     int8_t *const xq = (int8_t*)(ws + L.xq), *const hq = (int8_t*)(ws + L.hq);
     float *const xs = (float*)(ws + L.xs), *const hs = (float*)(ws + L.hs);
