@@ -72,7 +72,8 @@ struct GateGradOut {  // from dh, g and u: dg and du [T, 2m], h [T, m]
         for (int q = 0; q < 8; ++q) {
             const float s = sigma(g[q], T());
             const float gs = g[q] * s;
-            dg[q] = dh[q] * u[q] * (s + gs * (1.0f - s));
+            // sigma' first: dh u alone may pass the largest fp32 where a closed gate brings it back
+            dg[q] = dh[q] * (u[q] * (s + gs * (1.0f - s)));
             du[q] = dh[q] * gs;
             hh[q] = gs * u[q];
         }

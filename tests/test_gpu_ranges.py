@@ -59,3 +59,23 @@ def test_block_of_rows_and_scales_far_apart(T, d, m, dtype):
     torch.cuda.synchronize()
     assert bool(want.isfinite().all())
     assert torch.equal(got, want) and torch.equal(far, want)
+
+
+@pytest.mark.parametrize("T", [3, 40, 300])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_gradients_of_closed_gates(T, dtype):
+    """dh of 2^70 and u of 2^70 behind gates of -20 to -80: dg = dh u sigma'(g) is finite though dh u
+    is not."""
+    d = m = 64
+    x = _rand((T, d), T, dtype)
+    Wgu = _rand((2 * m, d), 1, dtype) / 8
+    Wd = torch.eye(d, device="cuda", dtype=DT[dtype])
+    dy = (2.0 ** 70 * (1 + _rand((T, d), 2).abs())).to(DT[dtype])
+    g = -20 - 60 * torch.rand((T, m), device="cuda", generator=torch.Generator("cuda").manual_seed(3))
+    kept = torch.cat([g, 2.0 ** 70 * (1 + _rand((T, m), 4).abs())], 1)
+    grads = B.elb_ffn_backward(dy, x, Wgu, Wd, kept)
+    torch.cuda.synchronize()
+    for got, ref, bound, name in zip(grads, *R.ffn_backward(dy, x, Wgu, Wd, kept),
+                                     ("dx", "dW_gate_up", "dW_down")):
+        assert bool(ref.isfinite().all()) and float(ref.abs().max()) < 2.0 ** 126
+        R.within(got, ref, bound, name)
