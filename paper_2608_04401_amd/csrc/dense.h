@@ -1345,27 +1345,17 @@ template <class E, class Epi>
 void run_product2(const DenseIn& d1, const DenseIn& d2, bool aligned, const Epi& e1,
                   const Epi& e2, hipStream_t s) {
     constexpr bool F = E::SZ == 4;
-    auto time = [&](FormId i) {
-        const FormCost& f = (F ? kFormCostsF32 : kFormCosts)[i];
-        return form_time(f, form_tiles(f, d1.rows, d1.cols) + form_tiles(f, d2.rows, d2.cols),
-                         (d1.K * E::SZ + 127) / 128, i != kTiles);
-    };
-    // The split forms are for small layers (tiles few, contraction long): us, large tiles / split:
-    // fp32 256 tokens, d = 128, m = 256 8.4 / 5.2, 2000 tokens, d = 128, m = 64 61 / 14, bf16 16384
-    // tokens, d = m = 256 114 / 41.
-    auto split = [&](float than) {
-        const float t32 = time(kSplit32x32), t64 = time(kSplit64x64);
-        if (t32 >= than && t64 >= than) return false;
-        if (t32 <= t64)
-            launch2<32, 32>(dense_split2<E, 32, 32, 8, 2, Epi>, 512, d1, d2, e1, e2, s);
-        else
-            launch2<64, 64>(dense_split2<E, 64, 64, 4, 2, Epi>, 256, d1, d2, e1, e2, s);
-        return true;
-    };
+    const FormId form = !aligned ? kTiles
+                                 : pick_form2(d1.rows, d1.cols, d2.rows, d2.cols,
+                                              (d1.K * E::SZ + 127) / 128, F);
+    switch (form) {
+        case kSplit32x32:
+            return launch2<32, 32>(dense_split2<E, 32, 32, 8, 2, Epi>, 512, d1, d2, e1, e2, s);
+        case kSplit64x64:
+            return launch2<64, 64>(dense_split2<E, 64, 64, 4, 2, Epi>, 256, d1, d2, e1, e2, s);
+        default: break;
+    }
     if constexpr (F) {
-        // (read down the rows, the tiles take 1.35 times their estimate: 512 tokens, d = m = 512,
-        // 18.4 us, split 14.0)
-        if (aligned && split(1.35f * time(kTiles))) return;
         if (aligned)
             launch2<64, 64>(dense_tiles2<E, 16, 64, 64, 2, KR, KR, true, 3, Epi>, 256, d1, d2, e1,
                             e2, s);
@@ -1373,12 +1363,10 @@ void run_product2(const DenseIn& d1, const DenseIn& d2, bool aligned, const Epi&
             launch2<64, 64>(dense_tiles2<E, 16, 64, 64, 2, KR, KR, false, 3, Epi>, 256, d1, d2,
                             e1, e2, s);
     } else {
-        const float pairs = time(kPairs), turns = time(kTurns);
-        if (aligned && split(pairs < turns ? pairs : turns)) return;
-        if (!aligned)
+        if (form == kTiles)
             launch2<128, 128>(dense_tiles2<E, 32, 128, 128, 2, KR, KR, false, 2, Epi>, 256, d1,
                               d2, e1, e2, s);
-        else if (pairs <= turns)
+        else if (form == kPairs)
             launch2<128, 128>(dense_pairs2<E, KR, KR, Epi>, 512, d1, d2, e1, e2, s);
         else
             launch2<256, 256>(dense_turns2<E, 256, 256, 2, KR, KR, Epi>, 512, d1, d2, e1, e2, s);

@@ -384,15 +384,10 @@ void run_quant(const DenseIn& d, const Epi& epi, hipStream_t s) {
                dim3(NW * 64), 0, s, d, mt, nt, epi);
 }
 
-constexpr int kFusedK = 2048;  // longest row that a wave keeps in registers, several rows at a time
 // Whether the product of float rows takes a form that quantises them itself.
 bool quant_fused(const int8_t* w, int64_t rows, int64_t cols, int64_t K) {
-    if (!aligned16(w, w)) return false;
-    switch (pick_form(rows, cols, (K + 127) / 128, false, true)) {
-        case kSplit16x16: case kSplit16x32: case kSplit16x64: case kSplit32x32:
-            return K <= kFusedK;
-        default: return false;
-    }
+    return aligned16(w, w) &&
+           form_quantises(pick_form(rows, cols, (K + 127) / 128, false, true), K);
 }
 
 // x [rows, K] of type T times w; only where quant_fused() says so

@@ -73,6 +73,38 @@ inline FormId pick_form(int64_t rows, int64_t cols, int64_t ktiles, bool fp32, b
     return (FormId)best;
 }
 
+// Two products of one contraction in one launch, both operands down the rows (the weight gradients):
+// split 32 x 32 or 64 x 64, or the large forms.  The split forms are for small layers (tiles few,
+// contraction long): us, large tiles / split: fp32 256 tokens, d = 128, m = 256 8.4 / 5.2, 2000 tokens,
+// d = 128, m = 64 61 / 14, bf16 16384 tokens, d = m = 256 114 / 41.
+inline FormId pick_form2(int64_t rows1, int64_t cols1, int64_t rows2, int64_t cols2, int64_t ktiles,
+                         bool fp32) {
+    auto time = [&](FormId i) {
+        const FormCost& f = (fp32 ? kFormCostsF32 : kFormCosts)[i];
+        return form_time(f, form_tiles(f, rows1, cols1) + form_tiles(f, rows2, cols2), ktiles,
+                         i != kTiles);
+    };
+    FormId large = kTiles;
+    float than;
+    if (fp32) {
+        // (read down the rows, the tiles take 1.35 times their estimate: 512 tokens, d = m = 512,
+        // 18.4 us, split 14.0)
+        than = 1.35f * time(kTiles);
+    } else {
+        const float pairs = time(kPairs), turns = time(kTurns);
+        large = pairs <= turns ? kPairs : kTurns;
+        than = pairs < turns ? pairs : turns;
+    }
+    const float t32 = time(kSplit32x32), t64 = time(kSplit64x64);
+    if (t32 >= than && t64 >= than) return large;
+    return t32 <= t64 ? kSplit32x32 : kSplit64x64;
+}
+
+// Whether an int8 product of float rows of K values quantises them itself, where it takes form f: one
+// of few rows, and rows that a wave keeps in registers, several at a time.
+constexpr int kFusedK = 2048;
+inline bool form_quantises(FormId f, int64_t K) { return f <= kSplit32x32 && K <= kFusedK; }
+
 // scratch of a product that may take kHalves: per tile the two blocks' fp32 (int32) partial tiles,
 // then a counter; 0 where another form is picked
 constexpr int64_t kPartialBytes = 256 * 256 * 4;
