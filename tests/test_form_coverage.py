@@ -114,3 +114,12 @@ def test_sizes_for_shared_tiles_share_them(forms):
     rounds = lambda T, c: -(-T // 256) * -(-c // 256) / 128
     assert any(rounds(T, d) > 2 for T, d, _ in SHARED_TILES)
     assert any(rounds(T, n) > 2 for T, n, _ in SHARED_TILES_I8)
+
+
+def test_sizes_without_tokens_take_every_form(forms):
+    """Of the weight gradients with an empty contraction."""
+    from form_cases import NO_TOKENS
+    got = block_kernels(forms, [(0, d, m, dt) for d, m, dt in NO_TOKENS])
+    assert {(dt, f) for dt, p, f in got if p == "dw"} == {
+        ("bf16", "32x32"), ("bf16", "64x64"), ("bf16", "pairs"), ("bf16", "turns"),
+        ("f32", "32x32"), ("f32", "64x64"), ("f32", "tiles")}
