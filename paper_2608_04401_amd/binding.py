@@ -4,6 +4,10 @@ Every function has the name of the C entry point it calls (include/elbow_moe.h) 
 torch tensors that live on the GPU; torch provides device memory and the current stream,
 every step of the computation runs in the library's HIP kernels.  There is no fallback:
 if the library is missing or a call fails, an exception is raised.
+
+The calls are outside autograd: they read tensors that require gradients like any other, record
+nothing, and their results never require gradients.  Where elb_ffn_forward is trained through,
+elb_ffn_backward gives its gradients (an autograd.Function of the two is a user's few lines).
 """
 from __future__ import annotations
 
@@ -461,7 +465,8 @@ def elb_ffn_workspace_bytes(T: int, d: int, m: int, dtype: int) -> int:
 
 def elb_ffn_forward(x, W_gate_up, W_down, residual=None, out=None, keep: bool = False):
     """The dense gated feed-forward block.  -> y, or with keep=True (y, gate_up): gate_up
-    [T, 2m] float32 is what elb_ffn_backward needs of the forward pass.  out may be residual or x."""
+    [T, 2m] float32 is what elb_ffn_backward needs of the forward pass.  out may be residual or x.
+    Outside autograd: y never requires a gradient."""
     T, d, m, dt, dev = _ffn_dims(x, W_gate_up, W_down)
     _want("residual", residual, (T, d), x.dtype, dev)
     _want("out", out, (T, d), x.dtype, dev)
