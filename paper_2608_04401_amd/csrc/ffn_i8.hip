@@ -148,9 +148,12 @@ __global__ __launch_bounds__(256) void quantize_rows(const T* __restrict__ x, in
 // The split form with the quantisation in it, for few rows: every block quantises its TM rows of x
 // into LDS (as the product's k-tiles) and then multiplies them with its weight rows, whose first
 // k-tiles are copied meanwhile.  The blocks repeat each other's quantisation, 16 or 32 rows of at
-// most KMAX values, which takes them less than the launch that it saves (us, in its own launch /
-// here: one token through the block of d = 2048, m = 1024 18.9 / 12.1; 40 tokens through a 2048 x
-// 2048 projection 10.7 / 8.5).
+// most KMAX values.  For up to some ten rows that takes them less than the launch that it saves, for
+// more rows, of bf16 above all, longer (us on the GPU, here / in its own launch, 2048 values to 2048
+// channels: one row bf16 7.0 / 7.8, fp32 5.1 / 7.1; 8 rows 7.7 / 8.2, 6.3 / 7.8; 16 rows 10.7 / 8.4,
+// 7.4 / 7.9; 40 rows 14.4 / 9.5, 7.3 / 8.4; 128 rows 19.3 / 9.9, 13.4 / 9.2; one token through the
+// block of d = 2048, m = 1024 10.6 / 14.2).  bf16 rows meet quotients of exactly a half far more often
+// than fp32 ones where their largest value has few bits, and those are settled one by one.
 // ------------------------------------------------------------------------------------------
 template <class T, int TM, int TN, int NW, bool PAIR, int S, int KMAX>
 struct QuantForm {

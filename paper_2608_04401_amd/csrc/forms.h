@@ -9,9 +9,15 @@
 //   64 rows, 2048 columns: 32 x 32 split 4.9, 32 x 64 5.9, 64 x 64 6.8, 16 x 16 (two rounds) 7.6.
 //   4096 rows, 2048 columns (128 turns tiles, 512 pairs tiles): bf16 of 128 k-tiles pairs 146,
 //   halves 126, of 256 k-tiles 303 and 228; int8 of 64 k-tiles pairs 72, halves 85.
+// Halves win over several rounds of the chip too where the contraction is long (us, halves / best other):
+// bf16 320 tiles of 256 k-tiles 578 / 690, of 448 970 / 1378, 384 of 256 634 / 679, 640 of 448 1704 /
+// 1790; int8 320 of 512 1122 / 1447; near the choice the two are level (384 of 192 491 / 495).
 // Over 144 such products the choice (without halves) is 0.3 % slower than the best form on average,
-// 13 % at worst, and between pairs and turns over 72 larger ones 0.4 % and 9 % (fp32, 128 products:
-// 0.4 % and 10 %).
+// 13 % at worst, and between pairs and turns over 72 larger ones 0.4 % and 9 %.  fp32: 0.4 % and 10 %
+// over 128 products, 1.0 % and 15 % over 54 others (512 rows, 2048 columns, 64 k-tiles: tiles 43.3,
+// 64 x 64 split 37.6).  The fp32 tile form's time is met within 10 % at whole rounds of 256 tiles and
+// is up to 1.8 times the estimate just above one (272 tiles of 32 k-tiles 38.4, estimated 21.5), where
+// the other forms take as long (37 to 41).
 // Usable from host code without HIP (for tests).
 #pragma once
 
@@ -87,8 +93,10 @@ inline FormId pick_form2(int64_t rows1, int64_t cols1, int64_t rows2, int64_t co
     FormId large = kTiles;
     float than;
     if (fp32) {
-        // (read down the rows, the tiles take 1.35 times their estimate: 512 tokens, d = m = 512,
-        // 18.4 us, split 14.0)
+        // read down the rows, the tiles take 1.0 (many rounds) to 1.8 times (one) their estimate;
+        // with 1.35 the choice over 30 products of 256 .. 4096 tokens is 3 % slower than the best on
+        // average: 512 tokens, d = m = 512 split 13.8 us, tiles 18.0; 256 tokens, d = 2048, m = 1024
+        // 47.3, 35.0; at worst 39 %, 256 tokens, d = m = 1024, split 26.4, tiles 19.1
         than = 1.35f * time(kTiles);
     } else {
         const float pairs = time(kPairs), turns = time(kTurns);
@@ -101,7 +109,8 @@ inline FormId pick_form2(int64_t rows1, int64_t cols1, int64_t rows2, int64_t co
 }
 
 // Whether an int8 product of float rows of K values quantises them itself, where it takes form f: one
-// of few rows, and rows that a wave keeps in registers, several at a time.
+// of few rows, and rows that a wave keeps in registers, several at a time.  (The rows' count is no
+// term of it: see the times of both sides at QuantForm.)
 constexpr int kFusedK = 2048;
 inline bool form_quantises(FormId f, int64_t K) { return f <= kSplit32x32 && K <= kFusedK; }
 
