@@ -37,7 +37,8 @@ struct RowScale {
 
 // Eight values to whole numbers, four to a word.  x / s is taken as x inv, off by 2^-24 of itself,
 // at most 2^-17, and rounded by adding 3 2^22, which leaves the whole number in the low bits; where
-// it lies within 2^-14 of a half (one value in 8000), or s is small, the remainder settles it.
+// it lies within 2^-14 of a half (one value in 8000 of fp32 rows; of bf16 rows, whose quotients are ratios
+// of 8 bits and meet halves exactly, one in 500 to 6000), or s is small, the remainder settles it.
 template <class X>  // eight values: an array of floats, or as loaded
 __device__ __forceinline__ u32x2_t quantize8(const X& x, const RowScale& r) {
     constexpr float kMagic = 12582912.0f;
@@ -149,11 +150,11 @@ __global__ __launch_bounds__(256) void quantize_rows(const T* __restrict__ x, in
 // into LDS (as the product's k-tiles) and then multiplies them with its weight rows, whose first
 // k-tiles are copied meanwhile.  The blocks repeat each other's quantisation, 16 or 32 rows of at
 // most KMAX values.  For up to some ten rows that takes them less than the launch that it saves, for
-// more rows, of bf16 above all, longer (us on the GPU, here / in its own launch, 2048 values to 2048
-// channels: one row bf16 7.0 / 7.8, fp32 5.1 / 7.1; 8 rows 7.7 / 8.2, 6.3 / 7.8; 16 rows 10.7 / 8.4,
-// 7.4 / 7.9; 40 rows 14.4 / 9.5, 7.3 / 8.4; 128 rows 19.3 / 9.9, 13.4 / 9.2; one token through the
-// block of d = 2048, m = 1024 10.6 / 14.2).  bf16 rows meet quotients of exactly a half far more often
-// than fp32 ones where their largest value has few bits, and those are settled one by one.
+// more rows about as long, and longer from some hundred on (us on the GPU, here / in its own launch,
+// 2048 values to 2048 channels, fp32: one row 5.0 / 7.0, 8 rows 5.8 / 7.8, 16 rows 7.5 / 7.9, 40 rows
+// 8.5 / 8.5, 128 rows 12.2 / 9.2; one token through the bf16 block of d = 2048, m = 1024 10.6 / 14.2).
+// bf16 rows take longer where many quotients are settled (quantize8): gaussian ones 40 rows 10 to 14 /
+// 9.2, with one channel in 64 eight times as large 6.7 to 7.3 / 8.2.
 // ------------------------------------------------------------------------------------------
 template <class T, int TM, int TN, int NW, bool PAIR, int S, int KMAX>
 struct QuantForm {
