@@ -269,17 +269,17 @@ __global__ __launch_bounds__(NW * 64) void dense_quant(DenseIn d, int mt, int nt
     dense_block<Form, I8, TM, TN, KC, KC, PAIR>(d, m, n, sm, epi);
 }
 
-// v = v s c from left to right, eight values of a row.  FAR, for waves with a row whose s is 2^96 or
-// more: that s over 2^64 on the way, since v s alone (v up to 2^31) would pass the largest fp32 where
+// v = v s c from left to right, eight values of a row.  FAR, for waves with a row whose |s| is 2^96
+// or more: that s over 2^64 on the way, since v s alone (v up to 2^31) would pass the largest fp32 where
 // c brings it back.  Powers of two: no rounding differs.  A scalar branch chooses (us, 16384 x 4096 x
 // 512, mostly epilogue: never FAR 73.0, chosen 74.8, always 75.0; 2048 and 8192 deep 0 to 1 %).
 __device__ __forceinline__ bool any_far(float s) {
-    return __builtin_expect(__builtin_amdgcn_ballot_w64(s >= 0x1p96f) != 0, 0);
+    return __builtin_expect(__builtin_amdgcn_ballot_w64(fabsf(s) >= 0x1p96f) != 0, 0);
 }
 template <bool FAR>
 __device__ __forceinline__ void scale8(float (&v)[8], float s, const Eight<float>& c) {
 #pragma clang fp contract(off)  // the same roundings in every kernel
-    const bool far = FAR && s >= 0x1p96f;
+    const bool far = FAR && fabsf(s) >= 0x1p96f;
     const float down = far ? s * 0x1p-64f : s, up = far ? 0x1p64f : 1.0f;
 #pragma unroll
     for (int q = 0; q < 8; ++q) {

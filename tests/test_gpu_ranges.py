@@ -42,6 +42,9 @@ def test_products_of_rows_and_scales_far_apart(T, k, power, dtype):
         got = B.elb_gemm_i8(q, s, W, small, dtype=DT[dtype], residual=r)
         torch.cuda.synchronize()
         assert torch.equal(got, want) and bool(want.isfinite().all())
+    away = B.elb_gemm_i8(q, -s, W, small, dtype=DT[dtype])  # a scale's sign is the caller's affair
+    torch.cuda.synchronize()
+    assert torch.equal(away, -B.elb_linear_i8(x, W, c))
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
