@@ -72,8 +72,11 @@ struct GateGradOut {  // from dh, g and u: dg and du [T, 2m], h [T, m]
         for (int q = 0; q < 8; ++q) {
             const float s = sigma(g[q], T());
             const float gs = g[q] * s;
-            // sigma' first: dh u alone may pass the largest fp32 where a closed gate brings it back
-            dg[q] = dh[q] * (u[q] * (s + gs * (1.0f - s)));
+            // the larger of dh and u times sigma' first: no step leaves fp32's range where dg does not
+            // (dh u may pass the largest number before a closed gate, the smaller times sigma' the
+            // smallest)
+            const bool up = fabsf(u[q]) > fabsf(dh[q]);
+            dg[q] = (s + gs * (1.0f - s)) * (up ? u[q] : dh[q]) * (up ? dh[q] : u[q]);
             du[q] = dh[q] * gs;
             hh[q] = gs * u[q];
         }

@@ -82,3 +82,19 @@ def test_gradients_of_closed_gates(T, dtype):
                                      ("dx", "dW_gate_up", "dW_down")):
         assert bool(ref.isfinite().all()) and float(ref.abs().max()) < 2.0 ** 126
         R.within(got, ref, bound, name)
+
+
+@pytest.mark.parametrize("T", [3, 300])
+def test_gradients_of_small_up_projections(T):
+    """The other way round: dh of 2^60 and u of 2^-114 behind gates of -10 to -20: u sigma'(g) alone
+    would be below the smallest normal number, dg is not."""
+    d = m = 64
+    x = _rand((T, d), T)
+    Wgu, Wd = _rand((2 * m, d), 1) / 8, torch.eye(d, device="cuda")
+    dy = 2.0 ** 60 * (1 + _rand((T, d), 2).abs())
+    g = -10 - 10 * torch.rand((T, m), device="cuda", generator=torch.Generator("cuda").manual_seed(3))
+    kept = torch.cat([g, 2.0 ** -114 * (1 + _rand((T, m), 4).abs())], 1)
+    dW = B.elb_ffn_backward(dy, x, Wgu, Wd, kept, need=(False, True, False))[1]
+    torch.cuda.synchronize()
+    refs, bounds = R.ffn_backward(dy, x, Wgu, Wd, kept)
+    R.within(dW[:m], refs[1][:m], bounds[1][:m], "dW_gate")
