@@ -159,7 +159,7 @@ def prepare(case, seed):
         d = case["d"]
         s["residual"], s["block"] = (_normal(gen, (T, d), 1.0, dt) for _ in range(2))
         s["w_post"], s["w_pre"] = (_normal(gen, (d,), 0.1, dt, 1.0) for _ in range(2))
-        shape = {"none": None, "channel": (d,), "token": (T,), "full": (T, d)}[case["gate"]]
+        shape = {"none": None, "channel": (d,), "token": (T, 1), "full": (T, d)}[case["gate"]]
         s["gate"] = None if shape is None else _normal(gen, shape, 0.1, dt, 1.0)
         if kind == "norm_train":
             s["ds"], s["dn"] = (_normal(gen, (T, d), 1e-3, dt) for _ in range(2))
@@ -233,8 +233,6 @@ def _run_norm_plain(s):
     alpha, beta = case["residual_scale"], case["block_scale"]
     b, w_post, w_pre = s["block"].float(), s["w_post"].float(), s["w_pre"].float()
     gate = torch.ones((), device=b.device) if s["gate"] is None else s["gate"].float()
-    if case["gate"] == "token":
-        gate = gate[:, None]
     r_b = (b.square().mean(-1, keepdim=True) + EPS).rsqrt()
     b_hat = b * r_b
     p = w_post * b_hat
@@ -253,7 +251,7 @@ def _run_norm_plain(s):
         if case["gate"] == "full":
             out.append(q * p)
         elif case["gate"] == "token":
-            out.append((q * p).sum(-1))
+            out.append((q * p).sum(-1, keepdim=True))
         elif case["gate"] == "channel":
             out.append((q * p).sum(0, dtype=torch.float64))
         out += [(dp * b_hat).sum(0, dtype=torch.float64), (dn * s_hat).sum(0, dtype=torch.float64)]
@@ -330,7 +328,7 @@ def _exact_norm(s):
 
     add = normed(leaf["block"], leaf["w_post"]) * case["block_scale"]
     if "gate" in leaf:
-        add = add * (leaf["gate"].unsqueeze(1) if case["gate"] == "token" else leaf["gate"])
+        add = add * leaf["gate"]
     total = leaf["residual"] * case["residual_scale"] + add
     n = normed(total, leaf["w_pre"])
     out = (total.detach(), n.detach())
