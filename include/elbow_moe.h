@@ -375,6 +375,149 @@ int elb_ffn_forward_i8(const void *x, const int8_t *W_gate_up, const float *gate
                        size_t workspace_bytes, void *stream);
 
 /*
+ * Norms before and after a block, fused with its gate and the residual stream (an RMS norm has
+ * no mean and no bias).  Per token:
+ *   r_post = 1 / sqrt(mean(block^2) + eps),  p = w_post * block r_post     (w_post NULL: p = block)
+ *   sum    = residual_scale residual + block_scale gate * p
+ *   r_pre  = 1 / sqrt(mean(sum^2) + eps),    normed = w_pre * sum r_pre
+ * `block` is a block's output, `sum` the residual stream after it and `normed` the next block's
+ * input.  Without a block the call is a pre-norm alone, without w_pre the end of a block alone.
+ *   residual [T, d] dtype   or NULL: none (then block is required)
+ *   block    [T, d] dtype   or NULL: none (then gate and w_post have to be NULL too)
+ *   gate            dtype   by gate_kind: NULL, [d], [T] or [T, d]
+ *   w_post   [d]    dtype   or NULL: the block's output is not normalised
+ *   w_pre    [d]    dtype   or NULL: normed is not computed
+ *   eps                     finite, > 0
+ * Sums are fp32; sum and normed are each rounded once (normed from the unrounded sum).
+ * Requirements: d a positive multiple of 16, at most ELB_NORM_MAX_DIM; T < 2^31.
+ */
+#define ELB_NORM_MAX_DIM 16384
+typedef enum {
+    ELB_GATE_NONE = 0,
+    ELB_GATE_CHANNEL = 1, /* [d], the same for every token */
+    ELB_GATE_TOKEN = 2,   /* [T], the same for every channel */
+    ELB_GATE_FULL = 3     /* [T, d] */
+} elb_gate;
+
+typedef struct {
+    const void *residual, *block, *gate, *w_post, *w_pre;
+    int64_t T;
+    int32_t d;
+    int32_t gate_kind; /* elb_gate */
+    int32_t dtype;     /* elb_dtype */
+    float residual_scale, block_scale, eps;
+} elb_norm;
+
+/*
+ *   sum    [T, d] dtype  output, or NULL: not written; may be residual
+ *   normed [T, d] dtype  output; NULL exactly where w_pre is
+ *   r_post [T], r_pre [T] float  optional outputs (NULL: not written), for elb_norm_backward; r_post
+ *                        is written only with w_post, r_pre only with w_pre
+ * Apart from sum and residual, outputs share memory with no other tensor.
+ */
+int elb_norm_forward(const elb_norm *op, void *sum, void *normed, float *r_post, float *r_pre,
+                     void *stream);
+
+/*
+ * Gradients of elb_norm_forward from those of sum (as what comes later uses it) and normed:
+ *   s^ = sum r_pre,   S = d_sum + r_pre (w_pre * d_normed - s^ mean(s^ * w_pre * d_normed))
+ *   b^ = block r_post, q = block_scale S, d_p = q * gate
+ *   d_residual = residual_scale S,  d_block = r_post (w_post * d_p - b^ mean(b^ * w_post * d_p))
+ *   d_gate = q * p, d_w_post = d_p * b^, d_w_pre = d_normed * s^, the last three summed over what
+ *   the tensor is broadcast to
+ *   op                 as given to elb_norm_forward (residual is not read)
+ *   d_sum, d_normed    [T, d] dtype, either may be NULL (zero); d_normed needs w_pre, sum and r_pre
+ *   sum                [T, d] dtype as written by elb_norm_forward (for a pre-norm alone with
+ *                      residual_scale 1: the residual); read only with d_normed
+ *   r_post, r_pre      as written by elb_norm_forward
+ *   d_residual, d_block, d_gate, d_w_post, d_w_pre   outputs of dtype in the shapes of their tensors,
+ *                      each NULL: not computed; d_block, d_gate and d_w_post need the block
+ *   workspace          at least elb_norm_backward_workspace_bytes(T, d) bytes
+ * Outputs are overwritten and share memory with no other tensor of the call.  Sums are fp32 in a
+ * fixed order.  With T = 0 the gradients of w_post, w_pre and a gate per channel are written as zeros.
+ */
+size_t elb_norm_backward_workspace_bytes(int64_t T, int32_t d);
+int elb_norm_backward(const elb_norm *op, const void *d_sum, const void *d_normed, const void *sum,
+                      const float *r_post, const float *r_pre, void *d_residual, void *d_block,
+                      void *d_gate, void *d_w_post, void *d_w_pre, void *workspace,
+                      size_t workspace_bytes, void *stream);
+
+/*
+ * Rows to 4-bit values with a power-of-two scale for every 32 along the row (the layout of the 4-bit
+ * weights below):
+ *   a value is e2m1: code c in 0 .. 7 stands for 0, 0.5, 1, 1.5, 2, 3, 4, 6, c + 8 for its negative;
+ *   the byte at column i / 2 holds value i (even) in its low half and value i + 1 in its high half
+ *   a scale byte b stands for 2^(b - 127) (255: NaN)
+ * b is the least from 2 to 252 for which the group's largest magnitude is at most 6 2^(b - 127)
+ * (larger ones saturate), 255 for a group with an infinity or a NaN; values are rounded to the nearest
+ * of the eight, ties to the even code.
+ *   x     [rows, d]       dtype
+ *   q     [rows, d / 2]   uint8 output
+ *   scale [rows, d / 32]  uint8 output; x, q and scale share no memory
+ * Requirements: d a positive multiple of 32, at most 2^20; rows < 2^31.
+ */
+int elb_quantize_f4(const void *x, int64_t rows, int32_t d, int32_t dtype, uint8_t *q,
+                    uint8_t *scale, void *stream);
+
+/*
+ * A projection with 4-bit weights: y_tn = [residual_tn +] sum_i x_ti W_ni, W_ni the value of code
+ * (n, i) times its group's scale.
+ *   x        [T, k]       dtype
+ *   W        [n, k / 2]   uint8, W_scale [n, k / 32] uint8   as elb_quantize_f4 lays them out; scale
+ *                         bytes from 2 to 252 (others give unspecified, but in-bounds, results)
+ *   residual [T, n]       dtype   optional (NULL: none)
+ *   y        [T, n]       dtype   output; may be residual, shares memory with no other input
+ *   workspace             at least elb_linear_f4_workspace_bytes(T, n, k, dtype) bytes (may be 0)
+ * Products are exact, sums fp32, y is rounded once.
+ * Requirements: n a positive multiple of 16, k of 32, both at most 2^20; T < 2^31.
+ */
+size_t elb_linear_f4_workspace_bytes(int64_t T, int32_t n, int32_t k, int32_t dtype);
+int elb_linear_f4(const void *x, const uint8_t *W, const uint8_t *W_scale, const void *residual,
+                  int64_t T, int32_t n, int32_t k, int32_t dtype, void *y, void *workspace,
+                  size_t workspace_bytes, void *stream);
+
+/*
+ * The dense gated feed-forward block (elb_ffn_forward) with 4-bit weights.
+ *   x [T, d], residual [T, d] (or NULL), y [T, d]   dtype; y may be residual, and may share memory
+ *                                                   with x, with no other input
+ *   W_gate_up [2m, d / 2], gate_up_scale [2m, d / 32], W_down [d, m / 2], down_scale [d, m / 32]
+ *                                                   uint8, as for elb_linear_f4
+ *   workspace  at least elb_ffn_f4_workspace_bytes(T, d, m, dtype) bytes
+ * For ELB_BF16 h is rounded to bf16 before the second product, as in elb_ffn_forward.
+ * Requirements: d and m positive multiples of 32, at most 2^20; T < 2^31.
+ */
+size_t elb_ffn_f4_workspace_bytes(int64_t T, int32_t d, int32_t m, int32_t dtype);
+int elb_ffn_forward_f4(const void *x, const uint8_t *W_gate_up, const uint8_t *gate_up_scale,
+                       const uint8_t *W_down, const uint8_t *down_scale, const void *residual,
+                       int64_t T, int32_t d, int32_t m, int32_t dtype, void *y, void *workspace,
+                       size_t workspace_bytes, void *stream);
+
+/*
+ * The whole layer for at most ELB_FEW_TOKENS tokens in two launches, with experts in bf16 or in 4
+ * bits: routing as elb_moe_forward (the same bits of k, ids and w), then
+ *   y_t = [residual_t +] sum_{j<k_t} W_down[ids_tj] h_tj,
+ *   h_tj = w_tj silu(W_gate[ids_tj] x_t) * (W_up[ids_tj] x_t)
+ * with fp32 sums; h is rounded to bf16, y once at the end.
+ *   x [T, d], W_router [N, d], residual [T, d] (or NULL)   bf16
+ *   y [T, d]             bf16 output; may be residual or x, shares memory with no other tensor
+ *   gate_up_scale, down_scale   both NULL: W_gate_up [N, 2m, d] and W_down [N, d, m] are bf16;
+ *                        otherwise uint8 [N, 2m, d / 32] and [N, d, m / 32], and the weights uint8
+ *                        [N, 2m, d / 2] and [N, d, m / 2], as for elb_linear_f4
+ *   workspace            at least elb_moe_few_workspace_bytes(T, d, N, m, K) bytes
+ *   k_out [T], ids_out [T, K], w_out [T, K]   optional outputs (NULL: not written), as elb_route
+ * Requirements: T <= ELB_FEW_TOKENS (more: ELB_ERR_UNSUPPORTED), d and m positive multiples of 64, at
+ * most 2^20; 2 <= N <= ELB_MAX_EXPERTS, K <= 16 (a larger cap: ELB_ERR_UNSUPPORTED).
+ */
+#define ELB_FEW_TOKENS 16
+size_t elb_moe_few_workspace_bytes(int64_t T, int32_t d, int32_t N, int32_t m, int32_t K);
+int elb_moe_forward_few(const void *x, const void *W_router, const void *W_gate_up,
+                        const uint8_t *gate_up_scale, const void *W_down, const uint8_t *down_scale,
+                        const void *residual, int64_t T, int32_t d, int32_t N, int32_t m,
+                        const elb_route_params *params, void *y, void *workspace,
+                        size_t workspace_bytes, int32_t *k_out, int32_t *ids_out, float *w_out,
+                        void *stream);
+
+/*
  * Calibration of the matrix-core roofline (a measurement aid, not part of the layer): a
  * kernel of `blocks` blocks of 4 waves, each wave issuing iters x 8 back-to-back
  * v_mfma_f32_32x32x16_bf16 instructions (32 x 32 x 16 multiply-adds each) on register

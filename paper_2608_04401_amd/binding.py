@@ -40,6 +40,16 @@ class RouteParams(C.Structure):
                 ("renormalize", C.c_int32)]
 
 
+GATE_NONE, GATE_CHANNEL, GATE_TOKEN, GATE_FULL = 0, 1, 2, 3
+
+
+class NormOp(C.Structure):
+    _fields_ = [("residual", C.c_void_p), ("block", C.c_void_p), ("gate", C.c_void_p),
+                ("w_post", C.c_void_p), ("w_pre", C.c_void_p), ("T", C.c_int64),
+                ("d", C.c_int32), ("gate_kind", C.c_int32), ("dtype", C.c_int32),
+                ("residual_scale", C.c_float), ("block_scale", C.c_float), ("eps", C.c_float)]
+
+
 def lib():
     """Load libelbow_moe.so (built by paper_2608_04401_amd.build); raise if it is missing."""
     global _lib
@@ -87,6 +97,17 @@ def lib():
         "elb_linear_i8": ([P, P, P, P, I64, I32, I32, I32, P, P, SZ, P], C.c_int),
         "elb_ffn_i8_workspace_bytes": ([I64, I32, I32], SZ),
         "elb_ffn_forward_i8": ([P, P, P, P, P, P, I64, I32, I32, I32, P, P, SZ, P], C.c_int),
+        "elb_norm_forward": ([C.POINTER(NormOp), P, P, P, P, P], C.c_int),
+        "elb_norm_backward_workspace_bytes": ([I64, I32], SZ),
+        "elb_norm_backward": ([C.POINTER(NormOp)] + [P] * 11 + [SZ, P], C.c_int),
+        "elb_quantize_f4": ([P, I64, I32, I32, P, P, P], C.c_int),
+        "elb_linear_f4_workspace_bytes": ([I64, I32, I32, I32], SZ),
+        "elb_linear_f4": ([P, P, P, P, I64, I32, I32, I32, P, P, SZ, P], C.c_int),
+        "elb_ffn_f4_workspace_bytes": ([I64, I32, I32, I32], SZ),
+        "elb_ffn_forward_f4": ([P, P, P, P, P, P, I64, I32, I32, I32, P, P, SZ, P], C.c_int),
+        "elb_moe_few_workspace_bytes": ([I64, I32, I32, I32, I32], SZ),
+        "elb_moe_forward_few": ([P] * 7 + [I64, I32, I32, I32, C.POINTER(RouteParams), P, P, SZ,
+                                           P, P, P, P], C.c_int),
         "elb_calibrate_mfma_bf16": ([I32, I32, P, P], C.c_int64),
         "elb_calibrate_read_stream": ([P, I64, I32, P, P], C.c_int),
         "elb_profile_enable": ([C.c_int], C.c_int),
@@ -587,6 +608,207 @@ def elb_ffn_forward_i8(x, W_gate_up, gate_up_scale, W_down, down_scale, residual
         _ptr(x), _ptr(W_gate_up), _ptr(gate_up_scale), _ptr(W_down), _ptr(down_scale),
         _ptr(residual), T, d, m, dt, _ptr(y), _ptr(ws), ws.numel(), stream))
     return y
+
+
+def _norm_op(residual, block, w_post, w_pre, gate, residual_scale, block_scale, eps):
+    """(NormOp, T, d, a tensor of the stream's shape, device); the operands checked."""
+    like = block if block is not None else residual
+    if like is None:
+        raise ValueError("neither residual nor block")
+    T, d = _matrix("residual" if block is None else "block", like)
+    dt, dev = _dtype_code(like), _device(like)
+    _want("residual", residual, (T, d), like.dtype, dev)
+    _want("block", block, (T, d), like.dtype, dev)
+    _want("w_post", w_post, (d,), like.dtype, dev)
+    _want("w_pre", w_pre, (d,), like.dtype, dev)
+    kind = GATE_NONE
+    if gate is not None:
+        # [T, d] before [T, 1] and [d]: with d >= 16 no shape is two of them
+        kinds = {(T, d): GATE_FULL, (T, 1): GATE_TOKEN, (d,): GATE_CHANNEL}
+        kind = kinds.get(tuple(gate.shape))
+        if kind is None:
+            raise ValueError("gate must have shape [T, d], [T, 1] or [d], not %s"
+                             % (tuple(gate.shape),))
+        _want("gate", gate, gate.shape, like.dtype, dev)
+    op = NormOp(_ptr(residual), _ptr(block), _ptr(gate), _ptr(w_post), _ptr(w_pre), T, d, kind, dt,
+                residual_scale, block_scale, eps)
+    return op, T, d, like, dev
+
+
+def elb_norm_forward(residual=None, block=None, w_post=None, w_pre=None, gate=None,
+                     residual_scale: float = 1.0, block_scale: float = 1.0, eps: float = 1e-6,
+                     out=None, keep: bool = False):
+    """sum = residual_scale residual + block_scale gate * norm(block) (not normalised without
+    w_post) and normed = the norm of sum with w_pre (None without).  -> (sum, normed), or with
+    keep=True (sum, normed, kept): kept is what elb_norm_backward needs of the forward pass.
+    gate: [d], [T, 1], [T, d] or None.  out (of sum) may be residual.  Without a block, an out and a
+    residual_scale, sum is residual itself.  Outside autograd: results never require a gradient."""
+    op, T, d, like, dev = _norm_op(residual, block, w_post, w_pre, gate, residual_scale,
+                                   block_scale, eps)
+    _want("out", out, (T, d), like.dtype, dev)
+    same = out is None and block is None and residual_scale == 1.0
+    total = residual.detach() if same else torch.empty_like(like) if out is None else out
+    normed = None if w_pre is None else torch.empty_like(like)
+    kept = (None, None)
+    if keep:
+        kept = tuple(None if w is None else torch.empty(T, dtype=torch.float32, device=like.device)
+                     for w in (w_post, w_pre))
+    _check("elb_norm_forward", lib().elb_norm_forward(
+        C.byref(op), None if same else _ptr(total), _ptr(normed), _ptr(kept[0]), _ptr(kept[1]),
+        _stream()))
+    return (total, normed, kept) if keep else (total, normed)
+
+
+@functools.lru_cache(maxsize=256)
+def elb_norm_backward_workspace_bytes(T: int, d: int) -> int:
+    return int(lib().elb_norm_backward_workspace_bytes(T, d))
+
+
+def elb_norm_backward(d_sum, d_normed, sum, block, kept, w_post=None, w_pre=None, gate=None,
+                      residual_scale: float = 1.0, block_scale: float = 1.0,
+                      need=(True, True, True, True, True)):
+    """-> (d_residual, d_block, d_gate, d_w_post, d_w_pre), None where need is false or the forward
+    had no such tensor (d_residual always is computed if needed).  d_sum or d_normed may be None
+    (zero).  sum and kept from elb_norm_forward(..., keep=True), the rest as given to it."""
+    op, T, d, like, dev = _norm_op(sum if block is None else None, block, w_post, w_pre, gate,
+                                   residual_scale, block_scale, 1.0)
+    _want("d_sum", d_sum, (T, d), like.dtype, dev)
+    _want("d_normed", d_normed, (T, d), like.dtype, dev)
+    _want("sum", sum, (T, d), like.dtype, dev)
+    r_post, r_pre = kept
+    _want("kept", r_post, (T,), torch.float32, dev)
+    _want("kept", r_pre, (T,), torch.float32, dev)
+    shapes = (like, block, gate, w_post, w_pre)
+    out = [torch.empty_like(t) if n and t is not None else None for t, n in zip(shapes, need)]
+    stream = _stream()
+    ws = workspace(elb_norm_backward_workspace_bytes(T, d), like.device, stream)
+    _check("elb_norm_backward", lib().elb_norm_backward(
+        C.byref(op), _ptr(d_sum), _ptr(d_normed), _ptr(sum), _ptr(r_post), _ptr(r_pre),
+        *(_ptr(t) for t in out), _ptr(ws), ws.numel(), stream))
+    return tuple(out)
+
+
+def elb_quantize_f4(x: torch.Tensor):
+    """-> (q [rows, d / 2] uint8, scale [rows, d / 32] uint8): 4-bit values with a power-of-two scale
+    for every 32 of a row, in the layout that elb_linear_f4 takes.  Weights with leading dimensions
+    ([N, rows, d]) keep them."""
+    if x.dim() < 2:
+        raise ValueError("x must have two dimensions or more, not %d" % x.dim())
+    d = x.shape[-1]
+    dt = _dtype_code(x)
+    _want("x", x, x.shape, x.dtype, _device(x))
+    lead = tuple(x.shape[:-1])
+    q = torch.empty(lead + (d // 2,), dtype=torch.uint8, device=x.device)
+    scale = torch.empty(lead + (d // 32,), dtype=torch.uint8, device=x.device)
+    _check("elb_quantize_f4", lib().elb_quantize_f4(_ptr(x), x.numel() // max(d, 1), d, dt, _ptr(q),
+                                                    _ptr(scale), _stream()))
+    return q, scale
+
+
+@functools.lru_cache(maxsize=256)
+def elb_linear_f4_workspace_bytes(T: int, n: int, k: int, dtype: int) -> int:
+    return int(lib().elb_linear_f4_workspace_bytes(T, n, k, dtype))
+
+
+def elb_linear_f4(x, W, W_scale, residual=None, out=None) -> torch.Tensor:
+    """y [T, n] = [residual +] x [T, k] times 4-bit W [n, k / 2] with W_scale [n, k / 32]
+    (elb_quantize_f4).  out may be residual, not x."""
+    T, k = _matrix("x", x)
+    n = _matrix("W", W)[0]
+    dt = _dtype_code(x)
+    dev = _device(x)
+    _want("x", x, (T, k), x.dtype, dev)
+    _want("W", W, (n, k // 2), torch.uint8, dev)
+    _want("W_scale", W_scale, (n, k // 32), torch.uint8, dev)
+    _want("residual", residual, (T, n), x.dtype, dev)
+    _want("out", out, (T, n), x.dtype, dev)
+    y = torch.empty((T, n), dtype=x.dtype, device=x.device) if out is None else out
+    stream = _stream()
+    ws = workspace(elb_linear_f4_workspace_bytes(T, n, k, dt), x.device, stream)
+    _check("elb_linear_f4", lib().elb_linear_f4(
+        _ptr(x), _ptr(W), _ptr(W_scale), _ptr(residual), T, n, k, dt, _ptr(y), _ptr(ws),
+        ws.numel(), stream))
+    return y
+
+
+@functools.lru_cache(maxsize=256)
+def elb_ffn_f4_workspace_bytes(T: int, d: int, m: int, dtype: int) -> int:
+    return int(lib().elb_ffn_f4_workspace_bytes(T, d, m, dtype))
+
+
+def elb_ffn_forward_f4(x, W_gate_up, gate_up_scale, W_down, down_scale, residual=None,
+                       out=None) -> torch.Tensor:
+    """The dense gated feed-forward block with 4-bit weights (elb_quantize_f4 of the float ones):
+    W_gate_up [2m, d / 2], gate_up_scale [2m, d / 32], W_down [d, m / 2], down_scale [d, m / 32].
+    out may be residual or x."""
+    T, d = _matrix("x", x)
+    m = 2 * _matrix("W_down", W_down)[1]
+    dt = _dtype_code(x)
+    dev = _device(x)
+    _want("x", x, (T, d), x.dtype, dev)
+    _want("W_gate_up", W_gate_up, (2 * m, d // 2), torch.uint8, dev)
+    _want("gate_up_scale", gate_up_scale, (2 * m, d // 32), torch.uint8, dev)
+    _want("W_down", W_down, (d, m // 2), torch.uint8, dev)
+    _want("down_scale", down_scale, (d, m // 32), torch.uint8, dev)
+    _want("residual", residual, (T, d), x.dtype, dev)
+    _want("out", out, (T, d), x.dtype, dev)
+    y = torch.empty_like(x) if out is None else out
+    stream = _stream()
+    ws = workspace(elb_ffn_f4_workspace_bytes(T, d, m, dt), x.device, stream)
+    _check("elb_ffn_forward_f4", lib().elb_ffn_forward_f4(
+        _ptr(x), _ptr(W_gate_up), _ptr(gate_up_scale), _ptr(W_down), _ptr(down_scale),
+        _ptr(residual), T, d, m, dt, _ptr(y), _ptr(ws), ws.numel(), stream))
+    return y
+
+
+FEW_TOKENS = 16
+
+
+@functools.lru_cache(maxsize=256)
+def elb_moe_few_workspace_bytes(T: int, d: int, N: int, m: int, K: int) -> int:
+    return int(lib().elb_moe_few_workspace_bytes(T, d, N, m, K))
+
+
+def elb_moe_forward_few(x, W_router, W_gate_up, W_down, K: int = 8, eps: float = 1e-8,
+                        mode: int = MODE_ELBOW, renormalize: bool = False, residual=None,
+                        out=None, debug: bool = False, gate_up_scale=None, down_scale=None):
+    """The whole bf16 layer for at most FEW_TOKENS tokens in two launches.  W_gate_up [N, 2m, d] and
+    W_down [N, d, m] bf16; or, with gate_up_scale and down_scale, the 4-bit ones of elb_quantize_f4
+    (uint8 [N, 2m, d / 2] and [N, d, m / 2], scales [N, 2m, d / 32] and [N, d, m / 32]).  out may be
+    residual or x.  Returns y, or (y, {"k", "ids", "w"}) when debug=True."""
+    T, d = _matrix("x", x)
+    if W_down.dim() != 3:
+        raise ValueError("W_down must have three dimensions, not %d" % W_down.dim())
+    if (gate_up_scale is None) != (down_scale is None):
+        raise ValueError("gate_up_scale and down_scale go together")
+    f4 = gate_up_scale is not None
+    N, m = W_down.shape[0], W_down.shape[2] * (2 if f4 else 1)
+    if x.dtype != torch.bfloat16:
+        raise TypeError("x must be torch.bfloat16, not %s" % x.dtype)
+    dev = _device(x)
+    dt, half = (torch.uint8, 2) if f4 else (torch.bfloat16, 1)
+    _want("x", x, (T, d), x.dtype, dev)
+    _want("W_router", W_router, (N, d), x.dtype, dev)
+    _want("W_gate_up", W_gate_up, (N, 2 * m, d // half), dt, dev)
+    _want("W_down", W_down, (N, d, m // half), dt, dev)
+    _want("gate_up_scale", gate_up_scale, (N, 2 * m, d // 32), torch.uint8, dev)
+    _want("down_scale", down_scale, (N, d, m // 32), torch.uint8, dev)
+    _want("residual", residual, (T, d), x.dtype, dev)
+    _want("out", out, (T, d), x.dtype, dev)
+    y = torch.empty_like(x) if out is None else out
+    dbg = {}
+    if debug:
+        dbg = {"k": torch.empty(T, dtype=torch.int32, device=x.device),
+               "ids": torch.empty((T, K), dtype=torch.int32, device=x.device),
+               "w": torch.empty((T, K), dtype=torch.float32, device=x.device)}
+    p = RouteParams(K, eps, mode, int(renormalize))
+    stream = _stream()
+    ws = workspace(elb_moe_few_workspace_bytes(T, d, N, m, K), x.device, stream)
+    _check("elb_moe_forward_few", lib().elb_moe_forward_few(
+        _ptr(x), _ptr(W_router), _ptr(W_gate_up), _ptr(gate_up_scale), _ptr(W_down),
+        _ptr(down_scale), _ptr(residual), T, d, N, m, C.byref(p), _ptr(y), _ptr(ws), ws.numel(),
+        _ptr(dbg.get("k")), _ptr(dbg.get("ids")), _ptr(dbg.get("w")), stream))
+    return (y, dbg) if debug else y
 
 
 def elb_calibrate_read_stream(buf: torch.Tensor, blocks: int, out: torch.Tensor) -> None:

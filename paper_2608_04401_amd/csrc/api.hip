@@ -234,6 +234,58 @@ I8Layout i8_layout(int64_t T, int d, int m, bool most) {
     return L;
 }
 
+// ---- norms ----
+int check_norm(const elb_norm* p) {
+    if (!p) return fail(ELB_ERR_INVALID_ARG, "op is NULL");
+    if (int rc = check_dtype(p->dtype)) return rc;
+    if (int rc = check_dense(p->T, p->d, "d", 16, "d")) return rc;
+    if (p->d > ELB_NORM_MAX_DIM)
+        return fail(ELB_ERR_UNSUPPORTED, "d = %d exceeds ELB_NORM_MAX_DIM = %d", p->d,
+                    ELB_NORM_MAX_DIM);
+    if (p->gate_kind < ELB_GATE_NONE || p->gate_kind > ELB_GATE_FULL)
+        return fail(ELB_ERR_INVALID_ARG, "gate_kind = %d is not an elb_gate", p->gate_kind);
+    if (!(p->eps > 0.f) || !std::isfinite(p->eps))
+        return fail(ELB_ERR_INVALID_ARG, "eps = %g must be finite and > 0", (double)p->eps);
+    return ELB_OK;
+}
+int64_t gate_values(const elb_norm& p) {
+    return p.gate_kind == ELB_GATE_CHANNEL ? p.d
+           : p.gate_kind == ELB_GATE_TOKEN ? p.T
+           : p.gate_kind == ELB_GATE_FULL  ? p.T * p.d
+                                           : 0;
+}
+
+// ---- 4-bit weights ----
+int check_f4(int64_t T, int n, const char* nn, int k, const char* kn) {
+    if (int rc = check_dense(T, n, nn, k, kn)) return rc;
+    if (k % 32)
+        return fail(ELB_ERR_INVALID_ARG, "%s = %d must be a multiple of 32 (a group of 4-bit values)",
+                    kn, k);
+    return ELB_OK;
+}
+// sub-buffers of a projection's and the block's workspace; `most` as above
+struct F4Layout {
+    size_t h, wgu, wd, part, total;
+};
+F4Layout f4_layout(int64_t T, int n, int64_t k, int m, int dtype, bool most) {
+    F4Layout L{};
+    size_t o = 0;
+    auto take = [&](size_t bytes) {
+        const size_t at = o;
+        o += align_up(bytes);
+        return at;
+    };
+    const size_t e = esize(dtype);
+    L.h = take((size_t)T * m * e);
+    if (!f4_streams(T, dtype)) {
+        L.wgu = take((size_t)2 * m * n * e);
+        L.wd = take((size_t)n * k * e);
+        L.part = take(ffn_halves_bytes(T, n, k, dtype, most));
+    }
+    L.total = o;
+    return L;
+}
+
 // ---- the static scratch of the allocation-free entry point ----
 // One array per GPU the library runs on (a __device__ variable lives in each device's copy of
 // the code object).  In host code `scratch` is only a stand-in symbol: its device address is
@@ -861,6 +913,234 @@ int elb_ffn_forward_i8(const void* x, const int8_t* W_gate_up, const float* gate
     return hip_status(launch_linear_i8(h, ELB_F32, W_down, down_scale, residual, T, d, m, dtype, y,
                                        hq, hs, ws + L.part, s),
                       "linear_i8");
+}
+
+int elb_norm_forward(const elb_norm* op, void* sum, void* normed, float* r_post, float* r_pre,
+                     void* stream) {
+    g_err.clear();
+    if (int rc = check_norm(op)) return rc;
+    const elb_norm& p = *op;
+    if (p.T == 0) return ELB_OK;  // (tensors without a value may have no address)
+    if (!p.w_pre != !normed)
+        return fail(ELB_ERR_INVALID_ARG, "normed and w_pre go together");
+    if (!sum && !normed) return ELB_OK;  // nothing asked for
+    if (!p.residual && !p.block)
+        return fail(ELB_ERR_INVALID_ARG, "NULL tensor pointer: neither residual nor block");
+    if (!p.block && (p.w_post || p.gate_kind != ELB_GATE_NONE))
+        return fail(ELB_ERR_INVALID_ARG, "w_post and gate belong to a block");
+    if (p.gate_kind != ELB_GATE_NONE && !p.gate)
+        return fail(ELB_ERR_INVALID_ARG, "NULL tensor pointer: gate");
+    const int64_t e = esize(p.dtype), all = p.T * p.d * e;
+    const Span res{"residual", p.residual, all}, block{"block", p.block, all},
+        gate{"gate", p.gate_kind ? p.gate : nullptr, gate_values(p) * e},
+        post{"w_post", p.w_post, p.d * e}, pre{"w_pre", p.w_pre, p.d * e}, o_sum{"sum", sum, all},
+        o_normed{"normed", normed, all}, o_post{"r_post", p.w_post ? r_post : nullptr, p.T * 4},
+        o_pre{"r_pre", p.w_pre ? r_pre : nullptr, p.T * 4};
+    if (int rc = check_apart(o_sum, {block, gate, post, pre, o_normed, o_post, o_pre})) return rc;
+    if (sum != p.residual)
+        if (int rc = check_apart(o_sum, {res})) return rc;
+    if (int rc = check_apart(o_normed, {res, block, gate, post, pre, o_post, o_pre})) return rc;
+    if (int rc = check_apart(o_post, {res, block, gate, post, pre, o_pre})) return rc;
+    if (int rc = check_apart(o_pre, {res, block, gate, post, pre})) return rc;
+    return hip_status(launch_norm_forward(p, sum, normed, r_post, r_pre, (hipStream_t)stream),
+                      "norm_forward");
+}
+
+size_t elb_norm_backward_workspace_bytes(int64_t T, int32_t d) {
+    if (T < 0 || d < 1) return 0;
+    return align_up((size_t)norm_backward_blocks(T, d) * 3 * d * 4);
+}
+
+int elb_norm_backward(const elb_norm* op, const void* d_sum, const void* d_normed, const void* sum,
+                      const float* r_post, const float* r_pre, void* d_residual, void* d_block,
+                      void* d_gate, void* d_w_post, void* d_w_pre, void* workspace,
+                      size_t workspace_bytes, void* stream) {
+    g_err.clear();
+    if (int rc = check_norm(op)) return rc;
+    const elb_norm& p = *op;
+    if (!d_residual && !d_block && !d_gate && !d_w_post && !d_w_pre) return ELB_OK;
+    if (d_gate && p.gate_kind == ELB_GATE_NONE)
+        return fail(ELB_ERR_INVALID_ARG, "d_gate without a gate");
+    if ((d_w_post && !p.w_post) || (d_w_pre && !p.w_pre))
+        return fail(ELB_ERR_INVALID_ARG, "a norm weight's gradient without the weight");
+    if (p.T > 0) {
+        if (!d_sum && !d_normed)
+            return fail(ELB_ERR_INVALID_ARG, "NULL tensor pointer: neither d_sum nor d_normed");
+        if (d_normed && (!p.w_pre || !sum || !r_pre))
+            return fail(ELB_ERR_INVALID_ARG, "NULL tensor pointer: d_normed needs w_pre, sum and r_pre");
+        if ((d_block || d_gate || d_w_post) &&
+            (!p.block || (p.w_post && !r_post) || (p.gate_kind != ELB_GATE_NONE && !p.gate)))
+            return fail(ELB_ERR_INVALID_ARG, "NULL tensor pointer: block, r_post or gate");
+        if (int rc = check_workspace(workspace, workspace_bytes,
+                                     elb_norm_backward_workspace_bytes(p.T, p.d)))
+            return rc;
+    }
+    const int64_t e = esize(p.dtype), all = p.T * p.d * e, row = p.d * e;
+    const Span in[] = {{"d_sum", d_sum, all}, {"d_normed", d_normed, all}, {"sum", sum, all},
+                       {"r_post", r_post, p.T * 4}, {"r_pre", r_pre, p.T * 4},
+                       {"block", p.block, all},
+                       {"gate", p.gate_kind ? p.gate : nullptr, gate_values(p) * e},
+                       {"w_post", p.w_post, row}, {"w_pre", p.w_pre, row}};
+    const Span out[] = {{"d_residual", d_residual, all}, {"d_block", d_block, all},
+                        {"d_gate", d_gate, gate_values(p) * e}, {"d_w_post", d_w_post, row},
+                        {"d_w_pre", d_w_pre, row}};
+    for (int i = 0; i < 5; ++i) {
+        for (const Span& o : in)
+            if (int rc = check_apart(out[i], {o})) return rc;
+        for (int j = 0; j < i; ++j)
+            if (int rc = check_apart(out[i], {out[j]})) return rc;
+    }
+    return hip_status(launch_norm_backward(p, d_sum, d_normed, sum, r_post, r_pre, d_residual,
+                                           d_block, d_gate, d_w_post, d_w_pre, workspace,
+                                           (hipStream_t)stream),
+                      "norm_backward");
+}
+
+int elb_quantize_f4(const void* x, int64_t rows, int32_t d, int32_t dtype, uint8_t* q,
+                    uint8_t* scale, void* stream) {
+    g_err.clear();
+    if (int rc = check_dtype(dtype)) return rc;
+    if (int rc = check_f4(rows, 16, "d", d, "d")) return rc;
+    if (rows == 0) return ELB_OK;
+    if (!x || !q || !scale) return fail(ELB_ERR_INVALID_ARG, "NULL tensor pointer");
+    const Span in{"x", x, rows * d * (int64_t)esize(dtype)}, scales{"scale", scale, rows * (d / 32)};
+    if (int rc = check_apart({"q", q, rows * (d / 2)}, {in, scales})) return rc;
+    if (int rc = check_apart(scales, {in})) return rc;
+    return hip_status(launch_quantize_f4(x, rows, d, dtype, q, scale, (hipStream_t)stream),
+                      "quantize_f4");
+}
+
+size_t elb_linear_f4_workspace_bytes(int64_t T, int32_t n, int32_t k, int32_t dtype) {
+    if (T < 0 || n < 1 || k < 1 || (dtype != ELB_F32 && dtype != ELB_BF16)) return 0;
+    return f4_layout(T, n, k, 0, dtype, true).total;
+}
+
+int elb_linear_f4(const void* x, const uint8_t* W, const uint8_t* W_scale, const void* residual,
+                  int64_t T, int32_t n, int32_t k, int32_t dtype, void* y, void* workspace,
+                  size_t workspace_bytes, void* stream) {
+    g_err.clear();
+    if (int rc = check_dtype(dtype)) return rc;
+    if (int rc = check_f4(T, n, "n", k, "k")) return rc;
+    if (T == 0) return ELB_OK;
+    if (!x || !W || !W_scale || !y) return fail(ELB_ERR_INVALID_ARG, "NULL tensor pointer");
+    const F4Layout L = f4_layout(T, n, k, 0, dtype, false);
+    if (L.total)
+        if (int rc = check_workspace(workspace, workspace_bytes, L.total)) return rc;
+    const int64_t e = esize(dtype);
+    const Span out{"y", y, T * n * e};
+    if (int rc = check_apart(out, {{"x", x, T * k * e}, {"W", W, (int64_t)n * (k / 2)},
+                                   {"W_scale", W_scale, (int64_t)n * (k / 32)}}))
+        return rc;
+    if (int rc = check_residual(out, residual)) return rc;
+    char* const ws = (char*)workspace;
+    return hip_status(launch_linear_f4(x, W, W_scale, residual, T, n, k, dtype, y,
+                                       L.total ? ws + L.wd : nullptr,
+                                       L.total ? ws + L.part : nullptr, (hipStream_t)stream),
+                      "linear_f4");
+}
+
+size_t elb_ffn_f4_workspace_bytes(int64_t T, int32_t d, int32_t m, int32_t dtype) {
+    if (T < 0 || d < 1 || m < 1 || (dtype != ELB_F32 && dtype != ELB_BF16)) return 0;
+    return f4_layout(T, d, m, m, dtype, true).total;
+}
+
+int elb_ffn_forward_f4(const void* x, const uint8_t* W_gate_up, const uint8_t* gate_up_scale,
+                       const uint8_t* W_down, const uint8_t* down_scale, const void* residual,
+                       int64_t T, int32_t d, int32_t m, int32_t dtype, void* y, void* workspace,
+                       size_t workspace_bytes, void* stream) {
+    g_err.clear();
+    if (int rc = check_dtype(dtype)) return rc;
+    if (int rc = check_f4(T, m, "m", d, "d")) return rc;
+    if (int rc = check_f4(T, d, "d", m, "m")) return rc;
+    if (T == 0) return ELB_OK;
+    if (!x || !W_gate_up || !gate_up_scale || !W_down || !down_scale || !y)
+        return fail(ELB_ERR_INVALID_ARG, "NULL tensor pointer");
+    const F4Layout L = f4_layout(T, d, m, m, dtype, false);
+    if (int rc = check_workspace(workspace, workspace_bytes, L.total)) return rc;
+    const Span out{"y", y, T * d * (int64_t)esize(dtype)};
+    if (int rc = check_apart(out, {{"W_gate_up", W_gate_up, (int64_t)m * d},
+                                   {"gate_up_scale", gate_up_scale, (int64_t)2 * m * (d / 32)},
+                                   {"W_down", W_down, (int64_t)d * (m / 2)},
+                                   {"down_scale", down_scale, (int64_t)d * (m / 32)}}))
+        return rc;
+    if (int rc = check_residual(out, residual)) return rc;
+    char* const ws = (char*)workspace;
+    return hip_status(launch_ffn_f4(x, W_gate_up, gate_up_scale, W_down, down_scale, residual, T, d,
+                                    m, dtype, ws + L.h, ws + L.wgu, ws + L.wd, ws + L.part, y,
+                                    (hipStream_t)stream),
+                      "ffn_forward_f4");
+}
+
+// sub-buffers of the few-token layer's workspace
+struct FewLayout {
+    size_t h, k, ids, w, total;
+};
+static FewLayout few_layout(int64_t T, int m, int K) {
+    FewLayout L{};
+    const size_t rows = (size_t)T * K;
+    L.k = align_up(rows * m * 2);
+    L.ids = L.k + align_up((size_t)T * 4);
+    L.w = L.ids + align_up(rows * 4);
+    L.total = L.w + align_up(rows * 4);
+    return L;
+}
+
+size_t elb_moe_few_workspace_bytes(int64_t T, int32_t d, int32_t N, int32_t m, int32_t K) {
+    if (T < 0 || T > ELB_FEW_TOKENS || d < 1 || N < 1 || m < 1 || K < 1) return 0;
+    return few_layout(T, m, K).total;
+}
+
+int elb_moe_forward_few(const void* x, const void* W_router, const void* W_gate_up,
+                        const uint8_t* gate_up_scale, const void* W_down, const uint8_t* down_scale,
+                        const void* residual, int64_t T, int32_t d, int32_t N, int32_t m,
+                        const elb_route_params* params, void* y, void* workspace,
+                        size_t workspace_bytes, int32_t* k_out, int32_t* ids_out, float* w_out,
+                        void* stream) {
+    g_err.clear();
+    if (int rc = check_route_params(N, params)) return rc;
+    if (int rc = check_expert_dims(T, d, N, m, params->K, ELB_BF16)) return rc;
+    const int K = params->K;
+    if (T > ELB_FEW_TOKENS)
+        return fail(ELB_ERR_UNSUPPORTED, "T = %lld exceeds ELB_FEW_TOKENS = %d", (long long)T,
+                    ELB_FEW_TOKENS);
+    if (K > kLaneMaxK)
+        return fail(ELB_ERR_UNSUPPORTED, "K = %d: the layer for a few tokens takes caps up to %d", K,
+                    kLaneMaxK);
+    if (d > kMaxDim || m > kMaxDim)
+        return fail(ELB_ERR_UNSUPPORTED, "d = %d or m = %d exceeds %d", d, m, kMaxDim);
+    if (!gate_up_scale != !down_scale)
+        return fail(ELB_ERR_INVALID_ARG, "gate_up_scale and down_scale go together");
+    if (T == 0) return ELB_OK;
+    if (!x || !W_router || !W_gate_up || !W_down || !y)
+        return fail(ELB_ERR_INVALID_ARG, "NULL tensor pointer");
+    const FewLayout L = few_layout(T, m, K);
+    if (int rc = check_workspace(workspace, workspace_bytes, L.total)) return rc;
+    const int64_t weights = (int64_t)N * m * d;  // of a projection
+    const bool f4 = gate_up_scale != nullptr;
+    const Span in[] = {{"x", x, T * d * 2}, {"W_router", W_router, (int64_t)N * d * 2},
+                       {"W_gate_up", W_gate_up, f4 ? weights : weights * 4},
+                       {"W_down", W_down, f4 ? weights / 2 : weights * 2},
+                       {"gate_up_scale", gate_up_scale, weights / 16},
+                       {"down_scale", down_scale, weights / 32},
+                       {"residual", residual, T * d * 2}};
+    const Span out[] = {{"y", y, T * d * 2}, {"k_out", k_out, T * 4}, {"ids_out", ids_out, T * K * 4},
+                        {"w_out", w_out, T * K * 4}};
+    // x is read before y is written, and each value of residual by the lane that writes y
+    if (int rc = check_apart(out[0], {in[1], in[2], in[3], in[4], in[5], out[1], out[2], out[3]}))
+        return rc;
+    if (int rc = check_residual(out[0], residual)) return rc;
+    for (int i = 1; i < 4; ++i) {
+        for (const Span& o : in)
+            if (int rc = check_apart(out[i], {o})) return rc;
+        if (int rc = check_apart(out[i], {out[i % 3 + 1]})) return rc;
+    }
+    char* const ws = (char*)workspace;
+    return hip_status(
+        launch_moe_few(x, W_router, W_gate_up, gate_up_scale, W_down, down_scale, residual, T, d, N,
+                       m, *params, ws, y, k_out ? k_out : (int*)(ws + L.k),
+                       ids_out ? ids_out : (int*)(ws + L.ids),
+                       w_out ? w_out : (float*)(ws + L.w), cus_per_device(), (hipStream_t)stream),
+        "moe_forward_few");
 }
 
 int64_t elb_calibrate_mfma_bf16(int32_t blocks, int32_t iters, float* out, void* stream) {

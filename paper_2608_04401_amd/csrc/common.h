@@ -216,6 +216,40 @@ hipError_t launch_gate_up_i8(const void* x, int dtype, const int8_t* w, const fl
                              int64_t T, int d, int m, float* h, int8_t* q, float* scale,
                              hipStream_t s);
 
+// norms around a block (norm.hip).  The backward's scratch: norm_backward_blocks(T, d) x 3 x d floats
+// for the sums over rows
+constexpr int kNormBlocks = 256;
+int norm_backward_blocks(int64_t T, int d);
+hipError_t launch_norm_forward(const elb_norm& p, void* sum, void* normed, float* r_post,
+                               float* r_pre, hipStream_t s);
+hipError_t launch_norm_backward(const elb_norm& p, const void* ds, const void* dn, const void* sum,
+                                const float* r_post, const float* r_pre, void* dres, void* dblock,
+                                void* dgate, void* dw_post, void* dw_pre, void* part,
+                                hipStream_t s);
+
+// 4-bit weights (f4.hip).  Few tokens stream them as they are; for more they are converted to
+// dtype in scratch (w; wgu and wd) and multiplied by the dense forms, with `part` of ffn_halves_bytes
+bool f4_streams(int64_t T, int dtype);
+hipError_t launch_quantize_f4(const void* x, int64_t rows, int d, int dtype, uint8_t* q,
+                              uint8_t* scale, hipStream_t s);
+hipError_t launch_linear_f4(const void* x, const uint8_t* W, const uint8_t* W_scale,
+                            const void* res, int64_t T, int n, int k, int dtype, void* y, void* w,
+                            void* part, hipStream_t s);
+hipError_t launch_ffn_f4(const void* x, const uint8_t* Wgu, const uint8_t* gu_scale,
+                         const uint8_t* Wd, const uint8_t* d_scale, const void* res, int64_t T,
+                         int d, int m, int dtype, void* h, void* wgu, void* wd, void* part, void* y,
+                         hipStream_t s);
+// y = [res +] x W^T by the dense forms (ffn.hip)
+hipError_t launch_linear(const void* x, const void* W, const void* res, int64_t T, int n, int k,
+                         int dtype, void* part, void* y, hipStream_t s);
+
+// the whole layer for at most ELB_FEW_TOKENS tokens (few.hip); scale pointers null: bf16 experts.
+// h: scratch [T K, m] bf16
+hipError_t launch_moe_few(const void* x, const void* Wr, const void* Wgu, const uint8_t* gu_scale,
+                          const void* Wd, const uint8_t* d_scale, const void* res, int64_t T, int d,
+                          int N, int m, const elb_route_params& p, void* h, void* y, int* k,
+                          int* ids, float* w, int cus, hipStream_t s);
+
 // calibration: back-to-back bf16 MFMAs, blocks x 4 waves x iters x 8 of them; out [blocks * 4]
 hipError_t launch_calibrate_mfma(int blocks, int iters, float* out, hipStream_t s);
 hipError_t launch_calibrate_read(const void* buf, int64_t bytes, int blocks, uint32_t* out,

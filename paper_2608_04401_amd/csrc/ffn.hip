@@ -114,6 +114,13 @@ struct Block {
         return hipGetLastError();
     }
 
+    static hipError_t linear(const void* x, const void* W, const void* res, int64_t T_, int n, int k,
+                             void* part, void* y, hipStream_t s) {
+        ProfileScope prof("linear", s);
+        product<KC, false>(x, k, W, k, T_, n, k, PlainOut<T>{(T*)y, (const T*)res, n}, s, part);
+        return hipGetLastError();
+    }
+
     static hipError_t backward(const void* dy, const void* x, const void* Wgu, const void* Wd,
                                const float* keep, int64_t T_, int d, int m, void* dgu, void* h,
                                void* part, void* dx, void* dWgu, void* dWd, hipStream_t s) {
@@ -158,6 +165,12 @@ hipError_t launch_ffn_forward(const void* x, const void* Wgu, const void* Wd, co
     return dtype == ELB_BF16
                ? Block<Bf16, bf16_t>::forward(x, Wgu, Wd, res, T, d, m, h, part, gate_up, y, s)
                : Block<F32, float>::forward(x, Wgu, Wd, res, T, d, m, h, part, gate_up, y, s);
+}
+
+hipError_t launch_linear(const void* x, const void* W, const void* res, int64_t T, int n, int k,
+                         int dtype, void* part, void* y, hipStream_t s) {
+    return dtype == ELB_BF16 ? Block<Bf16, bf16_t>::linear(x, W, res, T, n, k, part, y, s)
+                             : Block<F32, float>::linear(x, W, res, T, n, k, part, y, s);
 }
 
 hipError_t launch_ffn_backward(const void* dy, const void* x, const void* Wgu, const void* Wd,

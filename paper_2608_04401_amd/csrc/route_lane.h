@@ -583,6 +583,19 @@ __device__ __forceinline__ void route_token_x16(float* row, int N, int K, float 
     }
 }
 
+// ---- the router's summation order ----
+constexpr int RW = 4;  // waves per router block
+
+// The order in which every router kernel accumulates a logit (so that all of them give the same
+// bits): the d / 32 k-steps of 32 are cut into RW contiguous slices, slice s holding steps
+// [s n / RW, (s + 1) n / RW); each slice is one chain of MFMAs over its steps in order,
+// starting from zero, and the logit is ((P_0 + P_1) + P_2) + P_3 in fp32.
+__device__ __forceinline__ void router_slice(int d, int s, int& first, int& count) {
+    const int n = d / 32;
+    first = s * n / RW;
+    count = (s + 1) * n / RW - first;
+}
+
 }  // namespace
 
 }  // namespace elb

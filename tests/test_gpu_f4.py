@@ -1,0 +1,211 @@
+"""GPU: 4-bit weights with group scales: quantisation, projections and the dense block."""
+import pytest
+import torch
+
+from paper_2608_04401_amd import binding as B
+
+import block_ref as R
+import dense_ref as D
+from dense_ref import shifted, within
+
+BF16, F32 = torch.bfloat16, torch.float32
+pytestmark = pytest.mark.gpu
+
+
+def gen(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+def normal(g, *shape, std=1.0, dtype=F32):
+    return (torch.randn(shape, generator=g, device="cuda") * std).to(dtype)
+
+
+def codes(g, *shape):
+    """Every code, and scales over a range in which sums stay finite."""
+    q = torch.randint(0, 256, shape[:-1] + (shape[-1] // 2,), generator=g, device="cuda",
+                      dtype=torch.uint8)
+    s = torch.randint(118, 124, shape[:-1] + (shape[-1] // 32,), generator=g, device="cuda",
+                      dtype=torch.uint8)
+    return q, s
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("rows,d", [(1, 32), (3, 96), (70, 1056), (300, 2048)])
+def test_quantise(rows, d, dtype):
+    for std in (1.0, 1e-30, 1e30):
+        x = normal(gen(rows + d), rows, d, std=std, dtype=dtype)
+        q, s = B.elb_quantize_f4(x)
+        torch.cuda.synchronize()
+        code, scale = R.quantize_f4(x)
+        assert torch.equal(s, scale) and torch.equal(q, R.pack_f4(code))
+
+
+def test_quantise_borders():
+    """Every tie, powers of two and 1.5 times them, zeros of both signs, subnormals, the largest."""
+    ties = torch.tensor([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0], dtype=torch.float64)
+    rows = []
+    for e in (-149, -130, -126, -125, -124, -20, 0, 1, 100, 123, 124, 125):
+        v = torch.cat([ties, ties * (1 - 2.0 ** -20), ties * (1 + 2.0 ** -20),
+                       torch.tensor([0.0, -0.0, 6.0, 0.5, 1.5, 3.0, 4.0])])
+        v = torch.cat([v, torch.zeros(32 - v.numel(), dtype=torch.float64)])
+        for top in (6.0, 6.0 * (1 + 2.0 ** -22), 6.0 * (1 - 2.0 ** -23), 4.0, 3.0):
+            v = v.clone()
+            v[30] = top
+            rows += [(v * 2.0 ** e).clamp(-3.4e38, 3.4e38), (-v * 2.0 ** e).clamp(-3.4e38, 3.4e38)]
+    rows += [torch.zeros(32, dtype=torch.float64), torch.full((32,), 3.4028234e38,
+                                                              dtype=torch.float64)]
+    x = torch.stack(rows).float().cuda()
+    q, s = B.elb_quantize_f4(x)
+    torch.cuda.synchronize()
+    code, scale = R.quantize_f4(x)
+    assert torch.equal(s, scale) and torch.equal(q, R.pack_f4(code))
+    bad = torch.zeros(3, 64, device="cuda")
+    bad[0, 3], bad[1, 40], bad[2, 0] = float("nan"), float("inf"), -float("inf")
+    s = B.elb_quantize_f4(bad)[1]
+    torch.cuda.synchronize()
+    assert s.tolist() == [[255, 2], [2, 255], [255, 2]]
+
+
+def test_quantise_unaligned_and_leading_dimensions():
+    x = normal(gen(3), 4, 5, 64, dtype=BF16)
+    q, s = B.elb_quantize_f4(x)
+    q2, s2 = B.elb_quantize_f4(shifted(x, 1).view(20, 64))
+    torch.cuda.synchronize()
+    assert q.shape == (4, 5, 32) and s.shape == (4, 5, 2)
+    assert torch.equal(q.view(20, 32), q2) and torch.equal(s.view(20, 2), s2)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_every_code_and_scale(dtype):
+    """x picks single weights out: each code at each scale byte from 2 to 252, exactly."""
+    n, k = 256, 32
+    q = torch.zeros((n, k // 2), dtype=torch.uint8, device="cuda")
+    q[:] = torch.tensor([0x10, 0x32, 0x54, 0x76, 0x98, 0xBA, 0xDC, 0xFE] * 2, device="cuda")
+    s = torch.arange(n, device="cuda").clamp(2, 252).to(torch.uint8)[:, None].contiguous()
+    want = R.from_f4(q, s)
+    for T in (1, 32, 100):
+        x = torch.zeros((T, k), dtype=dtype, device="cuda")
+        at = torch.arange(T, device="cuda")
+        x[at, at % k] = 1
+        y = B.elb_linear_f4(x, q, s)
+        torch.cuda.synchronize()
+        assert torch.equal(y.double(), want.t()[at % k])
+
+
+SIZES = [(32, 16), (64, 32), (96, 48), (160, 16), (256, 528), (1056, 80), (2048, 1040), (8192, 64)]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("T", [1, 2, 15, 16, 17, 31, 33, 48, 64, 65, 100, 257])
+def test_linear(T, dtype):
+    g = gen(T)
+    for k, n in SIZES:
+        W, s = codes(g, n, k)
+        x, res = normal(g, T, k, dtype=dtype), normal(g, T, n, dtype=dtype)
+        w = R.from_f4(W, s)
+        for r in (None, res):
+            y = B.elb_linear_f4(x, W, s, residual=r)
+            torch.cuda.synchronize()
+            within(y, *R.linear(x, w, r), label="T %d k %d n %d" % (T, k, n))
+
+
+@pytest.mark.parametrize("T,k,n", [(1, 64, 16400), (3, 32, 40000), (40, 256, 9008), (500, 2048, 2048),
+                                   (1, 65536, 32)])
+def test_linear_large(T, k, n):
+    g = gen(n)
+    W, s = codes(g, n, k)
+    for dtype in (BF16, F32):
+        x = normal(g, T, k, dtype=dtype)
+        y = B.elb_linear_f4(x, W, s)
+        torch.cuda.synchronize()
+        within(y, *R.linear(x, R.from_f4(W, s)))
+
+
+def test_fp32_tokens_keep_their_bits():
+    """An fp32 x in a product with one weight of 1 a row comes back bit for bit: its three parts add
+    up to it, small values and large ones."""
+    k, n = 256, 256
+    q = torch.zeros((n, k), dtype=torch.uint8, device="cuda")
+    q[torch.arange(n), torch.arange(n)] = 2  # code of 1
+    W, s = R.pack_f4(q), torch.full((n, k // 32), 127, dtype=torch.uint8, device="cuda")
+    g = gen(1)
+    for T in (1, 20, 64):
+        x = normal(g, T, k) * torch.exp2(torch.randint(-90, 120, (T, k), generator=g,
+                                                       device="cuda").float())
+        x[0, 0], x[0, 1], x[0, 2] = 3.4028234e38, 1.17549435e-38, 0.0
+        y = B.elb_linear_f4(x, W, s)
+        torch.cuda.synchronize()
+        small = x.abs() < 2.0 ** -100  # whose last part may leave the normal range
+        assert torch.equal(y[~small], x[~small])
+        assert bool(((y - x).abs()[small] <= 2.0 ** -120).all())
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("T", [1, 16, 20, 50, 64, 65, 300])
+def test_block(T, dtype):
+    g = gen(T)
+    for d, m in ((32, 32), (64, 96), (544, 160), (2048, 1024)):
+        gu, sgu = B.elb_quantize_f4(normal(g, 2 * m, d, std=d ** -0.5))
+        dn, sd = B.elb_quantize_f4(normal(g, d, m, std=m ** -0.5))
+        x, res = normal(g, T, d, dtype=dtype), normal(g, T, d, dtype=dtype)
+        wgu, wd = R.from_f4(gu, sgu, dtype), R.from_f4(dn, sd, dtype)
+        for r in (None, res):
+            y = B.elb_ffn_forward_f4(x, gu, sgu, dn, sd, residual=r)
+            torch.cuda.synchronize()
+            ref, bound, _, _ = D.ffn_forward(x, wgu, wd, r)
+            # the parts of an fp32 x: three products for one
+            within(y, ref, bound if dtype == BF16 else 3 * bound, label="d %d m %d" % (d, m))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("T", [3, 40, 130])
+def test_in_place_unaligned_and_what_lies_around(T, dtype):
+    g = gen(7)
+    d, m = 288, 192
+    gu, sgu = B.elb_quantize_f4(normal(g, 2 * m, d, std=0.06))
+    dn, sd = B.elb_quantize_f4(normal(g, d, m, std=0.07))
+    x = normal(g, T, d, dtype=dtype)
+    lin = B.elb_linear_f4(x, gu, sgu)
+    want = B.elb_ffn_forward_f4(x, gu, sgu, dn, sd, residual=x)
+    a = x.clone()
+    got = B.elb_ffn_forward_f4(a, gu, sgu, dn, sd, residual=a, out=a)
+    torch.cuda.synchronize()
+    assert got is a and torch.equal(a, want)
+    odd = [shifted(t, i + 1) for i, t in enumerate((x, gu, sgu, dn, sd))]
+    buf = torch.full((T + 2, 2 * m), 7.0, dtype=dtype, device="cuda")
+    within_lin = B.elb_linear_f4(odd[0], odd[1], odd[2], out=buf[1:-1])
+    block = B.elb_ffn_forward_f4(*odd, residual=odd[0])
+    torch.cuda.synchronize()
+    assert bool((buf[0] == 7).all() and (buf[-1] == 7).all())
+    # the dense forms sum in another order off a 16-byte boundary
+    if T <= 64:
+        assert torch.equal(within_lin, lin) and torch.equal(block, want)
+    within(within_lin, *R.linear(x, R.from_f4(gu, sgu)))
+    res = normal(g, T, 2 * m, dtype=dtype)
+    y = B.elb_linear_f4(x, gu, sgu, residual=res)
+    z = res.clone()
+    assert B.elb_linear_f4(x, gu, sgu, residual=z, out=z) is z
+    torch.cuda.synchronize()
+    assert torch.equal(z, y)
+
+
+def test_a_row_alone():
+    """A streamed row's bits do not depend on how many rows go with it, up to a tile of 16."""
+    g = gen(9)
+    W, s = codes(g, 528, 1056)
+    x = normal(g, 16, 1056, dtype=BF16)
+    y = B.elb_linear_f4(x, W, s)
+    for r in (0, 7, 15):
+        one = B.elb_linear_f4(x[r:r + 1].contiguous(), W, s)
+        torch.cuda.synchronize()
+        assert torch.equal(one[0], y[r])
+
+
+def test_no_tokens():
+    q, s = codes(gen(1), 64, 64)
+    z = lambda *sh: torch.zeros(sh, dtype=BF16, device="cuda")
+    assert B.elb_linear_f4(z(0, 64), q, s).shape == (0, 64)
+    assert B.elb_ffn_forward_f4(z(0, 64), *codes(gen(1), 128, 64), q, s).shape == (0, 64)
+    assert B.elb_quantize_f4(z(0, 64))[0].shape == (0, 32)
