@@ -1073,21 +1073,23 @@ int elb_ffn_forward_f4(const void* x, const uint8_t* W_gate_up, const uint8_t* g
 
 // sub-buffers of the few-token layer's workspace
 struct FewLayout {
-    size_t h, k, ids, w, total;
+    size_t h, k, ids, w, part, count, total;
 };
-static FewLayout few_layout(int64_t T, int m, int K) {
+static FewLayout few_layout(int64_t T, int d, int m, int K) {
     FewLayout L{};
     const size_t rows = (size_t)T * K;
     L.k = align_up(rows * m * 2);
     L.ids = L.k + align_up((size_t)T * 4);
     L.w = L.ids + align_up(rows * 4);
-    L.total = L.w + align_up(rows * 4);
+    L.part = L.w + align_up(rows * 4);
+    L.count = L.part + (size_t)(d / 64) * few_shares(d) * 4096;
+    L.total = L.count + align_up((size_t)(d / 64) * 4);
     return L;
 }
 
 size_t elb_moe_few_workspace_bytes(int64_t T, int32_t d, int32_t N, int32_t m, int32_t K) {
-    if (T < 0 || T > ELB_FEW_TOKENS || d < 1 || N < 1 || m < 1 || K < 1) return 0;
-    return few_layout(T, m, K).total;
+    if (T < 0 || T > ELB_FEW_TOKENS || d < 64 || N < 1 || m < 1 || K < 1) return 0;
+    return few_layout(T, d, m, K).total;
 }
 
 int elb_moe_forward_few(const void* x, const void* W_router, const void* W_gate_up,
@@ -1113,7 +1115,7 @@ int elb_moe_forward_few(const void* x, const void* W_router, const void* W_gate_
     if (T == 0) return ELB_OK;
     if (!x || !W_router || !W_gate_up || !W_down || !y)
         return fail(ELB_ERR_INVALID_ARG, "NULL tensor pointer");
-    const FewLayout L = few_layout(T, m, K);
+    const FewLayout L = few_layout(T, d, m, K);
     if (int rc = check_workspace(workspace, workspace_bytes, L.total)) return rc;
     const int64_t weights = (int64_t)N * m * d;  // of a projection
     const bool f4 = gate_up_scale != nullptr;
@@ -1137,7 +1139,7 @@ int elb_moe_forward_few(const void* x, const void* W_router, const void* W_gate_
     char* const ws = (char*)workspace;
     return hip_status(
         launch_moe_few(x, W_router, W_gate_up, gate_up_scale, W_down, down_scale, residual, T, d, N,
-                       m, *params, ws, y, k_out ? k_out : (int*)(ws + L.k),
+                       m, *params, ws, (float*)(ws + L.part), (int*)(ws + L.count), y, k_out ? k_out : (int*)(ws + L.k),
                        ids_out ? ids_out : (int*)(ws + L.ids),
                        w_out ? w_out : (float*)(ws + L.w), cus_per_device(), (hipStream_t)stream),
         "moe_forward_few");

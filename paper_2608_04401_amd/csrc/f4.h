@@ -1,14 +1,18 @@
-// 4-bit weights with group scales, and the ring that streams weights past a few tokens.
+// 4-bit weights with group scales, and the pieces that stream weights past a few tokens.
 //
 // A weight is e2m1 (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives: sign, two bits of exponent, one of
 // mantissa), two to a byte, the earlier along the contraction in the low half; 32 of them share a
 // scale 2^(b - 127), b a byte.  v_cvt_scalef32_pk_bf16_fp4 makes two of them, scaled, bf16 (exactly),
 // so a product costs half an instruction a weight before its MFMA.
 //
-// Operands lie in registers as they come from memory: a lane loads 16 bytes of weight row (lane & 15),
-// its quarter (lane >> 4) of a step of 64 bytes.  That is 8 bf16 or 32 4-bit values, so a step of the
-// contraction is one v_mfma_f32_16x16x32_bf16 or four; in the i-th of the four, quarter c multiplies
-// values 32 c + 8 i .. + 7 of the step, and the tokens' operand is loaded to match.
+// Weights are streamed in units of 128 bytes of 16 NF rows (64 bf16 or 256 4-bit values of the
+// contraction), copied in whole lines into a wave's own LDS and read from there as MFMA operands.
+// (Operands loaded straight into registers, 16 rows of 64 bytes an instruction, reached a third of that
+// rate: 8 waves of a block read a router of 64 rows of 4 KB in 9 us.)  In LDS a row's eight 16-byte
+// chunks are swizzled (kc_swz).  Lane l of a fragment has row l % 16 and quarter c = l / 16 of each
+// half of the unit: 8 bf16, one v_mfma_f32_16x16x32_bf16; or 32 4-bit values, which are turned between
+// the quarters (a 4 x 4 transposition of words in four swaps) into the operands of four, the i-th
+// of them group i of the half, so that the tokens' operand is contiguous in the same way.
 #pragma once
 
 #include "dense.h"
@@ -18,6 +22,8 @@ namespace elb {
 namespace {
 
 typedef __bf16 bf16x2v_t __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x2_byte_t __attribute__((ext_vector_type(2), aligned(1)));
+typedef uint32_t u32_byte_t __attribute__((aligned(1)));
 
 // eight 4-bit weights times a power of two
 __device__ __forceinline__ bf16x8_t f4_to_bf16(uint32_t w, float scale) {
@@ -31,58 +37,136 @@ __device__ __forceinline__ bf16x8_t f4_to_bf16(uint32_t w, float scale) {
 }
 __device__ __forceinline__ float f4_scale(uint32_t b) { return __uint_as_float(b << 23); }
 
-// ---- weights of a step: 16 bytes a lane of each fragment of 16 rows ----
+// words a and b, each of four quarters of a wave: (a0 a1 b0 b1), (a2 a3 b2 b3)
+__device__ __forceinline__ void swap_halves(uint32_t& a, uint32_t& b) {
+    const auto r = __builtin_amdgcn_permlane32_swap(a, b, false, false);
+    a = r[0];
+    b = r[1];
+}
+// (a0 b0 a2 b2), (a1 b1 a3 b3)
+__device__ __forceinline__ void swap_quarters(uint32_t& a, uint32_t& b) {
+    const auto r = __builtin_amdgcn_permlane16_swap(a, b, false, false);
+    a = r[0];
+    b = r[1];
+}
+
+// this wave's lane's 32-bit LDS address of a pointer into LDS, in a scalar register
+__device__ __forceinline__ uint32_t lds_address(const char* p) {
+    return __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_void_t*)p);
+}
+
+// ---- weight types: KU, the contraction of a unit; J, MFMAs of a half of it ----
 struct WBf16 {
-    static constexpr int KS = 32, J = 1;  // contraction of a step, MFMAs that it takes
-    struct Frag {
+    static constexpr int KU = 64, J = 1, SCALES = 0;
+    struct Half {  // a fragment's operands of half a unit
         u32x4_t v;
+        __device__ __forceinline__ bf16x8_t get(int) const { return __builtin_bit_cast(bf16x8_t, v); }
     };
-    const bf16_t* w;
-    int64_t ld;  // elements
-    __device__ __forceinline__ void load(Frag& f, int64_t row, int k) const {
-        f.v = *reinterpret_cast<const u32x4_any_t*>(w + row * ld + k);
-    }
-    static __device__ __forceinline__ bf16x8_t get(const Frag& f, int) {
-        return __builtin_bit_cast(bf16x8_t, f.v);
+    static __device__ __forceinline__ int64_t row_bytes(int64_t k) { return 2 * k; }
+    // half h of the unit in LDS at p, row l16 of fragment f
+    static __device__ __forceinline__ void read(Half& o, const char* p, int, int f, int h, int l16,
+                                                int c) {
+        o.v = *reinterpret_cast<const u32x4_t*>(p + (16 * f + l16) * 128 +
+                                                kc_swz(l16, 4 * h + c) * 16);
     }
 };
 struct WF4 {
-    static constexpr int KS = 128, J = 4;
-    struct Frag {
-        u32x4_t v;
-        uint32_t s;
+    static constexpr int KU = 256, J = 4, SCALES = 8;  // scale bytes of a row
+    struct Half {
+        uint32_t v[4], s;
+        // (the scales of both halves lie in a row's eight bytes: s holds those of this one)
+        __device__ __forceinline__ bf16x8_t get(int i) const {
+            return f4_to_bf16(v[i], f4_scale(s >> (8 * i) & 255u));
+        }
     };
-    const uint8_t *w, *scale;
-    int64_t ld;  // values
-    __device__ __forceinline__ void load(Frag& f, int64_t row, int k) const {
-        const int64_t o = row * ld + k;
-        f.v = *reinterpret_cast<const u32x4_byte_t*>(w + (o >> 1));
-        f.s = scale[o >> 5];
-    }
-    static __device__ __forceinline__ bf16x8_t get(const Frag& f, int i) {
-        return f4_to_bf16(f.v[i], f4_scale(f.s));
+    static __device__ __forceinline__ int64_t row_bytes(int64_t k) { return k / 2; }
+    // rows: of the unit, whose scales lie behind them
+    static __device__ __forceinline__ void read(Half& o, const char* p, int rows, int f, int h,
+                                                int l16, int c) {
+        const int r = 16 * f + l16;
+        const u32x4_t v = *reinterpret_cast<const u32x4_t*>(p + r * 128 +
+                                                            kc_swz(l16, 4 * h + c) * 16);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o.v[i] = v[i];
+        o.s = *reinterpret_cast<const uint32_t*>(p + rows * 128 + r * 8 + 4 * h);
+        swap_halves(o.v[0], o.v[2]);
+        swap_halves(o.v[1], o.v[3]);
+        swap_quarters(o.v[0], o.v[1]);
+        swap_quarters(o.v[2], o.v[3]);
     }
 };
 
-// Steps 0 .. n - 1 through R register slots: R - 1 steps are in flight while one is multiplied.
-// load(step, slot) for steps in order (none past the last), mma(step, slot).
-template <int R, class Slot, class Load, class Mma>
-__device__ __forceinline__ void ring(int n, Load&& load, Mma&& mma) {
-    Slot s[R];
+// One wave's copies of a unit of weights: 16 NF rows (PAIR: the second half of them `apart` rows of
+// the tensor further on) of 128 bytes, and the rows' eight scale bytes behind them.  DMA: tensors on
+// 16-byte boundaries, and scale rows on 4-byte ones; otherwise ordinary loads.
+template <class W, int NF, bool PAIR, bool DMA>
+struct Stream {
+    static constexpr int ROWS = 16 * NF;
+    static constexpr int BYTES = ROWS * 128 + (W::SCALES ? (ROWS + 31) / 32 * 256 : 0);
+    typedef Copier<KC, ROWS, 1, 1, PAIR, DMA> C;
+    static constexpr int N = C::N + (W::SCALES ? (ROWS + 31) / 32 : 0);  // copy instructions
+    C copy;
+    const uint8_t* scale[(ROWS + 31) / 32];  // of the lane's rows
+    int groups;                              // of a row
+
+    // row0: the tile's first row; rows: valid ones from there on (of each half with PAIR)
+    __device__ __forceinline__ void init(const void* w, const uint8_t* s, int64_t row0, int rows,
+                                         int64_t apart, int64_t k, int lane) {
+        const int64_t ld = W::row_bytes(k);
+        copy.init((const char*)w + row0 * ld, (const char*)w + (row0 + apart) * ld, ld, rows, ld,
+                  lane, 0);
+        if (!W::SCALES) return;
+        groups = (int)(k / 32);
+        constexpr int HR = PAIR ? ROWS / 2 : ROWS;
 #pragma unroll
-    for (int p = 0; p < R - 1; ++p)
-        if (p < n) load(p, s[p]);
-    for (int j = 0; j < n; j += R) {
-#pragma unroll
-        for (int p = 0; p < R; ++p) {
-            if (j + p >= n) break;
-            if (j + p + R - 1 < n) load(j + p + R - 1, s[(p + R - 1) % R]);
-            // this step's loads before its products, which wait for an earlier step's only
-            __builtin_amdgcn_sched_barrier(0);
-            mma(j + p, s[p]);
-            __builtin_amdgcn_sched_barrier(0);
+        for (int i = 0; i < (ROWS + 31) / 32; ++i) {
+            int r = 32 * i + (lane >> 1);  // two words a row
+            r = r < ROWS ? r : ROWS - 1;
+            int64_t row = row0;
+            if (PAIR && r >= HR) {
+                row += apart;
+                r -= HR;
+            }
+            scale[i] = s + (row + (r < rows ? r : rows - 1)) * groups;
         }
     }
+    // unit u to LDS at lds (ldsp: the same as a pointer); past uend zeros
+    __device__ __forceinline__ void issue(int u, int uend, uint32_t lds, char* ldsp, int lane) const {
+        copy.issue(u, uend, lds, ldsp, lane, 0);
+        if constexpr (W::SCALES != 0) {
+            const int g = 8 * u + 4 * (lane & 1);
+#pragma unroll
+            for (int i = 0; i < (ROWS + 31) / 32; ++i) {
+                if constexpr (DMA) {
+                    // groups past the row's last: its last four, which no product takes
+                    const uint8_t* const p = scale[i] + (g < groups ? g : groups - 4);
+                    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, off"
+                                 :: "s"(lds + ROWS * 128 + i * 256), "v"(p) : "memory", "m0");
+                } else if (32 * i + (lane >> 1) < ROWS) {
+                    uint32_t v = 0;
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        if (g + q < groups) v |= (uint32_t)scale[i][g + q] << (8 * q);
+                    *reinterpret_cast<uint32_t*>(ldsp + ROWS * 128 + i * 256 + lane * 4) = v;
+                }
+            }
+        }
+    }
+    // the same rows of another matrix, w_bytes and s_bytes further on
+    __device__ __forceinline__ Stream moved(int64_t w_bytes, int64_t s_bytes) const {
+        Stream o = *this;
+#pragma unroll
+        for (int b = 0; b < C::NB; ++b) o.copy.base[b] += w_bytes;
+        if (W::SCALES) {
+#pragma unroll
+            for (int i = 0; i < (ROWS + 31) / 32; ++i) o.scale[i] += s_bytes;
+        }
+        return o;
+    }
+};
+// whether weights and scales of rows of k values may be copied by DMA
+inline bool f4_copies(const void* w, const void* s, int64_t k) {
+    return (uintptr_t)w % 16 == 0 && (uintptr_t)s % 4 == 0 && k % 128 == 0;
 }
 
 }  // namespace

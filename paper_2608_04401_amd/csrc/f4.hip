@@ -82,10 +82,12 @@ template <>
 struct Tok<bf16_t> {
     static constexpr int P = 1;
     u32x4_t v;
-    __device__ __forceinline__ void load(const bf16_t* p) {
-        v = *reinterpret_cast<const u32x4_any_t*>(p);
+    // values 128 h + 32 i + 8 c .. + 7 of row r of a unit of 256, in LDS as four k-tiles of TM rows
+    template <int TM>
+    __device__ __forceinline__ void read(const char* p, int r, int h, int i, int c) {
+        v = *reinterpret_cast<const u32x4_t*>(p + (2 * h + i / 2) * TM * 128 + r * 128 +
+                                              kc_swz(r, i % 2 * 4 + c) * 16);
     }
-    __device__ __forceinline__ void zero() { v = u32x4_t{0, 0, 0, 0}; }
     __device__ __forceinline__ void parts(bf16x8_t (&o)[1]) const {
         o[0] = __builtin_bit_cast(bf16x8_t, v);
     }
@@ -94,11 +96,12 @@ template <>
 struct Tok<float> {
     static constexpr int P = 3;
     f32x4_t a, b;
-    __device__ __forceinline__ void load(const float* p) {
-        a = *reinterpret_cast<const f32x4_any_t*>(p);
-        b = *reinterpret_cast<const f32x4_any_t*>(p + 4);
+    template <int TM>
+    __device__ __forceinline__ void read(const char* p, int r, int h, int i, int c) {
+        const char* const q = p + (4 * h + i) * TM * 128 + r * 128;
+        a = *reinterpret_cast<const f32x4_t*>(q + kc_swz(r, 2 * c) * 16);
+        b = *reinterpret_cast<const f32x4_t*>(q + kc_swz(r, 2 * c + 1) * 16);
     }
-    __device__ __forceinline__ void zero() { a = b = f32x4_t{0, 0, 0, 0}; }
     // the leading 8 bits, the next 8 and the rest: differences of a float and its leading bits are
     // exact.  (An infinity leaves NaN in the second part, and so in the sums.)
     __device__ __forceinline__ void parts(bf16x8_t (&o)[3]) const {
@@ -137,101 +140,109 @@ struct StreamIn {
 };
 
 // ------------------------------------------------------------------------------------------
-// A few tokens: 16 MT of them against NF fragments of 16 weight rows a block (PAIR: half of them gate
-// rows and the other half the matching up rows), the contraction in eight waves, whose partial tiles
-// are added in LDS in order.  Bound by the weights' stream, or by the latency of its start.
+// A few tokens: TM of them against NF fragments of 16 weight rows a block (PAIR: half of them gate rows
+// and the other half the matching up rows).  Each of NW waves has a share of the contraction and walks
+// it alone: a unit's weights and tokens are copied into the wave's LDS, read into registers, and the
+// next unit's copies run while this one is multiplied; no barrier until the waves' partial tiles are
+// added, in order.  Bound by the weights' stream, or by the latency of its start.
 // ------------------------------------------------------------------------------------------
-template <class X, int NF, int MT, int R, bool PAIR>
-__global__ __launch_bounds__(512) void stream_f4(StreamIn<X> in) {
-    constexpr int NW = 8, OF = PAIR ? NF / 2 : NF;  // output fragments
-    __shared__ f32x4_t part[NW][MT][NF][64];
+template <class X, int TM, int NF, int NW, bool PAIR, bool DMA>
+__global__ __launch_bounds__(64 * NW) void stream_f4(StreamIn<X> in) {
+    constexpr int OF = PAIR ? NF / 2 : NF;  // output fragments
+    constexpr int MT = (TM + 15) / 16, SUB = 256 * sizeof(X) / 128;
+    typedef Stream<WF4, NF, PAIR, DMA> B;
+    typedef Copier<KC, TM, sizeof(X), 1, false, DMA> A;
+    constexpr int AB = SUB * TM * 128, SLOT = (AB + B::BYTES + 255) / 256 * 256;
+    static_assert(MT * NF * 1024 <= SLOT && NW * SLOT <= 160 * 1024, "");
+    __shared__ __attribute__((aligned(1024))) char sm[NW * SLOT];
     const int lane = threadIdx.x & 63, l16 = lane & 15, hq = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int c0 = (int)blockIdx.x * 16 * OF;
-    const int64_t t0 = (int64_t)blockIdx.y * 16 * MT;
-    const int steps = (in.k + WF4::KS - 1) / WF4::KS;
-    const int s0 = steps * wave / NW, s1 = steps * (wave + 1) / NW;
-    const WF4 W{in.w, in.scale, in.k};
-    // columns are multiples of 16: a fragment is a tensor's or wholly past it, where the last is read
-    int64_t wrow[NF];
+    const int64_t t0 = (int64_t)blockIdx.y * TM;
+    const int units = (in.k + 255) / 256;
+    const int u0 = units * wave / NW, u1 = units * (wave + 1) / NW;
+    char* const slot = sm + wave * SLOT;
+    const uint32_t lds = lds_address(slot);
+    A a;
+    a.init(in.x + t0 * in.k, nullptr, (int64_t)in.k * sizeof(X),
+           in.T - t0 < TM ? (int)(in.T - t0) : TM, in.k, lane, 0);
+    B b;
+    b.init(in.w, in.scale, c0, in.cols - c0, in.cols, in.k, lane);
+    auto issue = [&](int u) {
 #pragma unroll
-    for (int f = 0; f < NF; ++f) {
-        int c = c0 + 16 * (f % OF);
-        c = c < in.cols ? c : in.cols - 16;
-        wrow[f] = (PAIR && f >= OF ? (int64_t)in.cols : 0) + c + l16;
-    }
-    const X* xp[MT];
-#pragma unroll
-    for (int t = 0; t < MT; ++t) {
-        const int64_t r = t0 + 16 * t + l16;
-        xp[t] = in.x + (r < in.T ? r : in.T - 1) * in.k;
-    }
-    struct Slot {
-        WF4::Frag w[NF];
-        Tok<X> x[MT][4];
+        for (int q = 0; q < SUB; ++q)
+            a.issue(SUB * u + q, SUB * u1, lds + q * TM * 128, slot + q * TM * 128, lane, 0);
+        b.issue(u, u1, lds + AB, slot + AB, lane);
     };
     f32x4_t acc[MT][NF];
 #pragma unroll
     for (int t = 0; t < MT; ++t)
 #pragma unroll
         for (int f = 0; f < NF; ++f) acc[t][f] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    ring<R, Slot>(
-        s1 - s0,
-        [&](int j, Slot& s) {
-            // quarters past the contraction: the row's last weights, and zeros for the tokens
-            int k = (s0 + j) * WF4::KS + 32 * hq;
-            const bool in_k = k < in.k;
-            k = in_k ? k : in.k - 32;
+    if (u0 < u1) issue(u0);
+    for (int u = u0; u < u1; ++u) {
+        ELB_WAIT_VMCNT(0);
+        asm volatile("" ::: "memory");  // the copies write LDS behind the compiler's back
+        WF4::Half w[NF][2];
+        Tok<X> x[MT][2][4];
 #pragma unroll
-            for (int f = 0; f < NF; ++f) W.load(s.w[f], wrow[f], k);
+        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+            for (int f = 0; f < NF; ++f)
+                WF4::read(w[f][h], slot + AB, 16 * NF, f, h, l16, hq);
 #pragma unroll
             for (int t = 0; t < MT; ++t)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) s.x[t][i].load(xp[t] + k + 8 * i);
-        },
-        [&](int j, Slot& s) {
-            if ((s0 + j + 1) * WF4::KS > in.k && (s0 + j) * WF4::KS + 32 * hq >= in.k) {
+                for (int i = 0; i < 4; ++i)
+                    x[t][h][i].template read<TM>(slot, TM < 16 ? l16 % TM : 16 * t + l16, h, i, hq);
+        }
+        // every read of the unit has returned before the next one's copies overwrite it
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (u + 1 < u1) issue(u + 1);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int t = 0; t < MT; ++t)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) s.x[t][i].zero();
-            }
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                bf16x8_t a[NF];
+                if (u * 256 + 128 * h + 32 * i >= in.k) break;
+                bf16x8_t wf[NF];
 #pragma unroll
-                for (int f = 0; f < NF; ++f) a[f] = WF4::get(s.w[f], i);
+                for (int f = 0; f < NF; ++f) wf[f] = w[f][h].get(i);
 #pragma unroll
                 for (int t = 0; t < MT; ++t) {
-                    bf16x8_t b[Tok<X>::P];
-                    s.x[t][i].parts(b);
+                    bf16x8_t xf[Tok<X>::P];
+                    x[t][h][i].parts(xf);
 #pragma unroll
                     for (int p = Tok<X>::P - 1; p >= 0; --p)
 #pragma unroll
                         for (int f = 0; f < NF; ++f)
-                            acc[t][f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[f], b[p],
+                            acc[t][f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf[f], xf[p],
                                                                                 acc[t][f], 0, 0, 0);
                 }
             }
-        });
+    }
+    // partial tiles, each in its wave's own LDS
+    auto part = [&](int w, int t, int f, int l) {
+        return reinterpret_cast<f32x4_t*>(sm + w * SLOT) + (t * NF + f) * 64 + l;
+    };
 #pragma unroll
     for (int t = 0; t < MT; ++t)
 #pragma unroll
-        for (int f = 0; f < NF; ++f) part[wave][t][f][lane] = acc[t][f];
+        for (int f = 0; f < NF; ++f) *part(wave, t, f, lane) = acc[t][f];
     __syncthreads();
     // a lane of a tile's fragment has columns 16 f + 4 (lane / 16) .. + 3 of token 16 t + lane % 16
     for (int i = threadIdx.x; i < MT * OF * 64; i += NW * 64) {
         const int l = i & 63, f = i / 64 % OF, t = i / (64 * OF);
         auto sum = [&](int ff) {
-            f32x4_t v = part[0][t][ff][l];
+            f32x4_t v = *part(0, t, ff, l);
 #pragma unroll
-            for (int w = 1; w < NW; ++w) v += part[w][t][ff][l];
+            for (int w = 1; w < NW; ++w) v += *part(w, t, ff, l);
             return v;
         };
         f32x4_t v = sum(f);
         const int64_t r = t0 + 16 * t + (l & 15);
         const int c = c0 + 16 * f + 4 * (l >> 4);
-        if (r >= in.T || c >= in.cols) continue;
+        if (r >= in.T || 16 * t + (l & 15) >= TM || c >= in.cols) continue;
         const int64_t o = r * in.cols + c;
         if constexpr (PAIR) {
             const f32x4_t u = sum(f + OF);
@@ -255,23 +266,32 @@ __global__ __launch_bounds__(512) void stream_f4(StreamIn<X> in) {
     }
 }
 
-template <class X, int NF, int MT, int R, bool PAIR>
+template <class X, int TM, int NF, int NW, bool PAIR>
 void run_stream(const StreamIn<X>& in, hipStream_t s) {
     constexpr int OC = 16 * (PAIR ? NF / 2 : NF);
-    const dim3 grid((unsigned)((in.cols + OC - 1) / OC), (unsigned)((in.T + 16 * MT - 1) / (16 * MT)));
-    ELB_LAUNCH((stream_f4<X, NF, MT, R, PAIR>), grid, dim3(512), 0, s, in);
+    const dim3 grid((unsigned)((in.cols + OC - 1) / OC), (unsigned)((in.T + TM - 1) / TM));
+    if (aligned16(in.x, in.w) && f4_copies(in.w, in.scale, in.k))
+        ELB_LAUNCH((stream_f4<X, TM, NF, NW, PAIR, true>), grid, dim3(64 * NW), 0, s, in);
+    else
+        ELB_LAUNCH((stream_f4<X, TM, NF, NW, PAIR, false>), grid, dim3(64 * NW), 0, s, in);
 }
 
 template <class X, bool PAIR>
 void stream(const StreamIn<X>& in, hipStream_t s) {
     constexpr bool F = sizeof(X) == 4;
-    if (in.T <= 16) {
-        if (!PAIR && in.cols <= 16 * 512) return run_stream<X, PAIR ? 2 : 1, 1, F ? 3 : 4, PAIR>(in, s);
-        if (in.cols <= 16 * (PAIR ? 512 : 1024)) return run_stream<X, 2, 1, F ? 3 : 4, PAIR>(in, s);
-        return run_stream<X, 4, 1, F ? 3 : 4, PAIR>(in, s);
+    const int rows = PAIR ? 2 * in.cols : in.cols;
+    if (in.T <= 8) {
+        if (!PAIR && rows <= 16 * 256) return run_stream<X, 8, PAIR ? 2 : 1, F ? 8 : 16, PAIR>(in, s);
+        if (rows <= 32 * 256) return run_stream<X, 8, 2, 8, PAIR>(in, s);
+        return run_stream<X, 8, 4, 8, PAIR>(in, s);
     }
-    if (in.T <= 32) return run_stream<X, 2, 2, F ? 2 : 3, PAIR>(in, s);
-    return run_stream<X, 2, F ? 2 : 4, F ? 2 : 2, PAIR>(in, s);
+    if (in.T <= 16) {
+        if (!PAIR && rows <= 16 * 256) return run_stream<X, 16, PAIR ? 2 : 1, F ? 4 : 8, PAIR>(in, s);
+        if (rows <= 32 * 256) return run_stream<X, 16, 2, F ? 4 : 8, PAIR>(in, s);
+        return run_stream<X, 16, 4, F ? 4 : 8, PAIR>(in, s);
+    }
+    if (F || in.T <= 32) return run_stream<X, 32, 2, 4, PAIR>(in, s);
+    return run_stream<X, F ? 32 : 64, 2, 4, PAIR>(in, s);
 }
 
 template <class T>

@@ -15,11 +15,13 @@ namespace elb {
 
 namespace {
 
-constexpr int kUpWaves = 8, kDownWaves = 16;
+constexpr int kUpWaves = 8, kDownWaves = 8;
 
-// The experts that some token has selected, and the slot t K + j that token t has of each (-1: none)
+// The experts that some token has selected (list[0 .. used)), and of each its tokens: a bit for each,
+// the slot t K + j of each (where its bit is set), and their slots in order.
 struct Slots {
-    int16_t slot[64][16];
+    uint32_t tokens[64];
+    int16_t slot[64][16], row[64][16];
     int list[64];
     int used;
 };
@@ -27,38 +29,27 @@ struct Slots {
 // k, ids: the routing of T tokens (at most 16 x 16 slots); by the whole block, which it synchronises
 __device__ __forceinline__ void find_slots(Slots& s, const int* k, const int* ids, int T, int K,
                                            int N) {
-    for (int i = threadIdx.x; i < 64 * 8; i += blockDim.x)
-        reinterpret_cast<uint32_t*>(s.slot)[i] = 0xffffffffu;
+    const int q = threadIdx.x;
+    int e = -1;
+    const int t = q / K;
+    if (q < T * K) {
+        e = ids[q];
+        if (q - t * K >= k[t] || e >= N) e = -1;
+    }
+    if (q < 64) s.tokens[q] = 0;
     __syncthreads();
-    if ((int)threadIdx.x < T * K) {
-        const int t = threadIdx.x / K, j = threadIdx.x - t * K;
-        const int e = ids[threadIdx.x];
-        if (j < k[t] && e >= 0 && e < N) s.slot[e][t] = (int16_t)threadIdx.x;
+    if (e >= 0) atomicOr(&s.tokens[e], 1u << t);
+    __syncthreads();
+    if (e >= 0) {
+        s.slot[e][t] = (int16_t)q;
+        s.row[e][__popc(s.tokens[e] & ((1u << t) - 1))] = (int16_t)q;
+    }
+    if (q < 64) {
+        const uint64_t used = __ballot(s.tokens[q] != 0);
+        if (s.tokens[q] != 0) s.list[__popcll(used & ((1ull << q) - 1))] = q;
+        if (q == 0) s.used = __popcll(used);
     }
     __syncthreads();
-    if (threadIdx.x < 64) {
-        const uint32_t* const row = reinterpret_cast<const uint32_t*>(s.slot[threadIdx.x]);
-        uint32_t all = 0xffffffffu;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) all &= row[i];
-        const uint64_t used = __ballot(all != 0xffffffffu);
-        if (all != 0xffffffffu)
-            s.list[__popcll(used & ((1ull << threadIdx.x) - 1))] = threadIdx.x;
-        if (threadIdx.x == 0) s.used = __popcll(used);
-    }
-    __syncthreads();
-}
-
-template <class W>
-__device__ __forceinline__ W expert(const void* w, const uint8_t* scale, int64_t at, int64_t ld);
-template <>
-__device__ __forceinline__ WBf16 expert<WBf16>(const void* w, const uint8_t*, int64_t at, int64_t ld) {
-    return {(const bf16_t*)w + at, ld};
-}
-template <>
-__device__ __forceinline__ WF4 expert<WF4>(const void* w, const uint8_t* scale, int64_t at,
-                                           int64_t ld) {
-    return {(const uint8_t*)w + at / 2, scale + at / 32, ld};
 }
 
 struct FewIn {
@@ -72,60 +63,102 @@ struct FewIn {
     bf16_t* y;
     int *k, *ids;
     float* w;
+    float* part;  // partial sums of launch 2 [column tiles, shares, 16, 64], and
+    int* count;   // how many of a column tile's are written (zeroed by launch 1)
+    int shares;
 };
 
-// NG: groups of 16 experts
-template <class W, int NG, int KMAX, int R>
+// A wave's tokens of 16 bytes a lane: row l16, values 8 hq .. of a run of 32
+__device__ __forceinline__ bf16x8_t as_frag(u32x4_t v) { return __builtin_bit_cast(bf16x8_t, v); }
+
+// ------------------------------------------------------------------------------------------
+// Launch 1.  NG: groups of 16 experts; DMA: x, W_router and the weights on 16-byte boundaries.
+// ------------------------------------------------------------------------------------------
+template <class W, int KMAX, bool DMA>
 __global__ __launch_bounds__(64 * kUpWaves) void few_up(FewIn in, XTable xt) {
+    typedef Stream<W, 4, true, DMA> B;
+    // a wave's LDS: a unit of weights, then its partial tiles; before that two units of the router
+    constexpr int PART = (B::BYTES + 255) / 256 * 256, SLOT = PART + 4096;
+    constexpr int RUNIT = 32 * 128 + 16 * 128;  // 32 rows of W_router, 16 of x
+    static_assert(2 * RUNIT <= SLOT, "");
+    __shared__ __attribute__((aligned(1024))) char sm[kUpWaves * SLOT];
     __shared__ float logits[RW][16 * 65];
-    __shared__ f32x4_t part[kUpWaves][4][64];
     __shared__ Slots slots;
     __shared__ int sk[16], sids[16 * kLaneMaxK];
     __shared__ float sw[16 * kLaneMaxK];
     const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, hq = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int T = in.T, d = in.d, N = in.N, m = in.m, K = in.K;
-    const bf16_t* const xr = in.x + (int64_t)(l16 < T ? l16 : T - 1) * d;
+    char* const slot = sm + wave * SLOT;
+    const uint32_t lds = lds_address(slot);
 
-    // ---- router: wave w has slice w % 4 of the contraction and every other group of experts ----
+    if (blockIdx.x == 0)
+        for (int i = tid; i < d / 64; i += 64 * kUpWaves) in.count[i] = 0;
+
+    // the tokens' operands of this wave's share of the contraction, where it is at most 256 long
+    const int units = (d + W::KU - 1) / W::KU;
+    const int u0 = units * wave / kUpWaves, u1 = units * (wave + 1) / kUpWaves;
+    const bool held = (units + kUpWaves - 1) / kUpWaves * W::KU <= 256;
+    const bf16_t* const xr = in.x + (int64_t)(l16 < T ? l16 : T - 1) * d + 8 * hq;
+    u32x4_t x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int k = u0 * W::KU + 32 * i;
+        x[i] = *reinterpret_cast<const u32x4_any_t*>(xr + (k < d ? k : d - 32));
+    }
+
+    // ---- router: wave w has slice w % 4 of the contraction and experts 32 (w / 4) .. + 31 ----
     {
-        constexpr int G = (NG + 1) / 2;
-        struct Slot {
-            u32x4_t a, b[G];
-        };
+        Copier<KC, 32, 2, 1, false, DMA> cw;
+        Copier<KC, 16, 2, 1, false, DMA> cx;
         int first, count;
         router_slice(d, wave & 3, first, count);
-        const bf16_t* wr[G];
+        const int e0 = 32 * (wave >> 2);
+        const int n = (count + 1) / 2;  // units of two steps of 32
+        cw.init(in.router + (int64_t)(e0 < N ? e0 : 0) * d + first * 32, nullptr, 2 * (int64_t)d,
+                e0 < N ? N - e0 : 0, count * 32, lane, 0);
+        cx.init(in.x + first * 32, nullptr, 2 * (int64_t)d, T, count * 32, lane, 0);
+        auto issue = [&](int u) {
+            const int at = (u & 1) * RUNIT;
+            cw.issue(u, n, lds + at, slot + at, lane, 0);
+            cx.issue(u, n, lds + at + 4096, slot + at + 4096, lane, 0);
+        };
+        f32x4_t acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+        issue(0);
+        issue(1);
+        for (int u = 0; u < n; ++u) {
+            ELB_WAIT_VMCNT(6);  // the unit after this one
+            asm volatile("" ::: "memory");
+            const char* const p = slot + (u & 1) * RUNIT;
+            u32x4_t a[2], b[2][2];
 #pragma unroll
-        for (int g = 0; g < G; ++g) {
-            const int n = 16 * (2 * g + (wave >> 2)) + l16;
-            wr[g] = in.router + (int64_t)(n < N ? n : N - 1) * d;
+            for (int s = 0; s < 2; ++s) {
+                a[s] = *reinterpret_cast<const u32x4_t*>(p + 4096 + l16 * 128 +
+                                                         kc_swz(l16, 4 * s + hq) * 16);
+#pragma unroll
+                for (int g = 0; g < 2; ++g)
+                    b[s][g] = *reinterpret_cast<const u32x4_t*>(p + (16 * g + l16) * 128 +
+                                                                kc_swz(l16, 4 * s + hq) * 16);
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the unit is free again
+            issue(u + 2);  // past the last one: zeros
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                if (2 * u + s >= count) break;
+#pragma unroll
+                for (int g = 0; g < 2; ++g)
+                    acc[g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_frag(a[s]), as_frag(b[s][g]),
+                                                                     acc[g], 0, 0, 0);
+            }
         }
-        f32x4_t acc[G];
 #pragma unroll
-        for (int g = 0; g < G; ++g) acc[g] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-        ring<8, Slot>(
-            count,
-            [&](int j, Slot& s) {
-                const int c = (first + j) * 32 + hq * 8;
-                s.a = *reinterpret_cast<const u32x4_any_t*>(xr + c);
-#pragma unroll
-                for (int g = 0; g < G; ++g)
-                    s.b[g] = *reinterpret_cast<const u32x4_any_t*>(wr[g] + c);
-            },
-            [&](int, Slot& s) {
-#pragma unroll
-                for (int g = 0; g < G; ++g)
-                    acc[g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                        __builtin_bit_cast(bf16x8_t, s.a), __builtin_bit_cast(bf16x8_t, s.b[g]),
-                        acc[g], 0, 0, 0);
-            });
-#pragma unroll
-        for (int g = 0; g < G; ++g)
+        for (int g = 0; g < 2; ++g)
 #pragma unroll
             for (int r = 0; r < 4; ++r)
-                logits[wave & 3][(4 * hq + r) * 65 + 16 * (2 * g + (wave >> 2)) + l16] = acc[g][r];
+                logits[wave & 3][(4 * hq + r) * 65 + e0 + 16 * g + l16] = acc[g][r];
     }
+    ELB_WAIT_VMCNT(0);  // the last copies, before their LDS is used again; and x
     __syncthreads();
     if (tid < 256) {  // whole waves: 16 lanes a token
         const int t = tid >> 4, sl = tid & 15;
@@ -160,157 +193,280 @@ __global__ __launch_bounds__(64 * kUpWaves) void few_up(FewIn in, XTable xt) {
 
     // ---- tasks: 32 columns of h of an expert, its 32 gate rows and the matching up rows ----
     const int per_e = m / 32, tasks = slots.used * per_e;
-    const int steps = (d + W::KS - 1) / W::KS;
-    const int s0 = steps * wave / kUpWaves, s1 = steps * (wave + 1) / kUpWaves;
-    for (int task = blockIdx.x; task < tasks; task += gridDim.x) {
-        const int u = task / per_e, c = task - u * per_e;
+    const int64_t w_bytes = W::row_bytes((int64_t)2 * m * d);  // of an expert
+    int task = blockIdx.x;
+    B b;
+    auto begin = [&](int t) {
+        const int u = t / per_e;
         const int e = __builtin_amdgcn_readfirstlane(slots.list[u]);
-        const W w = expert<W>(in.gate_up, in.gu_scale, (int64_t)e * 2 * m * d, d);
-        struct Slot {
-            typename W::Frag w[4];
-            u32x4_t x[W::J];
-        };
+        b.init((const char*)in.gate_up + e * w_bytes,
+               W::SCALES ? in.gu_scale + (int64_t)e * 2 * m * (d / 32) : nullptr,
+               32 * (t - u * per_e), 32, m, d, lane);
+        if (u0 < u1) b.issue(u0, u1, lds, slot, lane);
+        return e;
+    };
+    int e = task < tasks ? begin(task) : 0;
+    while (task < tasks) {
         f32x4_t acc[4];
 #pragma unroll
         for (int f = 0; f < 4; ++f) acc[f] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-        ring<R, Slot>(
-            s1 - s0,
-            [&](int j, Slot& s) {
-                int k = (s0 + j) * W::KS + W::KS / 4 * hq;
-                k = k < d ? k : d - W::KS / 4;
+        const int next = task + gridDim.x;
+        int next_e = 0;
+        for (int u = u0; u < u1; ++u) {
+            if (!held) {
 #pragma unroll
-                for (int f = 0; f < 4; ++f)
-                    w.load(s.w[f], (f < 2 ? 0 : m) + 32 * c + 16 * (f & 1) + l16, k);
-#pragma unroll
-                for (int i = 0; i < W::J; ++i)
-                    s.x[i] = *reinterpret_cast<const u32x4_any_t*>(xr + k + 8 * i);
-            },
-            [&](int j, Slot& s) {
-                const bool past = (s0 + j) * W::KS + W::KS / 4 * hq >= d;
-#pragma unroll
-                for (int i = 0; i < W::J; ++i) {
-                    if (past) s.x[i] = u32x4_t{0, 0, 0, 0};
-#pragma unroll
-                    for (int f = 0; f < 4; ++f)
-                        acc[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                            W::get(s.w[f], i), __builtin_bit_cast(bf16x8_t, s.x[i]), acc[f], 0, 0,
-                            0);
+                for (int i = 0; i < W::KU / 32; ++i) {
+                    const int k = u * W::KU + 32 * i;
+                    x[i] = *reinterpret_cast<const u32x4_any_t*>(xr + (k < d ? k : d - 32));
                 }
-            });
-        if (task != (int)blockIdx.x) __syncthreads();  // the last task's partial tiles have been read
+            }
+            ELB_WAIT_VMCNT(0);
+            asm volatile("" ::: "memory");
+            typename W::Half w[4][2];
 #pragma unroll
-        for (int f = 0; f < 4; ++f) part[wave][f][lane] = acc[f];
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int f = 0; f < 4; ++f) W::read(w[f][h], slot, 64, f, h, l16, hq);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the unit is free again
+            if (u + 1 < u1) b.issue(u + 1, u1, lds, slot, lane);
+            else if (next < tasks) next_e = begin(next);
+            __builtin_amdgcn_sched_barrier(0);
+            auto multiply = [&](int at) {  // at: the unit's first operand in x
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int i = 0; i < W::J; ++i) {
+                        if (u * W::KU + h * (W::KU / 2) + 32 * i >= d) break;
+#pragma unroll
+                        for (int f = 0; f < 4; ++f)
+                            acc[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                                w[f][h].get(i), as_frag(x[at + h * W::J + i]), acc[f], 0, 0, 0);
+                    }
+            };
+            if constexpr (W::KU == 256) {
+                multiply(0);
+            } else {
+                switch (held ? u - u0 : 0) {  // registers have no index
+                    case 0: multiply(0); break;
+                    case 1: multiply(2); break;
+                    case 2: multiply(4); break;
+                    default: multiply(6); break;
+                }
+            }
+        }
+        if (u0 == u1 && next < tasks) next_e = begin(next);
+        f32x4_t* const part = reinterpret_cast<f32x4_t*>(slot + PART);
+#pragma unroll
+        for (int f = 0; f < 4; ++f) part[f * 64 + lane] = acc[f];
         __syncthreads();
         // thread: token tid / 32, column tid % 32; a lane holds rows 4 (lane / 16) .. + 3 of its
         // fragment for token lane % 16
         const int t = tid >> 5, col = tid & 31, f = col >> 4;
         const int l = ((col & 15) >> 2) * 16 + t, i = col & 3;
-        const int slot = slots.slot[e][t];
-        if (slot >= 0) {
-            float g = part[0][f][l][i], up = part[0][f + 2][l][i];
+        if (slots.tokens[e] >> t & 1) {
+            const int at = slots.slot[e][t];
+            float g = 0.f, up = 0.f;
 #pragma unroll
-            for (int q = 1; q < kUpWaves; ++q) {
-                g += part[q][f][l][i];
-                up += part[q][f + 2][l][i];
+            for (int q = 0; q < kUpWaves; ++q) {
+                const float* const p = reinterpret_cast<const float*>(sm + q * SLOT + PART);
+                g += p[(f * 64 + l) * 4 + i];
+                up += p[((f + 2) * 64 + l) * 4 + i];
             }
-            in.h[(int64_t)slot * m + 32 * c + col] = f32_to_bf16(g * sigma_bf16(g) * up * sw[slot]);
+            in.h[(int64_t)at * m + 32 * (task - task / per_e * per_e) + col] =
+                f32_to_bf16(g * sigma_bf16(g) * up * sw[at]);
         }
+        __syncthreads();  // the partial tiles have been read
+        task = next;
+        e = next_e;
     }
 }
 
-// 16 columns of y a block; the used experts' contractions one behind the other, cut evenly into
-// sixteen waves
-template <class W, int R>
+// ------------------------------------------------------------------------------------------
+// Launch 2.  A block has 64 columns of y and one of `shares` shares of the contraction, the used
+// experts' units one behind the other (per expert as often as its tokens fill tiles of eight); its
+// waves take every eighth unit.  The last block of a column tile to write its partial sums adds all
+// of them, in the order of the shares; none waits for another.
+// ------------------------------------------------------------------------------------------
+template <class W, bool DMA>
 __global__ __launch_bounds__(64 * kDownWaves) void few_down(FewIn in) {
-    __shared__ f32x4_t part[kDownWaves][64];
+    typedef Stream<W, 4, false, DMA> B;
+    constexpr int SUB = W::KU / 64, AB = SUB * 8 * 128;  // eight rows of h
+    constexpr int SLOT = (AB + B::BYTES + 255) / 256 * 256;
+    static_assert(SLOT >= 4096, "");
+    __shared__ __attribute__((aligned(1024))) char sm[kDownWaves * SLOT];
     __shared__ Slots slots;
+    __shared__ int last;
     const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, hq = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int d = in.d, m = in.m;
-    find_slots(slots, in.k, in.ids, in.T, in.K, in.N);
-    const int per = (m + W::KS - 1) / W::KS, steps = slots.used * per;
-    const int s0 = steps * wave / kDownWaves, s1 = steps * (wave + 1) / kDownWaves;
-    const int64_t row = (int64_t)blockIdx.x * 16 + l16;
-    struct Slot {
-        typename W::Frag w;
-        u32x4_t x[W::J];
-        bool live;
-    };
-    f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
-    int u = s0 / per, s = s0 - u * per;  // of the next step to load
-    ring<R, Slot>(
-        s1 - s0,
-        [&](int, Slot& sl) {
-            const int e = __builtin_amdgcn_readfirstlane(slots.list[u]);
-            const int slot = slots.slot[e][l16];
-            int k = s * W::KS + W::KS / 4 * hq;
-            sl.live = slot >= 0 && k < m;
-            k = k < m ? k : m - W::KS / 4;
-            expert<W>(in.down, in.d_scale, (int64_t)e * d * m, m).load(sl.w, row, k);
-            const bf16_t* const hr = in.h + (int64_t)(slot >= 0 ? slot : 0) * m + k;
+    const int d = in.d, m = in.m, T = in.T;
+    const int tile = blockIdx.x, share = blockIdx.y;
+    find_slots(slots, in.k, in.ids, T, in.K, in.N);
+    char* const slot = sm + wave * SLOT;
+    const uint32_t lds = lds_address(slot);
+    const int per = (m + W::KU - 1) / W::KU, units = slots.used * per;
+    const int v0 = units * share / in.shares + wave, v1 = units * (share + 1) / in.shares;
+    const int64_t w_bytes = W::row_bytes((int64_t)d * m);
+    B b0;
+    b0.init(in.down, in.d_scale, 64 * tile, 64, 0, m, lane);
+    // rows of h: chunk lane % 8 of row lane / 8, in each of the unit's k-tiles of 64
+    const uint64_t hb = (uint64_t)in.h;
+    const u32x4_t hr = {uniform((uint32_t)hb), uniform((uint32_t)(hb >> 32)) & 0xffffu,
+                        uniform((uint32_t)(T * in.K) * (uint32_t)m * 2u), 0x00027000u};
+    const int chunk = kc_swz(lane >> 3, lane & 7) * 16;
+    auto issue = [&](int v, int pass) {
+        const int u = v / per, unit = v - u * per;
+        const int e = __builtin_amdgcn_readfirstlane(slots.list[u]);
+        b0.moved(e * w_bytes, W::SCALES ? (int64_t)e * d * (m / 32) : 0)
+            .issue(unit, per, lds + AB, slot + AB, lane);
+        const int rank = 8 * pass + (lane >> 3);
+        const int at = rank < __popc(slots.tokens[e]) ? slots.row[e][rank] : -1;
 #pragma unroll
-            for (int i = 0; i < W::J; ++i)
-                sl.x[i] = *reinterpret_cast<const u32x4_any_t*>(hr + 8 * i);
-            if (++s == per) s = 0, ++u;
-        },
-        [&](int, Slot& sl) {
+        for (int q = 0; q < SUB; ++q) {
+            const int k = unit * W::KU + 64 * q;  // m is a multiple of 64
+            const uint32_t off = at < 0 || k >= m ? kOutOfBounds
+                                                  : (uint32_t)at * (uint32_t)m * 2u +
+                                                        (uint32_t)k * 2u + chunk;
+            asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                         :: "s"(lds + q * 1024), "v"(off), "s"(hr) : "memory", "m0");
+        }
+        return e;
+    };
+    f32x4_t acc[4];
+#pragma unroll
+    for (int f = 0; f < 4; ++f) acc[f] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    int pass = 0, e = v0 < v1 ? issue(v0, 0) : 0;
+    for (int v = v0; v < v1;) {
+        ELB_WAIT_VMCNT(0);
+        asm volatile("" ::: "memory");
+        const uint32_t tokens = slots.tokens[e];
+        const int rank = __popc(tokens & ((1u << l16) - 1)) - 8 * pass;
+        const bool live = (tokens >> l16 & 1) && rank >= 0 && rank < 8;
+        const int r = live ? rank : 0;
+        typename W::Half w[4][2];
+        u32x4_t x[2][W::J];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+            for (int f = 0; f < 4; ++f) W::read(w[f][h], slot + AB, 64, f, h, l16, hq);
 #pragma unroll
             for (int i = 0; i < W::J; ++i) {
-                if (!sl.live) sl.x[i] = u32x4_t{0, 0, 0, 0};
-                acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                    W::get(sl.w, i), __builtin_bit_cast(bf16x8_t, sl.x[i]), acc, 0, 0, 0);
+                const int run = h * W::J + i;  // of 32 values
+                x[h][i] = *reinterpret_cast<const u32x4_t*>(
+                    slot + run / 2 * 1024 + r * 128 + kc_swz(r, run % 2 * 4 + hq) * 16);
             }
-        });
-    part[wave][lane] = acc;
-    __syncthreads();
-    if (tid >= 256) return;
-    const int t = tid >> 4, col = tid & 15;
-    if (t >= in.T) return;
-    const int l = (col >> 2) * 16 + t, i = col & 3;
-    float v = part[0][l][i];
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the unit is free again
+        const int k0 = v % per * W::KU;
+        // an expert of more than eight tokens takes another pass
+        if (8 * (pass + 1) < __popc(tokens)) {
+            ++pass;
+        } else {
+            pass = 0;
+            v += kDownWaves;
+        }
+        if (v < v1) e = issue(v, pass);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int q = 1; q < kDownWaves; ++q) v += part[q][l][i];
-    const int64_t o = (int64_t)t * d + (int64_t)blockIdx.x * 16 + col;
-    if (in.residual) v += bf16_to_f32(in.residual[o]);
-    in.y[o] = f32_to_bf16(v);
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < W::J; ++i) {
+                if (k0 + (h * W::J + i) * 32 >= m) break;
+                if (!live) x[h][i] = u32x4_t{0, 0, 0, 0};
+#pragma unroll
+                for (int f = 0; f < 4; ++f)
+                    acc[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[f][h].get(i),
+                                                                     as_frag(x[h][i]), acc[f], 0, 0,
+                                                                     0);
+            }
+    }
+    f32x4_t* const part = reinterpret_cast<f32x4_t*>(slot);
+#pragma unroll
+    for (int f = 0; f < 4; ++f) part[f * 64 + lane] = acc[f];
+    __syncthreads();
+    // value i: token i / 64, column i % 64
+    auto sum = [&](int i) {
+        const int t = i >> 6, col = i & 63;
+        const int at = ((col >> 4) * 64 + ((col & 15) >> 2) * 16 + t) * 4 + (col & 3);
+        float v = reinterpret_cast<const float*>(sm)[at];
+#pragma unroll
+        for (int q = 1; q < kDownWaves; ++q)
+            v += reinterpret_cast<const float*>(sm + q * SLOT)[at];
+        return v;
+    };
+    float* const mine = in.part + (int64_t)tile * in.shares * 1024;
+    auto put = [&](int i, float v) {
+        const int64_t o = (int64_t)(i >> 6) * d + 64 * tile + (i & 63);
+        if (in.residual) v += bf16_to_f32(in.residual[o]);
+        in.y[o] = f32_to_bf16(v);
+    };
+    if (in.shares == 1) {
+        for (int i = tid; i < T * 64; i += 64 * kDownWaves) put(i, sum(i));
+        return;
+    }
+    // The partial sums go past the L2, which blocks elsewhere on the chip do not share: agent-scope
+    // stores, done when the counter goes up, and agent-scope loads.  (A release fence would write
+    // the whole L2 back, for each block: 31 us in place of 2.)
+    for (int i = tid; i < T * 64; i += 64 * kDownWaves)
+        __hip_atomic_store(mine + share * 1024 + i, sum(i), __ATOMIC_RELAXED,
+                           __HIP_MEMORY_SCOPE_AGENT);
+    ELB_WAIT_VMCNT(0);
+    __syncthreads();
+    if (tid == 0)
+        last = __hip_atomic_fetch_add(in.count + tile, 1, __ATOMIC_RELAXED,
+                                      __HIP_MEMORY_SCOPE_AGENT) == in.shares - 1;
+    __syncthreads();
+    if (!last) return;
+    for (int i = tid; i < T * 64; i += 64 * kDownWaves) {
+        float p[16], v = 0.f;
+#pragma unroll
+        for (int q = 0; q < 16; ++q)
+            p[q] = q < in.shares ? __hip_atomic_load(mine + q * 1024 + i, __ATOMIC_RELAXED,
+                                                     __HIP_MEMORY_SCOPE_AGENT)
+                                 : 0.f;
+#pragma unroll
+        for (int q = 0; q < 16; ++q) v += p[q];
+        put(i, v);
+    }
 }
 
-template <class W, int NG, int RU>
-void run_up(const FewIn& in, unsigned blocks, hipStream_t s) {
-    const XTable xt = make_xtable(in.N);
-    if (in.K <= 8)
-        ELB_LAUNCH((few_up<W, NG, 8, RU>), dim3(blocks), dim3(64 * kUpWaves), 0, s, in, xt);
-    else
-        ELB_LAUNCH((few_up<W, NG, kLaneMaxK, RU>), dim3(blocks), dim3(64 * kUpWaves), 0, s, in, xt);
-}
-
-template <class W, int RU, int RD>
+template <class W, bool DMA>
 hipError_t few(const FewIn& in, int cus, hipStream_t s) {
     {
         ProfileScope prof("few_up", s);
         const int most = (in.T * in.K < in.N ? in.T * in.K : in.N) * (in.m / 32);
-        const unsigned blocks = most < cus ? most : cus;
-        if (in.N > 48) run_up<W, 4, RU>(in, blocks, s);
-        else if (in.N > 32) run_up<W, 3, RU>(in, blocks, s);
-        else if (in.N > 16) run_up<W, 2, RU>(in, blocks, s);
-        else run_up<W, 1, RU>(in, blocks, s);
+        const dim3 blocks((unsigned)(most < cus ? most : cus));
+        const XTable xt = make_xtable(in.N);
+        if (in.K <= 8)
+            ELB_LAUNCH((few_up<W, 8, DMA>), blocks, dim3(64 * kUpWaves), 0, s, in, xt);
+        else
+            ELB_LAUNCH((few_up<W, kLaneMaxK, DMA>), blocks, dim3(64 * kUpWaves), 0, s, in, xt);
         if (hipError_t e = hipGetLastError()) return e;
     }
     ProfileScope prof("few_down", s);
-    ELB_LAUNCH((few_down<W, RD>), dim3(in.d / 16), dim3(64 * kDownWaves), 0, s, in);
+    ELB_LAUNCH((few_down<W, DMA>), dim3(in.d / 64, in.shares), dim3(64 * kDownWaves), 0, s, in);
     return hipGetLastError();
 }
 
 }  // namespace
 
+// shares of launch 2's contraction: so many that its blocks fill the compute units
+int few_shares(int d) {
+    const int n = 256 / (d / 64);
+    return n < 1 ? 1 : n > 16 ? 16 : n;
+}
+
 hipError_t launch_moe_few(const void* x, const void* Wr, const void* Wgu, const uint8_t* gu_scale,
                           const void* Wd, const uint8_t* d_scale, const void* res, int64_t T, int d,
-                          int N, int m, const elb_route_params& p, void* h, void* y, int* k,
-                          int* ids, float* w, int cus, hipStream_t s) {
+                          int N, int m, const elb_route_params& p, void* h, float* part, int* count,
+                          void* y, int* k, int* ids, float* w, int cus, hipStream_t s) {
     const FewIn in{(const bf16_t*)x, (const bf16_t*)Wr, Wgu, Wd, gu_scale, d_scale,
                    (const bf16_t*)res, (int)T, d, N, m, p.K, p.mode, p.renormalize, p.eps,
-                   (bf16_t*)h, (bf16_t*)y, k, ids, w};
-    return gu_scale ? few<WF4, 4, 4>(in, cus, s) : few<WBf16, 8, 8>(in, cus, s);
+                   (bf16_t*)h, (bf16_t*)y, k, ids, w, part, count, few_shares(d)};
+    const bool dma = aligned16(x, Wr) && aligned16(Wgu, Wd);
+    if (!gu_scale) return dma ? few<WBf16, true>(in, cus, s) : few<WBf16, false>(in, cus, s);
+    return dma && f4_copies(Wgu, gu_scale, d) && f4_copies(Wd, d_scale, m)
+               ? few<WF4, true>(in, cus, s)
+               : few<WF4, false>(in, cus, s);
 }
 
 }  // namespace elb
