@@ -610,29 +610,38 @@ def elb_ffn_forward_i8(x, W_gate_up, gate_up_scale, W_down, down_scale, residual
     return y
 
 
+def _gate_kind(gate, T: int, d: int) -> int:
+    """By shape: [d], [T, 1] or [T, d] (d >= 16, so that no shape is two of them)."""
+    shape = gate.shape
+    if len(shape) == 1 and shape[0] == d:
+        return GATE_CHANNEL
+    if len(shape) == 2 and shape[0] == T and shape[1] in (1, d):
+        return GATE_TOKEN if shape[1] == 1 else GATE_FULL
+    raise ValueError("gate must have shape [T, d], [T, 1] or [d], not %s" % (tuple(shape),))
+
+
 def _norm_op(residual, block, w_post, w_pre, gate, residual_scale, block_scale, eps):
-    """(NormOp, T, d, a tensor of the stream's shape, device); the operands checked."""
-    like = block if block is not None else residual
+    """(NormOp, a tensor of the stream's shape, its shape, type and device); the operands checked."""
+    like = residual if block is None else block
     if like is None:
         raise ValueError("neither residual nor block")
-    T, d = _matrix("residual" if block is None else "block", like)
+    shape, dtype = _matrix("residual" if block is None else "block", like), like.dtype
+    T, d = shape
     dt, dev = _dtype_code(like), _device(like)
-    _want("residual", residual, (T, d), like.dtype, dev)
-    _want("block", block, (T, d), like.dtype, dev)
-    _want("w_post", w_post, (d,), like.dtype, dev)
-    _want("w_pre", w_pre, (d,), like.dtype, dev)
+    _want("residual" if block is None else "block", like, shape, dtype, dev)
+    if residual is not like:
+        _want("residual", residual, shape, dtype, dev)
+    if w_post is not None:
+        _want("w_post", w_post, (d,), dtype, dev)
+    if w_pre is not None:
+        _want("w_pre", w_pre, (d,), dtype, dev)
     kind = GATE_NONE
     if gate is not None:
-        # [T, d] before [T, 1] and [d]: with d >= 16 no shape is two of them
-        kinds = {(T, d): GATE_FULL, (T, 1): GATE_TOKEN, (d,): GATE_CHANNEL}
-        kind = kinds.get(tuple(gate.shape))
-        if kind is None:
-            raise ValueError("gate must have shape [T, d], [T, 1] or [d], not %s"
-                             % (tuple(gate.shape),))
-        _want("gate", gate, gate.shape, like.dtype, dev)
+        kind = _gate_kind(gate, T, d)
+        _want("gate", gate, gate.shape, dtype, dev)
     op = NormOp(_ptr(residual), _ptr(block), _ptr(gate), _ptr(w_post), _ptr(w_pre), T, d, kind, dt,
                 residual_scale, block_scale, eps)
-    return op, T, d, like, dev
+    return op, like, shape, dtype, dev
 
 
 def elb_norm_forward(residual=None, block=None, w_post=None, w_pre=None, gate=None,
@@ -643,19 +652,25 @@ def elb_norm_forward(residual=None, block=None, w_post=None, w_pre=None, gate=No
     keep=True (sum, normed, kept): kept is what elb_norm_backward needs of the forward pass.
     gate: [d], [T, 1], [T, d] or None.  out (of sum) may be residual.  Without a block, an out and a
     residual_scale, sum is residual itself.  Outside autograd: results never require a gradient."""
-    op, T, d, like, dev = _norm_op(residual, block, w_post, w_pre, gate, residual_scale,
-                                   block_scale, eps)
-    _want("out", out, (T, d), like.dtype, dev)
-    same = out is None and block is None and residual_scale == 1.0
-    total = residual.detach() if same else torch.empty_like(like) if out is None else out
+    op, like, shape, dtype, dev = _norm_op(residual, block, w_post, w_pre, gate, residual_scale,
+                                           block_scale, eps)
+    same = block is None and out is None and residual_scale == 1.0
+    if same:
+        total = residual.detach()
+    elif out is None:
+        total = torch.empty_like(like)
+    else:
+        _want("out", out, shape, dtype, dev)
+        total = out
     normed = None if w_pre is None else torch.empty_like(like)
     kept = (None, None)
     if keep:
-        kept = tuple(None if w is None else torch.empty(T, dtype=torch.float32, device=like.device)
-                     for w in (w_post, w_pre))
-    _check("elb_norm_forward", lib().elb_norm_forward(
-        C.byref(op), None if same else _ptr(total), _ptr(normed), _ptr(kept[0]), _ptr(kept[1]),
-        _stream()))
+        kept = tuple(None if w is None else torch.empty(shape[:1], dtype=torch.float32,
+                                                        device=like.device) for w in (w_post, w_pre))
+    status = lib().elb_norm_forward(C.byref(op), None if same else total.data_ptr(), _ptr(normed),
+                                    _ptr(kept[0]), _ptr(kept[1]), _stream())
+    if status:
+        _check("elb_norm_forward", status)
     return (total, normed, kept) if keep else (total, normed)
 
 
@@ -670,21 +685,23 @@ def elb_norm_backward(d_sum, d_normed, sum, block, kept, w_post=None, w_pre=None
     """-> (d_residual, d_block, d_gate, d_w_post, d_w_pre), None where need is false or the forward
     had no such tensor (d_residual always is computed if needed).  d_sum or d_normed may be None
     (zero).  sum and kept from elb_norm_forward(..., keep=True), the rest as given to it."""
-    op, T, d, like, dev = _norm_op(sum if block is None else None, block, w_post, w_pre, gate,
-                                   residual_scale, block_scale, 1.0)
-    _want("d_sum", d_sum, (T, d), like.dtype, dev)
-    _want("d_normed", d_normed, (T, d), like.dtype, dev)
-    _want("sum", sum, (T, d), like.dtype, dev)
+    op, like, shape, dtype, dev = _norm_op(sum if block is None else None, block, w_post, w_pre,
+                                           gate, residual_scale, block_scale, 1.0)
+    for name, t in (("d_sum", d_sum), ("d_normed", d_normed), ("sum", sum)):
+        if t is not None:
+            _want(name, t, shape, dtype, dev)
     r_post, r_pre = kept
-    _want("kept", r_post, (T,), torch.float32, dev)
-    _want("kept", r_pre, (T,), torch.float32, dev)
-    shapes = (like, block, gate, w_post, w_pre)
-    out = [torch.empty_like(t) if n and t is not None else None for t, n in zip(shapes, need)]
+    _want("kept", r_post, shape[:1], torch.float32, dev)
+    _want("kept", r_pre, shape[:1], torch.float32, dev)
+    out = [torch.empty_like(t) if n and t is not None else None
+           for t, n in zip((like, block, gate, w_post, w_pre), need)]
     stream = _stream()
-    ws = workspace(elb_norm_backward_workspace_bytes(T, d), like.device, stream)
-    _check("elb_norm_backward", lib().elb_norm_backward(
+    ws = workspace(elb_norm_backward_workspace_bytes(*shape), like.device, stream)
+    status = lib().elb_norm_backward(
         C.byref(op), _ptr(d_sum), _ptr(d_normed), _ptr(sum), _ptr(r_post), _ptr(r_pre),
-        *(_ptr(t) for t in out), _ptr(ws), ws.numel(), stream))
+        *[_ptr(t) for t in out], ws.data_ptr(), ws.numel(), stream)
+    if status:
+        _check("elb_norm_backward", status)
     return tuple(out)
 
 

@@ -263,11 +263,11 @@ int check_f4(int64_t T, int n, const char* nn, int k, const char* kn) {
                     kn, k);
     return ELB_OK;
 }
-// sub-buffers of a projection's and the block's workspace; `most` as above
+// sub-buffers of the workspace of a projection (m = 0) or of the block (n = d, k = m); `most` as above
 struct F4Layout {
     size_t h, wgu, wd, part, total;
 };
-F4Layout f4_layout(int64_t T, int n, int64_t k, int m, int dtype, bool most) {
+F4Layout f4_layout(int64_t T, int n, int k, int m, int dtype, bool most) {
     F4Layout L{};
     size_t o = 0;
     auto take = [&](size_t bytes) {
@@ -277,12 +277,16 @@ F4Layout f4_layout(int64_t T, int n, int64_t k, int m, int dtype, bool most) {
     };
     const size_t e = esize(dtype);
     L.h = take((size_t)T * m * e);
-    if (!f4_streams(T, dtype)) {
-        L.wgu = take((size_t)2 * m * n * e);
-        L.wd = take((size_t)n * k * e);
-        L.part = take(ffn_halves_bytes(T, n, k, dtype, most));
+    if (most ? T <= kStreamedAlways : f4_streams(T, n, k, m > 0, dtype)) {
+        L.part = take(most ? f4_part_reserve(T, n, k, dtype) : f4_part_bytes(T, n, k, dtype));
+        L.total = o;
+        return L;
     }
-    L.total = o;
+    const size_t streamed = most ? o + align_up(f4_part_reserve(T, n, k, dtype)) : 0;
+    L.wgu = take((size_t)2 * m * n * e);
+    L.wd = take((size_t)n * k * e);
+    L.part = take(ffn_halves_bytes(T, n, k, dtype, most));
+    L.total = std::max(o, streamed);
     return L;
 }
 

@@ -228,8 +228,14 @@ hipError_t launch_norm_backward(const elb_norm& p, const void* ds, const void* d
                                 hipStream_t s);
 
 // 4-bit weights (f4.hip).  Few tokens stream them as they are; for more they are converted to
-// dtype in scratch (w; wgu and wd) and multiplied by the dense forms, with `part` of ffn_halves_bytes
-bool f4_streams(int64_t T, int dtype);
+// dtype in scratch (w; wgu and wd) and multiplied by the dense forms, with `part` of ffn_halves_bytes.
+// part: null, or f4_part_bytes, where they are streamed
+constexpr int64_t kStreamedAlways = 64, kMostStreamed = 2048;
+bool f4_streams(int64_t T, int n, int k, bool block, int dtype);
+// scratch of the streamed product [T, k] x [n, k] for blocks that share a tile, and the most of it that
+// any batch of up to T tokens needs
+size_t f4_part_bytes(int64_t T, int n, int k, int dtype);
+size_t f4_part_reserve(int64_t T, int n, int k, int dtype);
 hipError_t launch_quantize_f4(const void* x, int64_t rows, int d, int dtype, uint8_t* q,
                               uint8_t* scale, hipStream_t s);
 hipError_t launch_linear_f4(const void* x, const uint8_t* W, const uint8_t* W_scale,

@@ -97,8 +97,8 @@ struct WF4 {
 };
 
 // One wave's copies of a unit of weights: 16 NF rows (PAIR: the second half of them `apart` rows of
-// the tensor further on) of 128 bytes, and the rows' eight scale bytes behind them.  DMA: tensors on
-// 16-byte boundaries, and scale rows on 4-byte ones; otherwise ordinary loads.
+// the tensor further on) of 128 bytes, and the rows' eight scale bytes behind them.  DMA: weights on
+// 16-byte boundaries; otherwise ordinary loads, as for scales whose rows are off 4-byte ones.
 template <class W, int NF, bool PAIR, bool DMA>
 struct Stream {
     static constexpr int ROWS = 16 * NF;
@@ -108,15 +108,20 @@ struct Stream {
     C copy;
     const uint8_t* scale[(ROWS + 31) / 32];  // of the lane's rows
     int groups;                              // of a row
+    const uint8_t* end;                      // of the scales
+    bool words;                              // scale rows start on 4-byte boundaries
 
-    // row0: the tile's first row; rows: valid ones from there on (of each half with PAIR)
+    // row0: the tile's first row; rows: valid ones from there on (of each half with PAIR); all: rows of
+    // the matrix
     __device__ __forceinline__ void init(const void* w, const uint8_t* s, int64_t row0, int rows,
-                                         int64_t apart, int64_t k, int lane) {
+                                         int64_t apart, int64_t all, int64_t k, int lane) {
         const int64_t ld = W::row_bytes(k);
         copy.init((const char*)w + row0 * ld, (const char*)w + (row0 + apart) * ld, ld, rows, ld,
                   lane, 0);
         if (!W::SCALES) return;
         groups = (int)(k / 32);
+        end = s + all * groups;
+        words = DMA && (groups & 3) == 0 && ((uintptr_t)s & 3) == 0;
         constexpr int HR = PAIR ? ROWS / 2 : ROWS;
 #pragma unroll
         for (int i = 0; i < (ROWS + 31) / 32; ++i) {
@@ -130,26 +135,41 @@ struct Stream {
             scale[i] = s + (row + (r < rows ? r : rows - 1)) * groups;
         }
     }
+    // scale words on their way to LDS by ordinary loads
+    struct Pending {
+        uint32_t v[(ROWS + 31) / 32];
+    };
     // unit u to LDS at lds (ldsp: the same as a pointer); past uend zeros
-    __device__ __forceinline__ void issue(int u, int uend, uint32_t lds, char* ldsp, int lane) const {
+    __device__ __forceinline__ void issue(int u, int uend, uint32_t lds, char* ldsp, int lane,
+                                          Pending& pending) const {
         copy.issue(u, uend, lds, ldsp, lane, 0);
         if constexpr (W::SCALES != 0) {
             const int g = 8 * u + 4 * (lane & 1);
 #pragma unroll
             for (int i = 0; i < (ROWS + 31) / 32; ++i) {
-                if constexpr (DMA) {
-                    // groups past the row's last: its last four, which no product takes
+                // groups past the row's last: other bytes of the tensor, which no product takes
+                if (words) {
                     const uint8_t* const p = scale[i] + (g < groups ? g : groups - 4);
                     asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, off"
-                                 :: "s"(lds + ROWS * 128 + i * 256), "v"(p) : "memory", "m0");
-                } else if (32 * i + (lane >> 1) < ROWS) {
-                    uint32_t v = 0;
-#pragma unroll
-                    for (int q = 0; q < 4; ++q)
-                        if (g + q < groups) v |= (uint32_t)scale[i][g + q] << (8 * q);
-                    *reinterpret_cast<uint32_t*>(ldsp + ROWS * 128 + i * 256 + lane * 4) = v;
+                                 :: "s"(uniform(lds + ROWS * 128 + i * 256)), "v"(p)
+                                 : "memory", "m0");
+                } else {
+                    // a word at any byte; the tensor's last one moved down to lie in it
+                    const uint8_t* const p = scale[i] + (g < groups ? g : 0);
+                    const int64_t over = p + 4 - end;
+                    const int past = over > 0 ? (int)over : 0;
+                    pending.v[i] = *reinterpret_cast<const u32_byte_t*>(p - past) >> (8 * past);
                 }
             }
+        }
+    }
+    // after the wait for a unit, before it is read
+    __device__ __forceinline__ void settle(const Pending& pending, char* ldsp, int lane) const {
+        if constexpr (W::SCALES != 0) {
+            if (words) return;
+#pragma unroll
+            for (int i = 0; i < (ROWS + 31) / 32; ++i)
+                *reinterpret_cast<uint32_t*>(ldsp + ROWS * 128 + i * 256 + lane * 4) = pending.v[i];
         }
     }
     // the same rows of another matrix, w_bytes and s_bytes further on
@@ -160,15 +180,11 @@ struct Stream {
         if (W::SCALES) {
 #pragma unroll
             for (int i = 0; i < (ROWS + 31) / 32; ++i) o.scale[i] += s_bytes;
+            o.end += s_bytes;
         }
         return o;
     }
 };
-// whether weights and scales of rows of k values may be copied by DMA
-inline bool f4_copies(const void* w, const void* s, int64_t k) {
-    return (uintptr_t)w % 16 == 0 && (uintptr_t)s % 4 == 0 && k % 128 == 0;
-}
-
 }  // namespace
 
 }  // namespace elb

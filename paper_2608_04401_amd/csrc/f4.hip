@@ -129,6 +129,9 @@ struct Tok<float> {
     }
 };
 
+constexpr int kMostShares = 16, kMostSharing = 512;  // shares of a tile, blocks of tiles with shares
+Counters f4_counters(void* part, int64_t T, int n, int k, int dtype);
+
 template <class X>
 struct StreamIn {
     const X* x;
@@ -137,6 +140,12 @@ struct StreamIn {
     X* out;
     int64_t T;
     int cols, k;  // output columns; PAIR: weight rows [0, cols) gates, [cols, 2 cols) ups
+    // shares > 1: a tile's contraction in that many blocks; their partial sums [tiles, shares, TM, 16 NF],
+    // and how many of a tile's are written (zero before the launch)
+    int shares;
+    float* part;
+    uint32_t* count;
+    Counters clear;  // the next launch's counters
 };
 
 // ------------------------------------------------------------------------------------------
@@ -144,7 +153,9 @@ struct StreamIn {
 // and the other half the matching up rows).  Each of NW waves has a share of the contraction and walks
 // it alone: a unit's weights and tokens are copied into the wave's LDS, read into registers, and the
 // next unit's copies run while this one is multiplied; no barrier until the waves' partial tiles are
-// added, in order.  Bound by the weights' stream, or by the latency of its start.
+// added, in order.  Bound by the weights' stream, or by the latency of its start.  Where tiles are few,
+// blocks share the contraction of one (blockIdx.z): the last of them to write its partial sums adds all,
+// in the order of the shares; none waits for another.
 // ------------------------------------------------------------------------------------------
 template <class X, int TM, int NF, int NW, bool PAIR, bool DMA>
 __global__ __launch_bounds__(64 * NW) void stream_f4(StreamIn<X> in) {
@@ -159,20 +170,24 @@ __global__ __launch_bounds__(64 * NW) void stream_f4(StreamIn<X> in) {
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int c0 = (int)blockIdx.x * 16 * OF;
     const int64_t t0 = (int64_t)blockIdx.y * TM;
-    const int units = (in.k + 255) / 256;
-    const int u0 = units * wave / NW, u1 = units * (wave + 1) / NW;
+    if (blockIdx.x == 0 && blockIdx.y == 0 && blockIdx.z == 0)
+        for (int i = threadIdx.x; i < in.clear.n; i += 64 * NW) in.clear.p[i] = 0;
+    const int units = (in.k + 255) / 256, ways = NW * in.shares, way = NW * blockIdx.z + wave;
+    const int u0 = units * way / ways, u1 = units * (way + 1) / ways;
     char* const slot = sm + wave * SLOT;
     const uint32_t lds = lds_address(slot);
     A a;
     a.init(in.x + t0 * in.k, nullptr, (int64_t)in.k * sizeof(X),
            in.T - t0 < TM ? (int)(in.T - t0) : TM, in.k, lane, 0);
     B b;
-    b.init(in.w, in.scale, c0, in.cols - c0, in.cols, in.k, lane);
+    b.init(in.w, in.scale, c0, in.cols - c0, in.cols, PAIR ? 2 * (int64_t)in.cols : in.cols, in.k,
+           lane);
+    typename B::Pending pending = {};
     auto issue = [&](int u) {
 #pragma unroll
         for (int q = 0; q < SUB; ++q)
             a.issue(SUB * u + q, SUB * u1, lds + q * TM * 128, slot + q * TM * 128, lane, 0);
-        b.issue(u, u1, lds + AB, slot + AB, lane);
+        b.issue(u, u1, lds + AB, slot + AB, lane, pending);
     };
     f32x4_t acc[MT][NF];
 #pragma unroll
@@ -182,6 +197,7 @@ __global__ __launch_bounds__(64 * NW) void stream_f4(StreamIn<X> in) {
     if (u0 < u1) issue(u0);
     for (int u = u0; u < u1; ++u) {
         ELB_WAIT_VMCNT(0);
+        b.settle(pending, slot + AB, lane);
         asm volatile("" ::: "memory");  // the copies write LDS behind the compiler's back
         WF4::Half w[NF][2];
         Tok<X> x[MT][2][4];
@@ -230,22 +246,20 @@ __global__ __launch_bounds__(64 * NW) void stream_f4(StreamIn<X> in) {
 #pragma unroll
         for (int f = 0; f < NF; ++f) *part(wave, t, f, lane) = acc[t][f];
     __syncthreads();
-    // a lane of a tile's fragment has columns 16 f + 4 (lane / 16) .. + 3 of token 16 t + lane % 16
-    for (int i = threadIdx.x; i < MT * OF * 64; i += NW * 64) {
-        const int l = i & 63, f = i / 64 % OF, t = i / (64 * OF);
-        auto sum = [&](int ff) {
-            f32x4_t v = *part(0, t, ff, l);
+    // fragment f of token tile t in the block's sum, four values a lane
+    auto sum = [&](int t, int f, int l) {
+        f32x4_t v = *part(0, t, f, l);
 #pragma unroll
-            for (int w = 1; w < NW; ++w) v += *part(w, t, ff, l);
-            return v;
-        };
-        f32x4_t v = sum(f);
+        for (int w = 1; w < NW; ++w) v += *part(w, t, f, l);
+        return v;
+    };
+    // a lane of a tile's fragment has columns 16 f + 4 (lane / 16) .. + 3 of token 16 t + lane % 16
+    auto put = [&](int t, int f, int l, f32x4_t v, f32x4_t u) {
         const int64_t r = t0 + 16 * t + (l & 15);
         const int c = c0 + 16 * f + 4 * (l >> 4);
-        if (r >= in.T || 16 * t + (l & 15) >= TM || c >= in.cols) continue;
+        if (r >= in.T || 16 * t + (l & 15) >= TM || c >= in.cols) return;
         const int64_t o = r * in.cols + c;
         if constexpr (PAIR) {
-            const f32x4_t u = sum(f + OF);
 #pragma unroll
             for (int q = 0; q < 4; ++q)
                 v[q] = v[q] * (sizeof(X) == 2 ? sigma_bf16(v[q]) : sigma_f32(v[q])) * u[q];
@@ -263,36 +277,142 @@ __global__ __launch_bounds__(64 * NW) void stream_f4(StreamIn<X> in) {
             if (!PAIR && in.res) v += *reinterpret_cast<const f32x4_any_t*>(in.res + o);
             *reinterpret_cast<f32x4_any_t*>(in.out + o) = v;
         }
+    };
+    constexpr int PIECES = MT * OF * 64;  // of four values
+    if (PAIR || in.shares == 1) {
+        for (int i = threadIdx.x; i < PIECES; i += NW * 64) {
+            const int l = i & 63, f = i / 64 % OF, t = i / (64 * OF);
+            put(t, f, l, sum(t, f, l), PAIR ? sum(t, (f + OF) % NF, l) : f32x4_t{});
+        }
+        return;
+    }
+    if constexpr (!PAIR) {
+        // The partial sums go past the L2, which blocks elsewhere on the chip do not share: agent-scope
+        // stores, done when the counter goes up, and agent-scope loads.  (A release fence would
+        // write the whole L2 back, for each block: some 30 us.)
+        const int64_t tile = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+        float* const mine = in.part + tile * in.shares * (PIECES * 4);
+        __shared__ int last;
+        for (int i = threadIdx.x; i < PIECES; i += NW * 64) {
+            const f32x4_t v = sum(i / (64 * OF), i / 64 % OF, i & 63);
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                __hip_atomic_store(mine + ((int64_t)blockIdx.z * 4 + q) * PIECES + i, v[q],
+                                   __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+        ELB_WAIT_VMCNT(0);
+        __syncthreads();
+        if (threadIdx.x == 0)
+            last = __hip_atomic_fetch_add(in.count + tile, 1u, __ATOMIC_RELAXED,
+                                          __HIP_MEMORY_SCOPE_AGENT) == (uint32_t)in.shares - 1;
+        __syncthreads();
+        if (!last) return;
+        for (int i = threadIdx.x; i < PIECES; i += NW * 64) {
+            f32x4_t v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+            for (int z = 0; z < in.shares; ++z)
+#pragma unroll
+                for (int q = 0; q < 4; ++q)
+                    v[q] += __hip_atomic_load(mine + ((int64_t)z * 4 + q) * PIECES + i,
+                                              __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            put(i / (64 * OF), i / 64 % OF, i & 63, v, f32x4_t{});
+        }
     }
 }
 
 template <class X, int TM, int NF, int NW, bool PAIR>
 void run_stream(const StreamIn<X>& in, hipStream_t s) {
     constexpr int OC = 16 * (PAIR ? NF / 2 : NF);
-    const dim3 grid((unsigned)((in.cols + OC - 1) / OC), (unsigned)((in.T + TM - 1) / TM));
-    if (aligned16(in.x, in.w) && f4_copies(in.w, in.scale, in.k))
+    const dim3 grid((unsigned)((in.cols + OC - 1) / OC), (unsigned)((in.T + TM - 1) / TM),
+                    (unsigned)in.shares);
+    if (aligned16(in.x, in.w))
         ELB_LAUNCH((stream_f4<X, TM, NF, NW, PAIR, true>), grid, dim3(64 * NW), 0, s, in);
     else
         ELB_LAUNCH((stream_f4<X, TM, NF, NW, PAIR, false>), grid, dim3(64 * NW), 0, s, in);
 }
 
-template <class X, bool PAIR>
-void stream(const StreamIn<X>& in, hipStream_t s) {
-    constexpr bool F = sizeof(X) == 4;
-    const int rows = PAIR ? 2 * in.cols : in.cols;
-    if (in.T <= 8) {
-        if (!PAIR && rows <= 16 * 256) return run_stream<X, 8, PAIR ? 2 : 1, F ? 8 : 16, PAIR>(in, s);
-        if (rows <= 32 * 256) return run_stream<X, 8, 2, 8, PAIR>(in, s);
-        return run_stream<X, 8, 4, 8, PAIR>(in, s);
-    }
-    if (in.T <= 16) {
-        if (!PAIR && rows <= 16 * 256) return run_stream<X, 16, PAIR ? 2 : 1, F ? 4 : 8, PAIR>(in, s);
-        if (rows <= 32 * 256) return run_stream<X, 16, 2, F ? 4 : 8, PAIR>(in, s);
-        return run_stream<X, 16, 4, F ? 4 : 8, PAIR>(in, s);
-    }
-    if (F || in.T <= 32) return run_stream<X, 32, 2, 4, PAIR>(in, s);
-    return run_stream<X, F ? 32 : 64, 2, 4, PAIR>(in, s);
+// The tile and waves of a streamed product, in how many shares its contraction is cut, and its
+// estimated time: start + rounds (round + iter * units of a wave) [+ share] us, with rounds of `per` blocks
+// on each of 256 compute units.  The constants are least-squares fits over 1 to 768 tokens and weights
+// of 1024 to 16384 rows of 512 to 8192 values; over these the choice is 0.4 % slower than the best form
+// on average and 18 % at worst (fp32, 96 tokens, 512 to 4096 11.2 for 9.6).  bf16, us, at both sides: 48
+// tokens, 8192 to 2048: 48 x 32 tiles in four shares 10.5, whole 15.7, 48 x 64 in four 12.0, whole 20.5;
+// 2048 to 16384: 48 x 64 9.0, 32 x 64 12.9, 48 x 32 11.0.
+struct StreamForm {
+    int tm, nf, nw, per;
+    float start, round, iter, share;
+    int shares = 1;
+    float time = 0;
+};
+constexpr StreamForm kStreamBf16[] = {
+    {8, 1, 16, 1, 1.2f, 1.75f, 1.6f, 3.5f},   {8, 2, 8, 2, 1.7f, 1.7f, 1.0f, 2.7f},
+    {8, 4, 8, 1, 1.5f, 2.0f, 1.72f, 2.8f},    {16, 1, 8, 1, 1.63f, 1.29f, 0.92f, 3.2f},
+    {16, 2, 8, 1, 1.44f, 1.58f, 1.19f, 2.8f}, {16, 4, 8, 1, 1.5f, 1.8f, 1.88f, 2.9f},
+    {32, 2, 4, 1, 1.34f, 1.35f, 1.24f, 3.5f}, {32, 4, 4, 1, 0.93f, 2.15f, 1.82f, 4.0f},
+    {48, 2, 4, 1, 1.07f, 1.7f, 1.58f, 4.2f},  {48, 4, 4, 1, 0.57f, 2.6f, 2.29f, 4.9f}};
+constexpr StreamForm kStreamF32[] = {
+    {8, 1, 8, 1, 1.39f, 1.4f, 2.22f, 3.5f},   {8, 2, 8, 1, 1.22f, 1.7f, 2.71f, 2.8f},
+    {8, 4, 8, 1, 1.65f, 1.65f, 3.7f, 2.8f},   {16, 1, 4, 1, 1.5f, 1.45f, 1.46f, 3.3f},
+    {16, 2, 4, 1, 1.22f, 1.48f, 2.1f, 3.3f},  {16, 4, 4, 1, 0.84f, 2.11f, 2.76f, 3.4f},
+    {32, 2, 4, 1, 1.14f, 1.35f, 3.42f, 3.6f}};
+int stream_tiles(const StreamForm& f, int64_t T, int rows) {
+    return (rows + 16 * f.nf - 1) / (16 * f.nf) * (int)((T + f.tm - 1) / f.tm);
 }
+StreamForm stream_form(int64_t T, int cols, int k, bool pair, bool f32) {
+    const int rows = pair ? 2 * cols : cols, units = (k + 255) / 256;
+    StreamForm best = kStreamBf16[0];
+    bool any = false;
+    const StreamForm* const table = f32 ? kStreamF32 : kStreamBf16;
+    const int n = f32 ? (int)(sizeof(kStreamF32) / sizeof(kStreamF32[0]))
+                      : (int)(sizeof(kStreamBf16) / sizeof(kStreamBf16[0]));
+    for (int i = 0; i < n; ++i) {
+        StreamForm f = table[i];
+        // (the fits hold there; gate and up rows are two fragments at least)
+        if ((f.tm == 8 && T > 8) || (f.tm == 16 && T > 16 && !f32) || (pair && f.nf == 1)) continue;
+        const int64_t tiles = stream_tiles(f, T, rows);
+        for (f.shares = 1; f.shares <= (pair ? 1 : kMostShares); f.shares *= 2) {
+            if (f.shares > 1 && (f.shares * f.nw > units || tiles * f.shares > kMostSharing)) break;
+            const int64_t blocks = tiles * f.shares, rounds = (blocks + 256 * f.per - 1) / (256 * f.per);
+            const int its = (units + f.nw * f.shares - 1) / (f.nw * f.shares);
+            f.time = f.start + (float)rounds * (f.round + f.iter * (float)its) +
+                     (f.shares > 1 ? f.share : 0.0f);
+            if (!any || f.time < best.time) best = f, any = true;
+        }
+    }
+    return best;
+}
+
+// the counters of a shared product's scratch, or none
+Counters f4_counters(void* part, int64_t T, int n, int k, int dtype) {
+    const StreamForm f = stream_form(T, n, k, false, dtype == ELB_F32);
+    if (!part || f.shares == 1) return {nullptr, 0};
+    const int tiles = stream_tiles(f, T, n);
+    const size_t each = (size_t)f.shares * ((f.tm + 15) / 16 * 16) * 16 * f.nf * 4;
+    return {reinterpret_cast<uint32_t*>((char*)part + tiles * each), tiles};
+}
+
+template <class X, bool PAIR>
+void stream(StreamIn<X> in, void* part, hipStream_t s) {
+    constexpr bool F = sizeof(X) == 4;
+    const StreamForm f = stream_form(in.T, in.cols, in.k, PAIR, F);
+    in.shares = f.shares;
+    in.part = (float*)part;
+    in.count = f4_counters(part, in.T, in.cols, in.k, F ? ELB_F32 : ELB_BF16).p;
+    switch (f.tm * 8 + f.nf) {
+        case 8 * 8 + 1: return run_stream<X, 8, PAIR ? 2 : 1, F ? 8 : 16, PAIR>(in, s);
+        case 8 * 8 + 2: return run_stream<X, 8, 2, 8, PAIR>(in, s);
+        case 8 * 8 + 4: return run_stream<X, 8, 4, 8, PAIR>(in, s);
+        case 16 * 8 + 1: return run_stream<X, 16, PAIR ? 2 : 1, F ? 4 : 8, PAIR>(in, s);
+        case 16 * 8 + 2: return run_stream<X, 16, 2, F ? 4 : 8, PAIR>(in, s);
+        case 16 * 8 + 4: return run_stream<X, 16, 4, F ? 4 : 8, PAIR>(in, s);
+        case 32 * 8 + 2: return run_stream<X, 32, 2, 4, PAIR>(in, s);
+        case 32 * 8 + 4: return run_stream<X, 32, F ? 2 : 4, 4, PAIR>(in, s);
+        case 48 * 8 + 2: return run_stream<X, F ? 32 : 48, 2, 4, PAIR>(in, s);
+        default: return run_stream<X, F ? 32 : 48, F ? 2 : 4, 4, PAIR>(in, s);
+    }
+}
+
+__global__ __launch_bounds__(256) void clear_f4(Counters c) { clear_counters(c.p, c.n); }
 
 template <class T>
 hipError_t expand(const uint8_t* q, const uint8_t* scale, int64_t values, void* w, Counters clear,
@@ -303,15 +423,29 @@ hipError_t expand(const uint8_t* q, const uint8_t* scale, int64_t values, void* 
     return hipGetLastError();
 }
 
+// cleared: an earlier launch of the call has set the counters of `part` to zero
+template <class T>
+hipError_t streamed(const void* x, const uint8_t* W, const uint8_t* W_scale, const void* res,
+                    int64_t T_, int n, int k, int dtype, void* y, void* part, bool cleared,
+                    hipStream_t s) {
+    if (!cleared) {
+        const Counters c = f4_counters(part, T_, n, k, dtype);
+        if (c.n) {
+            ProfileScope prof("clear_f4", s);
+            ELB_LAUNCH(clear_f4, dim3(1), dim3(256), 0, s, c);
+        }
+    }
+    ProfileScope prof("linear_f4", s);
+    stream<T, false>({(const T*)x, W, W_scale, (const T*)res, (T*)y, T_, n, k, 1, nullptr, nullptr,
+                      {nullptr, 0}}, part, s);
+    return hipGetLastError();
+}
+
 template <class T>
 hipError_t linear(const void* x, const uint8_t* W, const uint8_t* W_scale, const void* res,
-                  int64_t T_, int n, int k, int dtype, void* y, void* w, void* part,
-                  hipStream_t s) {
-    if (f4_streams(T_, dtype)) {
-        ProfileScope prof("linear_f4", s);
-        stream<T, false>({(const T*)x, W, W_scale, (const T*)res, (T*)y, T_, n, k}, s);
-        return hipGetLastError();
-    }
+                  int64_t T_, int n, int k, int dtype, void* y, void* w, void* part, hipStream_t s) {
+    if (f4_streams(T_, n, k, false, dtype))
+        return streamed<T>(x, W, W_scale, res, T_, n, k, dtype, y, part, false, s);
     const int64_t kt = ((int64_t)k * sizeof(T) + 127) / 128;
     if (hipError_t e = expand<T>(W, W_scale, (int64_t)n * k, w,
                                  halves_counters((char*)part, T_, n, kt, sizeof(T) == 4), s))
@@ -323,13 +457,14 @@ template <class T>
 hipError_t block(const void* x, const uint8_t* Wgu, const uint8_t* gu_scale, const uint8_t* Wd,
                  const uint8_t* d_scale, const void* res, int64_t T_, int d, int m, int dtype,
                  void* h, void* wgu, void* wd, void* part, void* y, hipStream_t s) {
-    if (f4_streams(T_, dtype)) {
+    if (f4_streams(T_, d, m, true, dtype)) {
         {
             ProfileScope prof("gate_up_f4", s);
-            stream<T, true>({(const T*)x, Wgu, gu_scale, nullptr, (T*)h, T_, m, d}, s);
+            stream<T, true>({(const T*)x, Wgu, gu_scale, nullptr, (T*)h, T_, m, d, 1, nullptr, nullptr,
+                             f4_counters(part, T_, d, m, dtype)}, nullptr, s);
             if (hipError_t e = hipGetLastError()) return e;
         }
-        return linear<T>(h, Wd, d_scale, res, T_, d, m, dtype, y, nullptr, nullptr, s);
+        return streamed<T>(h, Wd, d_scale, res, T_, d, m, dtype, y, part, true, s);
     }
     if (hipError_t e = expand<T>(Wgu, gu_scale, (int64_t)2 * m * d, wgu, {}, s)) return e;
     if (hipError_t e = expand<T>(Wd, d_scale, (int64_t)m * d, wd, {}, s)) return e;
@@ -338,7 +473,46 @@ hipError_t block(const void* x, const uint8_t* Wgu, const uint8_t* gu_scale, con
 
 }  // namespace
 
-bool f4_streams(int64_t T, int) { return T <= 64; }
+// Whether the product [T, k] x [n, k] (block: the dense block of width n and h of width k) streams its
+// weights, by estimated time, or converts them first (the bytes at 5 TB/s, then the best dense form, and
+// 6 us for the launch and the dense form's reads of what was just written).  us, streamed / converted, bf16: 256 tokens, 2048 to 8192 21 / 34, 384 29 / 35, 768 56 / 50;
+// 8192 to 2048 384 23 / 38, 512 40 / 36; fp32: 512 tokens, 8192 to 2048 109 / 179, 2048 to 16384 261 / 293.
+// Up to kStreamedAlways tokens nothing is converted, so that small batches need no scratch for it.
+bool f4_streams(int64_t T, int n, int k, bool block, int dtype) {
+    const bool f32 = dtype == ELB_F32;
+    if (T <= kStreamedAlways) return true;
+    if (T > kMostStreamed) return false;
+    auto converted = [&](int64_t rows, int64_t deep) {
+        const int64_t e = f32 ? 4 : 2, kt = (deep * e + 127) / 128;
+        const FormId f = pick_form(T, rows, kt, f32, true);
+        const FormCost& c = (f32 ? kFormCostsF32 : kFormCosts)[f];
+        return 6.0f + (float)(rows * deep) * (0.53f + (float)e) / 5e6f +
+               form_time(c, form_tiles(c, T, rows), kt, f != kTiles);
+    };
+    float s = stream_form(T, n, k, false, f32).time, c = converted(n, k);
+    if (block) {
+        s += stream_form(T, k, n, true, f32).time;
+        c += converted(2 * (int64_t)k, n);
+    }
+    return s < c;
+}
+
+// partial sums of a product whose contraction blocks share, and behind them a counter a tile
+size_t f4_part_bytes(int64_t T, int n, int k, int dtype) {
+    const StreamForm f = stream_form(T, n, k, false, dtype == ELB_F32);
+    if (f.shares == 1) return 0;
+    return (size_t)stream_tiles(f, T, n) *
+           ((size_t)f.shares * ((f.tm + 15) / 16 * 16) * 16 * f.nf * 4 + 4);
+}
+size_t f4_part_reserve(int64_t T, int n, int k, int dtype) {
+    // the form is the same within every 16 tokens but the first, whose halves differ
+    size_t most = T > 0 ? f4_part_bytes(T < 8 ? T : 8, n, k, dtype) : 0;
+    for (int64_t t = 16; t < T + 16 && t <= kMostStreamed; t += 16) {
+        const size_t b = f4_part_bytes(t < T ? t : T, n, k, dtype);
+        most = b > most ? b : most;
+    }
+    return most;
+}
 
 hipError_t launch_quantize_f4(const void* x, int64_t rows, int d, int dtype, uint8_t* q,
                               uint8_t* scale, hipStream_t s) {

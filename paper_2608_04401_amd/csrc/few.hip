@@ -84,6 +84,8 @@ __global__ __launch_bounds__(64 * kUpWaves) void few_up(FewIn in, XTable xt) {
     __shared__ __attribute__((aligned(1024))) char sm[kUpWaves * SLOT];
     __shared__ float logits[RW][16 * 65];
     __shared__ Slots slots;
+    __shared__ float sorted[kUpWaves][64];
+    __shared__ int order[kUpWaves][64];
     __shared__ int sk[16], sids[16 * kLaneMaxK];
     __shared__ float sw[16 * kLaneMaxK];
     const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, hq = lane >> 4;
@@ -160,27 +162,66 @@ __global__ __launch_bounds__(64 * kUpWaves) void few_up(FewIn in, XTable xt) {
     }
     ELB_WAIT_VMCNT(0);  // the last copies, before their LDS is used again; and x
     __syncthreads();
-    if (tid < 256) {  // whole waves: 16 lanes a token
-        const int t = tid >> 4, sl = tid & 15;
-        float l4[4];
+    if (T <= kUpWaves) {
+        // a wave per token, a lane per expert: its logit, and its rank by counting the (key, id)
+        // pairs before it, in the order of route_token_x16's network (one token: 3.5 us from here to
+        // the selection, 4.5 by that; with two tokens a wave 5.8 and 4.6)
+        if (wave < T) {
+            const int t = wave;
+            float l = -INFINITY;
+            if (lane < N) {
+                l = logits[0][t * 65 + lane];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int n = 4 * sl + i;
-            l4[i] = -INFINITY;
-            if (n < N) {
-                float v = logits[0][t * 65 + n];
-#pragma unroll
-                for (int q = 1; q < RW; ++q) v += logits[q][t * 65 + n];
-                l4[i] = v;
+                for (int q = 1; q < RW; ++q) l += logits[q][t * 65 + lane];
             }
-        }
+            const float key = N == 64 ? order_key(l) : order_key_any(l);
+            const int image = ord_flip32(__float_as_int(key));
+            const int64_t mine = ((int64_t)image << 32) | (uint32_t)(63 - lane);
+            int rank = 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) logits[0][t * 65 + 4 * sl + i] = l4[i];
+            for (int j = 0; j < 64; ++j) {
+                const int64_t other =
+                    ((int64_t)__builtin_amdgcn_readlane(image, j) << 32) | (uint32_t)(63 - j);
+                rank += other > mine;
+            }
+            sorted[t][rank] = key;
+            order[t][rank] = lane;
+        }
+        __syncthreads();
+        if (tid < 16 * kUpWaves) {  // whole waves: 16 lanes a token
+            const int t = tid >> 4, sl = tid & 15;
+            float key[4];
+            int id[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                key[i] = sorted[t][4 * sl + i];
+                id[i] = order[t][4 * sl + i];
+            }
+            route_sorted_x16<KMAX>(key, id, N, K, in.eps, in.mode, in.renorm, xt, t, t < T, sk,
+                                   sids, sw);
+        }
+    } else {
+        const int t = tid >> 4, sl = tid & 15;
+        if (tid < 256) {  // whole waves: 16 lanes a token
+            float l4[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int n = 4 * sl + i;
+                l4[i] = -INFINITY;
+                if (n < N) {
+                    l4[i] = logits[0][t * 65 + n];
+#pragma unroll
+                    for (int q = 1; q < RW; ++q) l4[i] += logits[q][t * 65 + n];
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) logits[0][t * 65 + 4 * sl + i] = l4[i];
+        }
+        __syncthreads();
+        if (tid < 256)
+            route_token_x16<KMAX>(logits[0] + t * 65, N, K, in.eps, in.mode, in.renorm, xt, t, t < T,
+                                  sk, sids, sw);
     }
-    __syncthreads();
-    if (tid < 256)
-        route_token_x16<KMAX>(logits[0] + (tid >> 4) * 65, N, K, in.eps, in.mode, in.renorm, xt,
-                              tid >> 4, (tid >> 4) < T, sk, sids, sw);
     __syncthreads();
     if (blockIdx.x == 0) {
         if (tid < T * K) {
@@ -196,13 +237,14 @@ __global__ __launch_bounds__(64 * kUpWaves) void few_up(FewIn in, XTable xt) {
     const int64_t w_bytes = W::row_bytes((int64_t)2 * m * d);  // of an expert
     int task = blockIdx.x;
     B b;
+    typename B::Pending pending = {};
     auto begin = [&](int t) {
         const int u = t / per_e;
         const int e = __builtin_amdgcn_readfirstlane(slots.list[u]);
         b.init((const char*)in.gate_up + e * w_bytes,
                W::SCALES ? in.gu_scale + (int64_t)e * 2 * m * (d / 32) : nullptr,
-               32 * (t - u * per_e), 32, m, d, lane);
-        if (u0 < u1) b.issue(u0, u1, lds, slot, lane);
+               32 * (t - u * per_e), 32, m, 2 * (int64_t)m, d, lane);
+        if (u0 < u1) b.issue(u0, u1, lds, slot, lane, pending);
         return e;
     };
     int e = task < tasks ? begin(task) : 0;
@@ -221,6 +263,7 @@ __global__ __launch_bounds__(64 * kUpWaves) void few_up(FewIn in, XTable xt) {
                 }
             }
             ELB_WAIT_VMCNT(0);
+            b.settle(pending, slot, lane);
             asm volatile("" ::: "memory");
             typename W::Half w[4][2];
 #pragma unroll
@@ -228,7 +271,7 @@ __global__ __launch_bounds__(64 * kUpWaves) void few_up(FewIn in, XTable xt) {
 #pragma unroll
                 for (int f = 0; f < 4; ++f) W::read(w[f][h], slot, 64, f, h, l16, hq);
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the unit is free again
-            if (u + 1 < u1) b.issue(u + 1, u1, lds, slot, lane);
+            if (u + 1 < u1) b.issue(u + 1, u1, lds, slot, lane, pending);
             else if (next < tasks) next_e = begin(next);
             __builtin_amdgcn_sched_barrier(0);
             auto multiply = [&](int at) {  // at: the unit's first operand in x
@@ -307,17 +350,18 @@ __global__ __launch_bounds__(64 * kDownWaves) void few_down(FewIn in) {
     const int v0 = units * share / in.shares + wave, v1 = units * (share + 1) / in.shares;
     const int64_t w_bytes = W::row_bytes((int64_t)d * m);
     B b0;
-    b0.init(in.down, in.d_scale, 64 * tile, 64, 0, m, lane);
+    b0.init(in.down, in.d_scale, 64 * tile, 64, 0, d, m, lane);
     // rows of h: chunk lane % 8 of row lane / 8, in each of the unit's k-tiles of 64
     const uint64_t hb = (uint64_t)in.h;
     const u32x4_t hr = {uniform((uint32_t)hb), uniform((uint32_t)(hb >> 32)) & 0xffffu,
                         uniform((uint32_t)(T * in.K) * (uint32_t)m * 2u), 0x00027000u};
     const int chunk = kc_swz(lane >> 3, lane & 7) * 16;
+    typename B::Pending pending = {};
     auto issue = [&](int v, int pass) {
         const int u = v / per, unit = v - u * per;
         const int e = __builtin_amdgcn_readfirstlane(slots.list[u]);
         b0.moved(e * w_bytes, W::SCALES ? (int64_t)e * d * (m / 32) : 0)
-            .issue(unit, per, lds + AB, slot + AB, lane);
+            .issue(unit, per, lds + AB, slot + AB, lane, pending);
         const int rank = 8 * pass + (lane >> 3);
         const int at = rank < __popc(slots.tokens[e]) ? slots.row[e][rank] : -1;
 #pragma unroll
@@ -337,6 +381,7 @@ __global__ __launch_bounds__(64 * kDownWaves) void few_down(FewIn in) {
     int pass = 0, e = v0 < v1 ? issue(v0, 0) : 0;
     for (int v = v0; v < v1;) {
         ELB_WAIT_VMCNT(0);
+        b0.settle(pending, slot + AB, lane);
         asm volatile("" ::: "memory");
         const uint32_t tokens = slots.tokens[e];
         const int rank = __popc(tokens & ((1u << l16) - 1)) - 8 * pass;
@@ -464,9 +509,7 @@ hipError_t launch_moe_few(const void* x, const void* Wr, const void* Wgu, const 
                    (bf16_t*)h, (bf16_t*)y, k, ids, w, part, count, few_shares(d)};
     const bool dma = aligned16(x, Wr) && aligned16(Wgu, Wd);
     if (!gu_scale) return dma ? few<WBf16, true>(in, cus, s) : few<WBf16, false>(in, cus, s);
-    return dma && f4_copies(Wgu, gu_scale, d) && f4_copies(Wd, d_scale, m)
-               ? few<WF4, true>(in, cus, s)
-               : few<WF4, false>(in, cus, s);
+    return dma ? few<WF4, true>(in, cus, s) : few<WF4, false>(in, cus, s);
 }
 
 }  // namespace elb

@@ -447,66 +447,19 @@ __device__ __forceinline__ float row_last(float v) {
     return __int_as_float(__builtin_amdgcn_ds_swizzle(__float_as_int(v), 0x10 | (0x0f << 5)));
 }
 
-// row: the token's 64 logits in LDS, -inf past the N experts; every lane of the group calls this
-// (valid: the token exists; only valid groups write)
+// The token's sorted keys and their experts, ranks 4 sl .. 4 sl + 3 in lane sl of the group; every lane
+// of the group calls this (valid: the token exists; only valid groups write).
 // lds_hist (optional): a 64-bin LDS histogram to which each selected expert of a valid token
 // adds one (the dispatch's per-group counts).
 template <int KMAX>
-__device__ __forceinline__ void route_token_x16(float* row, int N, int K, float eps,
-                                                int mode, int renorm, const XTable& xt, int64_t t,
-                                                bool valid, int* __restrict__ kout,
-                                                int* __restrict__ ids,
-                                                float* __restrict__ wout,
-                                                int* lds_hist = nullptr) {
+__device__ __forceinline__ void route_sorted_x16(const float (&key)[4], const int (&id)[4], int N,
+                                                 int K, float eps, int mode, int renorm,
+                                                 const XTable& xt, int64_t t, bool valid,
+                                                 int* __restrict__ kout, int* __restrict__ ids,
+                                                 float* __restrict__ wout,
+                                                 int* lds_hist = nullptr) {
     constexpr int NP = 64;
     const int sl = threadIdx.x & 15;
-    // ---- (key, id) pairs of positions 4 sl + i: key image high, 63 - id low ----
-    int64_t v[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int c = 4 * sl + i;
-        const float f = N == NP ? order_key(row[c]) : order_key_any(row[c]);
-        v[i] = ((int64_t)ord_flip32(__float_as_int(f)) << 32) |
-               (uint32_t)(NP - 1 - c);
-    }
-    // ---- bitonic sort, descending: position p = 4 sl + i ----
-#pragma unroll
-    for (int k = 2; k <= NP; k <<= 1) {
-#pragma unroll
-        for (int j = k >> 1; j >= 1; j >>= 1) {
-            if (j >= 4) {
-                const int m = j >> 2;  // partner lane sl ^ m, same i
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const int p = 4 * sl + i;
-                    const int64_t w = xor16_64(v[i], m);
-                    const bool desc = (p & k) == 0 || k == NP;
-                    const bool lower = (p & j) == 0;
-                    const bool take_max = lower == desc;
-                    const bool gt = w > v[i];
-                    v[i] = (gt == take_max) ? w : v[i];
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if (i & j) continue;
-                    const int p = 4 * sl + i;
-                    const bool desc = (p & k) == 0 || k == NP;
-                    const int64_t a = v[i], b = v[i | j];
-                    const bool sw = desc ? (b > a) : (a > b);
-                    v[i] = sw ? b : a;
-                    v[i | j] = sw ? a : b;
-                }
-            }
-        }
-    }
-    float key[4];
-    int id[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        key[i] = __int_as_float(ord_flip32((int)(v[i] >> 32)));
-        id[i] = NP - 1 - (int)(uint32_t)v[i];
-    }
     const float nl = neg_scaled(row_first(key[0]));
     float u[4];
 #pragma unroll
@@ -581,6 +534,67 @@ __device__ __forceinline__ void route_token_x16(float* row, int N, int K, float 
         }
         if (lds_hist && r < k) atomicAdd(&lds_hist[id[i]], 1);
     }
+}
+
+// row: the token's 64 logits in LDS, -inf past the N experts; the rest as route_sorted_x16
+template <int KMAX>
+__device__ __forceinline__ void route_token_x16(float* row, int N, int K, float eps,
+                                                int mode, int renorm, const XTable& xt, int64_t t,
+                                                bool valid, int* __restrict__ kout,
+                                                int* __restrict__ ids,
+                                                float* __restrict__ wout,
+                                                int* lds_hist = nullptr) {
+    constexpr int NP = 64;
+    const int sl = threadIdx.x & 15;
+    // ---- (key, id) pairs of positions 4 sl + i: key image high, 63 - id low ----
+    int64_t v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int c = 4 * sl + i;
+        const float f = N == NP ? order_key(row[c]) : order_key_any(row[c]);
+        v[i] = ((int64_t)ord_flip32(__float_as_int(f)) << 32) |
+               (uint32_t)(NP - 1 - c);
+    }
+    // ---- bitonic sort, descending: position p = 4 sl + i ----
+#pragma unroll
+    for (int k = 2; k <= NP; k <<= 1) {
+#pragma unroll
+        for (int j = k >> 1; j >= 1; j >>= 1) {
+            if (j >= 4) {
+                const int m = j >> 2;  // partner lane sl ^ m, same i
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int p = 4 * sl + i;
+                    const int64_t w = xor16_64(v[i], m);
+                    const bool desc = (p & k) == 0 || k == NP;
+                    const bool lower = (p & j) == 0;
+                    const bool take_max = lower == desc;
+                    const bool gt = w > v[i];
+                    v[i] = (gt == take_max) ? w : v[i];
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (i & j) continue;
+                    const int p = 4 * sl + i;
+                    const bool desc = (p & k) == 0 || k == NP;
+                    const int64_t a = v[i], b = v[i | j];
+                    const bool sw = desc ? (b > a) : (a > b);
+                    v[i] = sw ? b : a;
+                    v[i | j] = sw ? a : b;
+                }
+            }
+        }
+    }
+    float key[4];
+    int id[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        key[i] = __int_as_float(ord_flip32((int)(v[i] >> 32)));
+        id[i] = NP - 1 - (int)(uint32_t)v[i];
+    }
+    route_sorted_x16<KMAX>(key, id, N, K, eps, mode, renorm, xt, t, valid, kout, ids, wout,
+                           lds_hist);
 }
 
 // ---- the router's summation order ----

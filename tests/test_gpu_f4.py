@@ -191,16 +191,21 @@ def test_in_place_unaligned_and_what_lies_around(T, dtype):
     assert torch.equal(z, y)
 
 
-def test_a_row_alone():
-    """A streamed row's bits do not depend on how many rows go with it, up to a tile of 16."""
-    g = gen(9)
-    W, s = codes(g, 528, 1056)
-    x = normal(g, 16, 1056, dtype=BF16)
-    y = B.elb_linear_f4(x, W, s)
-    for r in (0, 7, 15):
-        one = B.elb_linear_f4(x[r:r + 1].contiguous(), W, s)
-        torch.cuda.synchronize()
-        assert torch.equal(one[0], y[r])
+def test_every_form():
+    """Batches and widths that take every tile of the streamed products, whole and in shares, and the
+    converted ones; rows whose scales lie on no word boundary among them."""
+    for k, n in ((2048, 2048), (8192, 1024), (4096, 528), (1120, 4112), (512, 16400)):
+        g = gen(k + n)
+        W, s = codes(g, n, k)
+        w = R.from_f4(W, s)
+        for T in (1, 9, 17, 33, 49, 65, 130, 300, 700):
+            for dtype in (BF16, F32):
+                x = normal(g, T, k, dtype=dtype)
+                y = B.elb_linear_f4(x, W, s)
+                again = B.elb_linear_f4(x, W, s)
+                torch.cuda.synchronize()
+                within(y, *R.linear(x, w), label="T %d k %d n %d" % (T, k, n))
+                assert torch.equal(y, again)
 
 
 def test_no_tokens():

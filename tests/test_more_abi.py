@@ -177,10 +177,11 @@ def test_f4_arguments():
         assert block(**{name: None}) == INVALID
     for name in ("x", "q", "scale"):
         assert quantize(**{name: None}) == INVALID
-    for T in (4, 100):
+    for T in (4, 3000):
         assert block(T=T, ws=None) == WORKSPACE and block(T=T, ws=ODD) == WORKSPACE
         assert block(T=T, nb=15) == WORKSPACE
-    assert linear(T=100, ws=None) == WORKSPACE and linear(T=100, nb=15) == WORKSPACE
+    # that many tokens take converted weights, in scratch
+    assert linear(T=3000, ws=None) == WORKSPACE and linear(T=3000, nb=15) == WORKSPACE
     none = {"x": None, "y": None}
     assert linear(T=0, ws=None, **none) == OK and block(T=0, ws=None, **none) == OK
     assert quantize(T=0, x=None) == OK
