@@ -218,7 +218,6 @@ hipError_t launch_gate_up_i8(const void* x, int dtype, const int8_t* w, const fl
 
 // norms around a block (norm.hip).  The backward's scratch: norm_backward_blocks(T, d) x 3 x d floats
 // for the sums over rows
-constexpr int kNormBlocks = 256;
 int norm_backward_blocks(int64_t T, int d);
 hipError_t launch_norm_forward(const elb_norm& p, void* sum, void* normed, float* r_post,
                                float* r_pre, hipStream_t s);

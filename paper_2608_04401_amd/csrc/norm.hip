@@ -71,6 +71,32 @@ __device__ __forceinline__ float row_rstd(const float (&v)[KEEP][8], int d, floa
     return 0x1p-64f / sqrtf(a / (float)d);
 }
 
+// Eight values as loaded, in as many registers as they have words (dense.h's Eight lets the compiler
+// split bf16 pairs, twice the registers: the backward of 4096 rows of 2048 then spilled, 60 us)
+template <class T>
+struct Packed;
+template <>
+struct Packed<bf16_t> {
+    u32x4_t v;
+    __device__ __forceinline__ void load(const bf16_t* p) {
+        v = *reinterpret_cast<const u32x4_any_t*>(p);
+    }
+    __device__ __forceinline__ float operator[](int i) const {
+        return __uint_as_float(i & 1 ? v[i / 2] & 0xffff0000u : v[i / 2] << 16);
+    }
+};
+template <>
+struct Packed<float> {
+    f32x4_t a, b;
+    __device__ __forceinline__ void load(const float* p) {
+        a = *reinterpret_cast<const f32x4_any_t*>(p);
+        b = *reinterpret_cast<const f32x4_any_t*>(p + 4);
+    }
+    __device__ __forceinline__ float operator[](int i) const { return i < 4 ? a[i] : b[i - 4]; }
+};
+__device__ __forceinline__ float one_value(const bf16_t* p) { return bf16_to_f32(*p); }
+__device__ __forceinline__ float one_value(const float* p) { return *p; }
+
 template <class T>
 struct NormIn {
     const T *residual, *block, *gate, *w_post, *w_pre;
@@ -81,7 +107,7 @@ struct NormIn {
 
 // the gate of row `row` at the eight columns from c on
 template <class T>
-__device__ __forceinline__ void load_gate(const NormIn<T>& in, int64_t row, int c, Eight<T>& g) {
+__device__ __forceinline__ void load_gate(const NormIn<T>& in, int64_t row, int c, Packed<T>& g) {
     if (in.gate_kind == ELB_GATE_CHANNEL) g.load(in.gate + c);
     else if (in.gate_kind == ELB_GATE_FULL) g.load(in.gate + row * in.d + c);
 }
@@ -96,7 +122,7 @@ __global__ __launch_bounds__(N == 64 ? 256 : N) void norm_forward(NormIn<T> in, 
     const int tid = threadIdx.x % N, d = in.d;
     const int64_t row = (int64_t)dense_block_number() * RPB + threadIdx.x / N;
     if (row >= in.rows) return;  // a whole wave, or a whole block
-    Eight<T> x[KEEP], b[KEEP], g[KEEP], wp[KEEP], wn[KEEP];
+    Packed<T> x[KEEP], b[KEEP], g[KEEP], wp[KEEP], wn[KEEP];
 #pragma unroll
     for (int i = 0; i < KEEP; ++i) {
         const int c = (i * N + tid) * 8;
@@ -109,11 +135,7 @@ __global__ __launch_bounds__(N == 64 ? 256 : N) void norm_forward(NormIn<T> in, 
     }
     float v[KEEP][8];
     float scale = in.beta;
-    if (in.gate_kind == ELB_GATE_TOKEN) {
-        Eight<T> one;
-        one.v[0] = in.gate[row];
-        scale *= one[0];
-    }
+    if (in.gate_kind == ELB_GATE_TOKEN) scale *= one_value(in.gate + row);
     if (in.block) {
 #pragma unroll
         for (int i = 0; i < KEEP; ++i)
@@ -173,8 +195,16 @@ struct NormGradIn {
     int cols;     // bit j: sum j is wanted
 };
 
-// RPB rows of N threads at a time, the block's rows RPB gridDim apart; the sums over the rows stay
-// in registers until the end, then the RPB of the block are added in LDS, in order.
+// What a row brings, as loaded
+template <class T, int KEEP>
+struct RowIn {
+    Packed<T> ds[KEEP], dn[KEEP], s[KEEP], b[KEEP], g[KEEP];
+    float rs, rb, gt;  // r_pre, r_post (1 without w_post), a gate per token
+};
+
+// RPB rows of N threads at a time, the block's rows RPB gridDim apart.  The sums over the rows stay in
+// registers until the end, then the RPB of the block are added in LDS, in order.  (The next rows loaded
+// ahead of the present ones' work take registers that the block's other rows need: 39 us for 25.)
 template <class T, int N, int KEEP, int RPB>
 __global__ __launch_bounds__(N* RPB) void norm_backward(NormIn<T> in, NormGradIn<T> gr) {
     constexpr int W = N * RPB / 64;
@@ -190,42 +220,54 @@ __global__ __launch_bounds__(N* RPB) void norm_backward(NormIn<T> in, NormGradIn
 #pragma unroll
             for (int q = 0; q < 8; ++q) acc[j][i][q] = 0.0f;
     const bool branch = gr.dblock || gr.dgate || (gr.cols & 6);
-    int ph = 0;
-    for (int64_t r0 = (int64_t)blockIdx.x * RPB; r0 < in.rows; r0 += (int64_t)gridDim.x * RPB) {
-        const int64_t row = r0 + sub;
+    const bool gated = in.gate_kind == ELB_GATE_CHANNEL || in.gate_kind == ELB_GATE_FULL;
+    typedef RowIn<T, KEEP> R;
+    auto load = [&](int64_t row, R& r) {
         const bool live = row < in.rows;
-        Eight<T> ds[KEEP], dn[KEEP], s[KEEP], b[KEEP], g[KEEP];
+        r.rs = r.rb = r.gt = 1.0f;
+        if (live && gr.dn) r.rs = gr.r_pre[row];
+        if (live && branch && in.w_post) r.rb = gr.r_post[row];
+        if (live && branch && in.gate_kind == ELB_GATE_TOKEN) r.gt = one_value(in.gate + row);
 #pragma unroll
         for (int i = 0; i < KEEP; ++i) {
             const int c = (i * N + tid) * 8;
-            ds[i] = dn[i] = s[i] = b[i] = g[i] = Eight<T>{};
+            r.ds[i] = r.dn[i] = r.s[i] = r.b[i] = r.g[i] = Packed<T>{};
             if (c >= d || !live) continue;
             const int64_t o = row * d + c;
-            if (gr.ds) ds[i].load(gr.ds + o);
+            if (gr.ds) r.ds[i].load(gr.ds + o);
             if (gr.dn) {
-                dn[i].load(gr.dn + o);
-                s[i].load(gr.sum + o);
+                r.dn[i].load(gr.dn + o);
+                r.s[i].load(gr.sum + o);
             }
             if (branch) {
-                b[i].load(in.block + o);
-                load_gate(in, row, c, g[i]);
+                r.b[i].load(in.block + o);
+                if (in.gate_kind == ELB_GATE_FULL) r.g[i].load(in.gate + o);
             }
         }
+    };
+    const int64_t step = (int64_t)gridDim.x * RPB;
+    int ph = 0;
+    R r;
+    for (int64_t r0 = (int64_t)blockIdx.x * RPB; r0 < in.rows; r0 += step) {
+        const int64_t row = r0 + sub;
+        const bool live = row < in.rows;
+        load(row, r);
+        // the norms' weights and a gate per channel are the same for every row, but are read again, from
+        // L1, rather than held in registers
+        asm volatile("" ::: "memory");
         float S[KEEP][8];
-        float rs = 0.0f, a = 0.0f;
+        float a = 0.0f;
         if (gr.dn) {
-            rs = live ? gr.r_pre[row] : 0.0f;
 #pragma unroll
             for (int i = 0; i < KEEP; ++i) {
-                const int c = (i * N + tid) * 8;
-                Eight<T> w = Eight<T>{};
-                if (c < d) w.load(in.w_pre + c);
+                Packed<T> wn = {};
+                if ((i * N + tid) * 8 < d) wn.load(in.w_pre + (i * N + tid) * 8);
 #pragma unroll
                 for (int q = 0; q < 8; ++q) {
-                    const float t = w[q] * dn[i][q], sh_ = s[i][q] * rs;
+                    const float t = wn[q] * r.dn[i][q], hat = r.s[i][q] * r.rs;
                     S[i][q] = t;
-                    a = fmaf(t, sh_, a);
-                    acc[0][i][q] = fmaf(dn[i][q], sh_, acc[0][i][q]);
+                    a = fmaf(t, hat, a);
+                    acc[0][i][q] = fmaf(r.dn[i][q], hat, acc[0][i][q]);
                 }
             }
             a = row_sum<N>(a, sh[0][ph]) * inv_d;
@@ -236,40 +278,34 @@ __global__ __launch_bounds__(N* RPB) void norm_backward(NormIn<T> in, NormGradIn
             float o[8];
 #pragma unroll
             for (int q = 0; q < 8; ++q) {
-                float t = ds[i][q];
-                if (gr.dn) t += rs * fmaf(-s[i][q] * rs, a, S[i][q]);
+                float t = r.ds[i][q];
+                if (gr.dn) t += r.rs * fmaf(-r.s[i][q] * r.rs, a, S[i][q]);
                 S[i][q] = t;
                 o[q] = in.alpha * t;
             }
             if (gr.dres && live && c < d) store8(gr.dres + row * d + c, o);
         }
         if (branch) {
-            float gt = 1.0f;
-            if (in.gate_kind == ELB_GATE_TOKEN && live) {
-                Eight<T> one;
-                one.v[0] = in.gate[row];
-                gt = one[0];
-            }
-            const float rb = in.w_post ? (live ? gr.r_post[row] : 0.0f) : 1.0f;
-            const bool gated = in.gate_kind == ELB_GATE_CHANNEL || in.gate_kind == ELB_GATE_FULL;
             float m = 0.0f, tok = 0.0f;
             float u[KEEP][8];
 #pragma unroll
             for (int i = 0; i < KEEP; ++i) {
                 const int c = (i * N + tid) * 8;
-                Eight<T> w = Eight<T>{};
-                if (in.w_post && c < d) w.load(in.w_post + c);
+                Packed<T> wp = {}, gc = {};
+                if (c < d && in.w_post) wp.load(in.w_post + c);
+                if (c < d && in.gate_kind == ELB_GATE_CHANNEL) gc.load(in.gate + c);
                 float o[8];
 #pragma unroll
                 for (int q = 0; q < 8; ++q) {
-                    const float bh = b[i][q] * rb, qv = in.beta * S[i][q];
-                    const float dp = qv * (gated ? g[i][q] : gt);
-                    const float p = in.w_post ? w[q] * bh : bh;
-                    o[q] = qv * p;
+                    const float bh = r.b[i][q] * r.rb, qv = in.beta * S[i][q];
+                    const float g = !gated ? r.gt : in.gate_kind == ELB_GATE_FULL ? r.g[i][q]
+                                                                                  : gc[q];
+                    const float dp = qv * g, w = in.w_post ? wp[q] : 1.0f;
+                    o[q] = qv * (w * bh);
                     tok += o[q];
                     acc[2][i][q] += o[q];
                     acc[1][i][q] = fmaf(dp, bh, acc[1][i][q]);
-                    u[i][q] = in.w_post ? w[q] * dp : dp;
+                    u[i][q] = w * dp;
                     m = fmaf(u[i][q], bh, m);
                 }
                 if (gr.dgate && in.gate_kind == ELB_GATE_FULL && live && c < d)
@@ -291,7 +327,7 @@ __global__ __launch_bounds__(N* RPB) void norm_backward(NormIn<T> in, NormGradIn
                     float o[8];
 #pragma unroll
                     for (int q = 0; q < 8; ++q)
-                        o[q] = in.w_post ? rb * fmaf(-b[i][q] * rb, m, u[i][q]) : u[i][q];
+                        o[q] = in.w_post ? r.rb * fmaf(-r.b[i][q] * r.rb, m, u[i][q]) : u[i][q];
                     store8(gr.dblock + row * d + c, o);
                 }
             }
@@ -311,14 +347,13 @@ __global__ __launch_bounds__(N* RPB) void norm_backward(NormIn<T> in, NormGradIn
 #pragma unroll
                 for (int q = 0; q < 8; ++q) cols[(sub * 8 + q) * N + tid] = acc[j][i][q];
                 __syncthreads();
-                // 8 N sums by N RPB threads
-#pragma unroll
+                // 8 N sums by N RPB threads, in the order of the columns
                 for (int k = threadIdx.x; k < 8 * N; k += N * RPB) {
-                    const int col = (i * N + k % N) * 8 + k / N;
-                    float t = cols[k];
+                    const int at = k % 8 * N + k / 8;
+                    float t = cols[at];
 #pragma unroll
-                    for (int r = 1; r < RPB; ++r) t += cols[r * 8 * N + k];
-                    if (col < d) out[col] = t;
+                    for (int p = 1; p < RPB; ++p) t += cols[p * 8 * N + at];
+                    if (i * N * 8 + k < d) out[i * N * 8 + k] = t;
                 }
             } else if (c < d) {
                 store8(out + c, acc[j][i]);
@@ -327,12 +362,12 @@ __global__ __launch_bounds__(N* RPB) void norm_backward(NormIn<T> in, NormGradIn
     }
 }
 
-// The sums over all blocks of the backward: 64 columns a block, four threads a column, each of which
-// adds a quarter of the blocks in order.
+// The sums over all blocks of the backward: 64 columns a block, sixteen threads a column, each of which
+// adds a sixteenth of the blocks in order.
 template <class T>
-__global__ __launch_bounds__(256) void norm_columns(const float* __restrict__ part, int blocks,
-                                                    int d, T* o0, T* o1, T* o2) {
-    __shared__ float sh[4][64];
+__global__ __launch_bounds__(1024) void norm_columns(const float* __restrict__ part, int blocks,
+                                                     int d, T* o0, T* o1, T* o2) {
+    __shared__ float sh[16][64];
     const int j = blockIdx.y, l = threadIdx.x & 63, w = threadIdx.x >> 6;
     const int c = blockIdx.x * 64 + l;
     T* const out = j == 0 ? o0 : j == 1 ? o1 : o2;
@@ -340,14 +375,16 @@ __global__ __launch_bounds__(256) void norm_columns(const float* __restrict__ pa
     float t = 0.0f;
     if (c < d) {
         const float* const p = part + (int64_t)j * d + c;
-        const int b1 = blocks * (w + 1) / 4;
-#pragma unroll 8
-        for (int b = blocks * w / 4; b < b1; ++b) t += p[(int64_t)b * 3 * d];
+        const int b1 = blocks * (w + 1) / 16;
+#pragma unroll 16
+        for (int b = blocks * w / 16; b < b1; ++b) t += p[(int64_t)b * 3 * d];
     }
     sh[w][l] = t;
     __syncthreads();
     if (w == 0 && c < d) {
-        t = ((sh[0][l] + sh[1][l]) + sh[2][l]) + sh[3][l];
+        t = sh[0][l];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) t += sh[i][l];
         if constexpr (sizeof(T) == 2) out[c] = f32_to_bf16(t);
         else out[c] = t;
     }
@@ -370,6 +407,7 @@ hipError_t forward_of(const elb_norm& p, void* sum, void* normed, float* r_post,
                        p.residual_scale, p.block_scale};
     T *const o = (T*)sum, *const n = (T*)normed;
     if (p.d <= 512) forward<T, 64, 1>(in, p.eps, o, n, r_post, r_pre, s);
+    else if (p.d <= 1024) forward<T, 128, 1>(in, p.eps, o, n, r_post, r_pre, s);
     else if (p.d <= 2048) forward<T, 256, 1>(in, p.eps, o, n, r_post, r_pre, s);
     else if (p.d <= 4096) forward<T, 256, 2>(in, p.eps, o, n, r_post, r_pre, s);
     else if (p.d <= 8192) forward<T, 1024, 1>(in, p.eps, o, n, r_post, r_pre, s);
@@ -377,8 +415,18 @@ hipError_t forward_of(const elb_norm& p, void* sum, void* normed, float* r_post,
     return hipGetLastError();
 }
 
-// rows that a block of the backward works on at a time
-int rows_at_once(int d) { return d <= 512 ? 16 : d <= 1024 ? 8 : d <= 2048 ? 4 : d <= 4096 ? 2 : 1; }
+// The backward's shape by row length: as many threads a row as leave a thread eight values, and rows to
+// fill a block of 512 threads.  (4096 rows of 2048, bf16, one row a block 29.4 us with the sums over the
+// blocks, two 28.1, four 29.4; 16384 rows 88, 86, 93; 2048 rows of 4096, 256 threads and sixteen values 43.)
+struct BackShape {
+    int threads, rows;
+};
+BackShape back_shape(int d) {
+    if (d <= 512) return {64, 8};
+    if (d <= 1024) return {128, 4};
+    if (d <= 2048) return {256, 2};
+    return {d <= 4096 ? 512 : 1024, 1};
+}
 
 template <class T, int N, int KEEP, int RPB>
 void backward(const NormIn<T>& in, const NormGradIn<T>& g, int blocks, hipStream_t s) {
@@ -399,26 +447,28 @@ hipError_t backward_of(const elb_norm& p, const void* ds, const void* dn, const 
     const int blocks = norm_backward_blocks(p.T, p.d);
     if (blocks) {
         ProfileScope prof("norm_backward", s);
-        if (p.d <= 512) backward<T, 64, 1, 16>(in, g, blocks, s);
-        else if (p.d <= 1024) backward<T, 128, 1, 8>(in, g, blocks, s);
-        else if (p.d <= 2048) backward<T, 256, 1, 4>(in, g, blocks, s);
-        else if (p.d <= 4096) backward<T, 256, 2, 2>(in, g, blocks, s);
+        if (p.d <= 512) backward<T, 64, 1, 8>(in, g, blocks, s);
+        else if (p.d <= 1024) backward<T, 128, 1, 4>(in, g, blocks, s);
+        else if (p.d <= 2048) backward<T, 256, 1, 2>(in, g, blocks, s);
+        else if (p.d <= 4096) backward<T, 512, 1, 1>(in, g, blocks, s);
         else if (p.d <= 8192) backward<T, 1024, 1, 1>(in, g, blocks, s);
         else backward<T, 1024, 2, 1>(in, g, blocks, s);
         if (hipError_t e = hipGetLastError()) return e;
     }
     if (!cols) return hipSuccess;
     ProfileScope prof("norm_columns", s);
-    ELB_LAUNCH(norm_columns<T>, dim3((p.d + 63) / 64, 3), dim3(256), 0, s, (const float*)part,
+    ELB_LAUNCH(norm_columns<T>, dim3((p.d + 63) / 64, 3), dim3(1024), 0, s, (const float*)part,
                blocks, p.d, (T*)dw_pre, (T*)dw_post, channel ? (T*)dgate : nullptr);
     return hipGetLastError();
 }
 
 }  // namespace
 
+// at most 1024 threads a compute unit
 int norm_backward_blocks(int64_t T, int d) {
-    const int64_t n = (T + rows_at_once(d) - 1) / rows_at_once(d);
-    return (int)(n < kNormBlocks ? n : kNormBlocks);
+    const BackShape b = back_shape(d);
+    const int64_t n = (T + b.rows - 1) / b.rows, most = 256 * 1024 / (b.threads * b.rows);
+    return (int)(n < most ? n : most);
 }
 
 hipError_t launch_norm_forward(const elb_norm& p, void* sum, void* normed, float* r_post,
