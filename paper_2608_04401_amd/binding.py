@@ -727,24 +727,38 @@ def elb_linear_f4_workspace_bytes(T: int, n: int, k: int, dtype: int) -> int:
     return int(lib().elb_linear_f4_workspace_bytes(T, n, k, dtype))
 
 
+def _scratch(nbytes: int, device, stream: int):
+    """(address, size) of a call's scratch; none where it needs none."""
+    if nbytes == 0:
+        return None, 0
+    ws = workspace(nbytes, device, stream)
+    return ws.data_ptr(), ws.numel()
+
+
 def elb_linear_f4(x, W, W_scale, residual=None, out=None) -> torch.Tensor:
     """y [T, n] = [residual +] x [T, k] times 4-bit W [n, k / 2] with W_scale [n, k / 32]
     (elb_quantize_f4).  out may be residual, not x."""
     T, k = _matrix("x", x)
     n = _matrix("W", W)[0]
+    dtype = x.dtype
     dt = _dtype_code(x)
     dev = _device(x)
-    _want("x", x, (T, k), x.dtype, dev)
+    _want("x", x, (T, k), dtype, dev)
     _want("W", W, (n, k // 2), torch.uint8, dev)
     _want("W_scale", W_scale, (n, k // 32), torch.uint8, dev)
-    _want("residual", residual, (T, n), x.dtype, dev)
-    _want("out", out, (T, n), x.dtype, dev)
-    y = torch.empty((T, n), dtype=x.dtype, device=x.device) if out is None else out
+    if residual is not None:
+        _want("residual", residual, (T, n), dtype, dev)
+    if out is None:
+        y = x.new_empty((T, n))
+    else:
+        _want("out", out, (T, n), dtype, dev)
+        y = out
     stream = _stream()
-    ws = workspace(elb_linear_f4_workspace_bytes(T, n, k, dt), x.device, stream)
-    _check("elb_linear_f4", lib().elb_linear_f4(
-        _ptr(x), _ptr(W), _ptr(W_scale), _ptr(residual), T, n, k, dt, _ptr(y), _ptr(ws),
-        ws.numel(), stream))
+    ws, nb = _scratch(elb_linear_f4_workspace_bytes(T, n, k, dt), x.device, stream)
+    status = lib().elb_linear_f4(x.data_ptr(), W.data_ptr(), W_scale.data_ptr(), _ptr(residual), T, n,
+                                 k, dt, y.data_ptr(), ws, nb, stream)
+    if status:
+        _check("elb_linear_f4", status)
     return y
 
 

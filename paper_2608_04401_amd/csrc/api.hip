@@ -263,11 +263,12 @@ int check_f4(int64_t T, int n, const char* nn, int k, const char* kn) {
                     kn, k);
     return ELB_OK;
 }
-// sub-buffers of the workspace of a projection (m = 0) or of the block (n = d, k = m); `most` as above
+// sub-buffers of the workspace of a projection (m = 0) or of the block (n = d, k = m)
 struct F4Layout {
     size_t h, wgu, wd, part, total;
 };
-F4Layout f4_layout(int64_t T, int n, int k, int m, int dtype, bool most) {
+// streams, part: as a plan has them, or to reserve for any batch of up to T tokens
+F4Layout f4_layout(int64_t T, int n, int k, int m, int dtype, bool streams, size_t part, bool most) {
     F4Layout L{};
     size_t o = 0;
     auto take = [&](size_t bytes) {
@@ -277,17 +278,26 @@ F4Layout f4_layout(int64_t T, int n, int k, int m, int dtype, bool most) {
     };
     const size_t e = esize(dtype);
     L.h = take((size_t)T * m * e);
-    if (most ? T <= kStreamedAlways : f4_streams(T, n, k, m > 0, dtype)) {
-        L.part = take(most ? f4_part_reserve(T, n, k, dtype) : f4_part_bytes(T, n, k, dtype));
+    if (streams) {
+        L.part = take(part);
         L.total = o;
         return L;
     }
-    const size_t streamed = most ? o + align_up(f4_part_reserve(T, n, k, dtype)) : 0;
+    const size_t streamed = o + align_up(part);
     L.wgu = take((size_t)2 * m * n * e);
     L.wd = take((size_t)n * k * e);
     L.part = take(ffn_halves_bytes(T, n, k, dtype, most));
     L.total = std::max(o, streamed);
     return L;
+}
+F4Layout f4_layout(const F4Plan& p, int64_t T, int n, int k, int m, int dtype) {
+    return f4_layout(T, n, k, m, dtype, p.streams, p.part, false);
+}
+// the most that a batch of up to T tokens needs (it never falls as T grows)
+size_t f4_reserve(int64_t T, int n, int k, int m, int dtype) {
+    return f4_layout(T, n, k, m, dtype, T <= kStreamedAlways,
+                     f4_part_reserve(T, n, k, dtype == ELB_F32), true)
+        .total;
 }
 
 // ---- the static scratch of the allocation-free entry point ----
@@ -1016,7 +1026,7 @@ int elb_quantize_f4(const void* x, int64_t rows, int32_t d, int32_t dtype, uint8
 
 size_t elb_linear_f4_workspace_bytes(int64_t T, int32_t n, int32_t k, int32_t dtype) {
     if (T < 0 || n < 1 || k < 1 || (dtype != ELB_F32 && dtype != ELB_BF16)) return 0;
-    return f4_layout(T, n, k, 0, dtype, true).total;
+    return f4_reserve(T, n, k, 0, dtype);
 }
 
 int elb_linear_f4(const void* x, const uint8_t* W, const uint8_t* W_scale, const void* residual,
@@ -1027,7 +1037,8 @@ int elb_linear_f4(const void* x, const uint8_t* W, const uint8_t* W_scale, const
     if (int rc = check_f4(T, n, "n", k, "k")) return rc;
     if (T == 0) return ELB_OK;
     if (!x || !W || !W_scale || !y) return fail(ELB_ERR_INVALID_ARG, "NULL tensor pointer");
-    const F4Layout L = f4_layout(T, n, k, 0, dtype, false);
+    const F4Plan p = f4_plan(T, n, k, false, dtype == ELB_F32);
+    const F4Layout L = f4_layout(p, T, n, k, 0, dtype);
     if (L.total)
         if (int rc = check_workspace(workspace, workspace_bytes, L.total)) return rc;
     const int64_t e = esize(dtype);
@@ -1037,7 +1048,7 @@ int elb_linear_f4(const void* x, const uint8_t* W, const uint8_t* W_scale, const
         return rc;
     if (int rc = check_residual(out, residual)) return rc;
     char* const ws = (char*)workspace;
-    return hip_status(launch_linear_f4(x, W, W_scale, residual, T, n, k, dtype, y,
+    return hip_status(launch_linear_f4(p, x, W, W_scale, residual, T, n, k, dtype, y,
                                        L.total ? ws + L.wd : nullptr,
                                        L.total ? ws + L.part : nullptr, (hipStream_t)stream),
                       "linear_f4");
@@ -1045,7 +1056,7 @@ int elb_linear_f4(const void* x, const uint8_t* W, const uint8_t* W_scale, const
 
 size_t elb_ffn_f4_workspace_bytes(int64_t T, int32_t d, int32_t m, int32_t dtype) {
     if (T < 0 || d < 1 || m < 1 || (dtype != ELB_F32 && dtype != ELB_BF16)) return 0;
-    return f4_layout(T, d, m, m, dtype, true).total;
+    return f4_reserve(T, d, m, m, dtype);
 }
 
 int elb_ffn_forward_f4(const void* x, const uint8_t* W_gate_up, const uint8_t* gate_up_scale,
@@ -1059,7 +1070,8 @@ int elb_ffn_forward_f4(const void* x, const uint8_t* W_gate_up, const uint8_t* g
     if (T == 0) return ELB_OK;
     if (!x || !W_gate_up || !gate_up_scale || !W_down || !down_scale || !y)
         return fail(ELB_ERR_INVALID_ARG, "NULL tensor pointer");
-    const F4Layout L = f4_layout(T, d, m, m, dtype, false);
+    const F4Plan p = f4_plan(T, d, m, true, dtype == ELB_F32);
+    const F4Layout L = f4_layout(p, T, d, m, m, dtype);
     if (int rc = check_workspace(workspace, workspace_bytes, L.total)) return rc;
     const Span out{"y", y, T * d * (int64_t)esize(dtype)};
     if (int rc = check_apart(out, {{"W_gate_up", W_gate_up, (int64_t)m * d},
@@ -1069,7 +1081,7 @@ int elb_ffn_forward_f4(const void* x, const uint8_t* W_gate_up, const uint8_t* g
         return rc;
     if (int rc = check_residual(out, residual)) return rc;
     char* const ws = (char*)workspace;
-    return hip_status(launch_ffn_f4(x, W_gate_up, gate_up_scale, W_down, down_scale, residual, T, d,
+    return hip_status(launch_ffn_f4(p, x, W_gate_up, gate_up_scale, W_down, down_scale, residual, T, d,
                                     m, dtype, ws + L.h, ws + L.wgu, ws + L.wd, ws + L.part, y,
                                     (hipStream_t)stream),
                       "ffn_forward_f4");

@@ -6,6 +6,7 @@
 #include <stdint.h>
 
 #include "elbow_moe.h"
+#include "f4_forms.h"
 
 namespace elb {
 
@@ -226,21 +227,14 @@ hipError_t launch_norm_backward(const elb_norm& p, const void* ds, const void* d
                                 void* dgate, void* dw_post, void* dw_pre, void* part,
                                 hipStream_t s);
 
-// 4-bit weights (f4.hip).  Few tokens stream them as they are; for more they are converted to
-// dtype in scratch (w; wgu and wd) and multiplied by the dense forms, with `part` of ffn_halves_bytes.
-// part: null, or f4_part_bytes, where they are streamed
-constexpr int64_t kStreamedAlways = 64, kMostStreamed = 2048;
-bool f4_streams(int64_t T, int n, int k, bool block, int dtype);
-// scratch of the streamed product [T, k] x [n, k] for blocks that share a tile, and the most of it that
-// any batch of up to T tokens needs
-size_t f4_part_bytes(int64_t T, int n, int k, int dtype);
-size_t f4_part_reserve(int64_t T, int n, int k, int dtype);
+// 4-bit weights (f4.hip), as planned (f4_plan).  Streamed: part, its bytes; converted: scratch for the
+// weights in dtype (w; wgu and wd) and part of ffn_halves_bytes
 hipError_t launch_quantize_f4(const void* x, int64_t rows, int d, int dtype, uint8_t* q,
                               uint8_t* scale, hipStream_t s);
-hipError_t launch_linear_f4(const void* x, const uint8_t* W, const uint8_t* W_scale,
+hipError_t launch_linear_f4(const F4Plan& p, const void* x, const uint8_t* W, const uint8_t* W_scale,
                             const void* res, int64_t T, int n, int k, int dtype, void* y, void* w,
                             void* part, hipStream_t s);
-hipError_t launch_ffn_f4(const void* x, const uint8_t* Wgu, const uint8_t* gu_scale,
+hipError_t launch_ffn_f4(const F4Plan& p, const void* x, const uint8_t* Wgu, const uint8_t* gu_scale,
                          const uint8_t* Wd, const uint8_t* d_scale, const void* res, int64_t T,
                          int d, int m, int dtype, void* h, void* wgu, void* wd, void* part, void* y,
                          hipStream_t s);

@@ -129,9 +129,6 @@ struct Tok<float> {
     }
 };
 
-constexpr int kMostShares = 16, kMostSharing = 512;  // shares of a tile, blocks of tiles with shares
-Counters f4_counters(void* part, int64_t T, int n, int k, int dtype);
-
 template <class X>
 struct StreamIn {
     const X* x;
@@ -331,73 +328,16 @@ void run_stream(const StreamIn<X>& in, hipStream_t s) {
         ELB_LAUNCH((stream_f4<X, TM, NF, NW, PAIR, false>), grid, dim3(64 * NW), 0, s, in);
 }
 
-// The tile and waves of a streamed product, in how many shares its contraction is cut, and its
-// estimated time: start + rounds (round + iter * units of a wave) [+ share] us, with rounds of `per` blocks
-// on each of 256 compute units.  The constants are least-squares fits over 1 to 768 tokens and weights
-// of 1024 to 16384 rows of 512 to 8192 values; over these the choice is 0.4 % slower than the best form
-// on average and 18 % at worst (fp32, 96 tokens, 512 to 4096 11.2 for 9.6).  bf16, us, at both sides: 48
-// tokens, 8192 to 2048: 48 x 32 tiles in four shares 10.5, whole 15.7, 48 x 64 in four 12.0, whole 20.5;
-// 2048 to 16384: 48 x 64 9.0, 32 x 64 12.9, 48 x 32 11.0.
-struct StreamForm {
-    int tm, nf, nw, per;
-    float start, round, iter, share;
-    int shares = 1;
-    float time = 0;
-};
-constexpr StreamForm kStreamBf16[] = {
-    {8, 1, 16, 1, 1.2f, 1.75f, 1.6f, 3.5f},   {8, 2, 8, 2, 1.7f, 1.7f, 1.0f, 2.7f},
-    {8, 4, 8, 1, 1.5f, 2.0f, 1.72f, 2.8f},    {16, 1, 8, 1, 1.63f, 1.29f, 0.92f, 3.2f},
-    {16, 2, 8, 1, 1.44f, 1.58f, 1.19f, 2.8f}, {16, 4, 8, 1, 1.5f, 1.8f, 1.88f, 2.9f},
-    {32, 2, 4, 1, 1.34f, 1.35f, 1.24f, 3.5f}, {32, 4, 4, 1, 0.93f, 2.15f, 1.82f, 4.0f},
-    {48, 2, 4, 1, 1.07f, 1.7f, 1.58f, 4.2f},  {48, 4, 4, 1, 0.57f, 2.6f, 2.29f, 4.9f}};
-constexpr StreamForm kStreamF32[] = {
-    {8, 1, 8, 1, 1.39f, 1.4f, 2.22f, 3.5f},   {8, 2, 8, 1, 1.22f, 1.7f, 2.71f, 2.8f},
-    {8, 4, 8, 1, 1.65f, 1.65f, 3.7f, 2.8f},   {16, 1, 4, 1, 1.5f, 1.45f, 1.46f, 3.3f},
-    {16, 2, 4, 1, 1.22f, 1.48f, 2.1f, 3.3f},  {16, 4, 4, 1, 0.84f, 2.11f, 2.76f, 3.4f},
-    {32, 2, 4, 1, 1.14f, 1.35f, 3.42f, 3.6f}};
-int stream_tiles(const StreamForm& f, int64_t T, int rows) {
-    return (rows + 16 * f.nf - 1) / (16 * f.nf) * (int)((T + f.tm - 1) / f.tm);
-}
-StreamForm stream_form(int64_t T, int cols, int k, bool pair, bool f32) {
-    const int rows = pair ? 2 * cols : cols, units = (k + 255) / 256;
-    StreamForm best = kStreamBf16[0];
-    bool any = false;
-    const StreamForm* const table = f32 ? kStreamF32 : kStreamBf16;
-    const int n = f32 ? (int)(sizeof(kStreamF32) / sizeof(kStreamF32[0]))
-                      : (int)(sizeof(kStreamBf16) / sizeof(kStreamBf16[0]));
-    for (int i = 0; i < n; ++i) {
-        StreamForm f = table[i];
-        // (the fits hold there; gate and up rows are two fragments at least)
-        if ((f.tm == 8 && T > 8) || (f.tm == 16 && T > 16 && !f32) || (pair && f.nf == 1)) continue;
-        const int64_t tiles = stream_tiles(f, T, rows);
-        for (f.shares = 1; f.shares <= (pair ? 1 : kMostShares); f.shares *= 2) {
-            if (f.shares > 1 && (f.shares * f.nw > units || tiles * f.shares > kMostSharing)) break;
-            const int64_t blocks = tiles * f.shares, rounds = (blocks + 256 * f.per - 1) / (256 * f.per);
-            const int its = (units + f.nw * f.shares - 1) / (f.nw * f.shares);
-            f.time = f.start + (float)rounds * (f.round + f.iter * (float)its) +
-                     (f.shares > 1 ? f.share : 0.0f);
-            if (!any || f.time < best.time) best = f, any = true;
-        }
-    }
-    return best;
-}
-
 // the counters of a shared product's scratch, or none
-Counters f4_counters(void* part, int64_t T, int n, int k, int dtype) {
-    const StreamForm f = stream_form(T, n, k, false, dtype == ELB_F32);
-    if (!part || f.shares == 1) return {nullptr, 0};
-    const int tiles = stream_tiles(f, T, n);
-    const size_t each = (size_t)f.shares * ((f.tm + 15) / 16 * 16) * 16 * f.nf * 4;
-    return {reinterpret_cast<uint32_t*>((char*)part + tiles * each), tiles};
+Counters f4_counters(const F4Plan& p, void* part) {
+    if (!p.part) return {nullptr, 0};
+    return {reinterpret_cast<uint32_t*>((char*)part + p.sums()), p.tiles};
 }
 
 template <class X, bool PAIR>
-void stream(StreamIn<X> in, void* part, hipStream_t s) {
+void stream(StreamIn<X> in, const StreamForm& f, hipStream_t s) {
     constexpr bool F = sizeof(X) == 4;
-    const StreamForm f = stream_form(in.T, in.cols, in.k, PAIR, F);
     in.shares = f.shares;
-    in.part = (float*)part;
-    in.count = f4_counters(part, in.T, in.cols, in.k, F ? ELB_F32 : ELB_BF16).p;
     switch (f.tm * 8 + f.nf) {
         case 8 * 8 + 1: return run_stream<X, 8, PAIR ? 2 : 1, F ? 8 : 16, PAIR>(in, s);
         case 8 * 8 + 2: return run_stream<X, 8, 2, 8, PAIR>(in, s);
@@ -423,29 +363,27 @@ hipError_t expand(const uint8_t* q, const uint8_t* scale, int64_t values, void* 
     return hipGetLastError();
 }
 
-// cleared: an earlier launch of the call has set the counters of `part` to zero
+// y = [res +] x W^T, streamed; cleared: an earlier launch of the call has set the counters to zero
 template <class T>
-hipError_t streamed(const void* x, const uint8_t* W, const uint8_t* W_scale, const void* res,
-                    int64_t T_, int n, int k, int dtype, void* y, void* part, bool cleared,
+hipError_t streamed(const F4Plan& p, const void* x, const uint8_t* W, const uint8_t* W_scale,
+                    const void* res, int64_t T_, int n, int k, void* y, void* part, bool cleared,
                     hipStream_t s) {
-    if (!cleared) {
-        const Counters c = f4_counters(part, T_, n, k, dtype);
-        if (c.n) {
-            ProfileScope prof("clear_f4", s);
-            ELB_LAUNCH(clear_f4, dim3(1), dim3(256), 0, s, c);
-        }
+    const Counters c = f4_counters(p, part);
+    if (c.n && !cleared) {
+        ProfileScope prof("clear_f4", s);
+        ELB_LAUNCH(clear_f4, dim3(1), dim3(256), 0, s, c);
     }
     ProfileScope prof("linear_f4", s);
-    stream<T, false>({(const T*)x, W, W_scale, (const T*)res, (T*)y, T_, n, k, 1, nullptr, nullptr,
-                      {nullptr, 0}}, part, s);
+    stream<T, false>({(const T*)x, W, W_scale, (const T*)res, (T*)y, T_, n, k, 1, (float*)part, c.p,
+                      {nullptr, 0}}, p.form, s);
     return hipGetLastError();
 }
 
 template <class T>
-hipError_t linear(const void* x, const uint8_t* W, const uint8_t* W_scale, const void* res,
-                  int64_t T_, int n, int k, int dtype, void* y, void* w, void* part, hipStream_t s) {
-    if (f4_streams(T_, n, k, false, dtype))
-        return streamed<T>(x, W, W_scale, res, T_, n, k, dtype, y, part, false, s);
+hipError_t linear(const F4Plan& p, const void* x, const uint8_t* W, const uint8_t* W_scale,
+                  const void* res, int64_t T_, int n, int k, int dtype, void* y, void* w, void* part,
+                  hipStream_t s) {
+    if (p.streams) return streamed<T>(p, x, W, W_scale, res, T_, n, k, y, part, false, s);
     const int64_t kt = ((int64_t)k * sizeof(T) + 127) / 128;
     if (hipError_t e = expand<T>(W, W_scale, (int64_t)n * k, w,
                                  halves_counters((char*)part, T_, n, kt, sizeof(T) == 4), s))
@@ -454,17 +392,17 @@ hipError_t linear(const void* x, const uint8_t* W, const uint8_t* W_scale, const
 }
 
 template <class T>
-hipError_t block(const void* x, const uint8_t* Wgu, const uint8_t* gu_scale, const uint8_t* Wd,
-                 const uint8_t* d_scale, const void* res, int64_t T_, int d, int m, int dtype,
-                 void* h, void* wgu, void* wd, void* part, void* y, hipStream_t s) {
-    if (f4_streams(T_, d, m, true, dtype)) {
+hipError_t block(const F4Plan& p, const void* x, const uint8_t* Wgu, const uint8_t* gu_scale,
+                 const uint8_t* Wd, const uint8_t* d_scale, const void* res, int64_t T_, int d, int m,
+                 int dtype, void* h, void* wgu, void* wd, void* part, void* y, hipStream_t s) {
+    if (p.streams) {
         {
             ProfileScope prof("gate_up_f4", s);
             stream<T, true>({(const T*)x, Wgu, gu_scale, nullptr, (T*)h, T_, m, d, 1, nullptr, nullptr,
-                             f4_counters(part, T_, d, m, dtype)}, nullptr, s);
+                             f4_counters(p, part)}, p.up, s);
             if (hipError_t e = hipGetLastError()) return e;
         }
-        return streamed<T>(h, Wd, d_scale, res, T_, d, m, dtype, y, part, true, s);
+        return streamed<T>(p, h, Wd, d_scale, res, T_, d, m, y, part, true, s);
     }
     if (hipError_t e = expand<T>(Wgu, gu_scale, (int64_t)2 * m * d, wgu, {}, s)) return e;
     if (hipError_t e = expand<T>(Wd, d_scale, (int64_t)m * d, wd, {}, s)) return e;
@@ -472,47 +410,6 @@ hipError_t block(const void* x, const uint8_t* Wgu, const uint8_t* gu_scale, con
 }
 
 }  // namespace
-
-// Whether the product [T, k] x [n, k] (block: the dense block of width n and h of width k) streams its
-// weights, by estimated time, or converts them first (the bytes at 5 TB/s, then the best dense form, and
-// 6 us for the launch and the dense form's reads of what was just written).  us, streamed / converted, bf16: 256 tokens, 2048 to 8192 21 / 34, 384 29 / 35, 768 56 / 50;
-// 8192 to 2048 384 23 / 38, 512 40 / 36; fp32: 512 tokens, 8192 to 2048 109 / 179, 2048 to 16384 261 / 293.
-// Up to kStreamedAlways tokens nothing is converted, so that small batches need no scratch for it.
-bool f4_streams(int64_t T, int n, int k, bool block, int dtype) {
-    const bool f32 = dtype == ELB_F32;
-    if (T <= kStreamedAlways) return true;
-    if (T > kMostStreamed) return false;
-    auto converted = [&](int64_t rows, int64_t deep) {
-        const int64_t e = f32 ? 4 : 2, kt = (deep * e + 127) / 128;
-        const FormId f = pick_form(T, rows, kt, f32, true);
-        const FormCost& c = (f32 ? kFormCostsF32 : kFormCosts)[f];
-        return 6.0f + (float)(rows * deep) * (0.53f + (float)e) / 5e6f +
-               form_time(c, form_tiles(c, T, rows), kt, f != kTiles);
-    };
-    float s = stream_form(T, n, k, false, f32).time, c = converted(n, k);
-    if (block) {
-        s += stream_form(T, k, n, true, f32).time;
-        c += converted(2 * (int64_t)k, n);
-    }
-    return s < c;
-}
-
-// partial sums of a product whose contraction blocks share, and behind them a counter a tile
-size_t f4_part_bytes(int64_t T, int n, int k, int dtype) {
-    const StreamForm f = stream_form(T, n, k, false, dtype == ELB_F32);
-    if (f.shares == 1) return 0;
-    return (size_t)stream_tiles(f, T, n) *
-           ((size_t)f.shares * ((f.tm + 15) / 16 * 16) * 16 * f.nf * 4 + 4);
-}
-size_t f4_part_reserve(int64_t T, int n, int k, int dtype) {
-    // the form is the same within every 16 tokens but the first, whose halves differ
-    size_t most = T > 0 ? f4_part_bytes(T < 8 ? T : 8, n, k, dtype) : 0;
-    for (int64_t t = 16; t < T + 16 && t <= kMostStreamed; t += 16) {
-        const size_t b = f4_part_bytes(t < T ? t : T, n, k, dtype);
-        most = b > most ? b : most;
-    }
-    return most;
-}
 
 hipError_t launch_quantize_f4(const void* x, int64_t rows, int d, int dtype, uint8_t* q,
                               uint8_t* scale, hipStream_t s) {
@@ -527,19 +424,19 @@ hipError_t launch_quantize_f4(const void* x, int64_t rows, int d, int dtype, uin
     return hipGetLastError();
 }
 
-hipError_t launch_linear_f4(const void* x, const uint8_t* W, const uint8_t* W_scale,
+hipError_t launch_linear_f4(const F4Plan& p, const void* x, const uint8_t* W, const uint8_t* W_scale,
                             const void* res, int64_t T, int n, int k, int dtype, void* y, void* w,
                             void* part, hipStream_t s) {
-    return (dtype == ELB_BF16 ? linear<bf16_t> : linear<float>)(x, W, W_scale, res, T, n, k, dtype, y,
-                                                                w, part, s);
+    return (dtype == ELB_BF16 ? linear<bf16_t> : linear<float>)(p, x, W, W_scale, res, T, n, k, dtype,
+                                                                y, w, part, s);
 }
 
-hipError_t launch_ffn_f4(const void* x, const uint8_t* Wgu, const uint8_t* gu_scale,
+hipError_t launch_ffn_f4(const F4Plan& p, const void* x, const uint8_t* Wgu, const uint8_t* gu_scale,
                          const uint8_t* Wd, const uint8_t* d_scale, const void* res, int64_t T,
                          int d, int m, int dtype, void* h, void* wgu, void* wd, void* part, void* y,
                          hipStream_t s) {
-    return (dtype == ELB_BF16 ? block<bf16_t> : block<float>)(x, Wgu, gu_scale, Wd, d_scale, res, T, d,
-                                                              m, dtype, h, wgu, wd, part, y, s);
+    return (dtype == ELB_BF16 ? block<bf16_t> : block<float>)(p, x, Wgu, gu_scale, Wd, d_scale, res, T,
+                                                              d, m, dtype, h, wgu, wd, part, y, s);
 }
 
 }  // namespace elb

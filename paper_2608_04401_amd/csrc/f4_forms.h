@@ -1,0 +1,122 @@
+// Which form a product with 4-bit weights takes (f4.hip): streamed as they are, and with which tile, or
+// converted for the dense forms.  Usable from host code without HIP (for tests).
+#pragma once
+
+#include "forms.h"
+
+namespace elb {
+
+constexpr int kMostShares = 16, kMostSharing = 512;  // shares of a tile, blocks of tiles with shares
+constexpr int64_t kStreamedAlways = 64, kMostStreamed = 2048;
+
+// The tile and waves of a streamed product, in how many shares its contraction is cut, and its
+// estimated time: start + rounds (round + iter * units of a wave) [+ share] us, with rounds of `per` blocks
+// on each of 256 compute units.  The constants are least-squares fits over 1 to 768 tokens and weights
+// of 1024 to 16384 rows of 512 to 8192 values; over these the choice is 0.4 % slower than the best form
+// on average and 18 % at worst (fp32, 96 tokens, 512 to 4096 11.2 for 9.6).  bf16, us, at both sides: 48
+// tokens, 8192 to 2048: 48 x 32 tiles in four shares 10.5, whole 15.7, 48 x 64 in four 12.0, whole 20.5;
+// 2048 to 16384: 48 x 64 9.0, 32 x 64 12.9, 48 x 32 11.0.
+struct StreamForm {
+    int tm, nf, nw, per;
+    float start, round, iter, share;
+    int shares = 1;
+    float time = 0;
+};
+constexpr StreamForm kStreamBf16[] = {
+    {8, 1, 16, 1, 1.2f, 1.75f, 1.6f, 3.5f},   {8, 2, 8, 2, 1.7f, 1.7f, 1.0f, 2.7f},
+    {8, 4, 8, 1, 1.5f, 2.0f, 1.72f, 2.8f},    {16, 1, 8, 1, 1.63f, 1.29f, 0.92f, 3.2f},
+    {16, 2, 8, 1, 1.44f, 1.58f, 1.19f, 2.8f}, {16, 4, 8, 1, 1.5f, 1.8f, 1.88f, 2.9f},
+    {32, 2, 4, 1, 1.34f, 1.35f, 1.24f, 3.5f}, {32, 4, 4, 1, 0.93f, 2.15f, 1.82f, 4.0f},
+    {48, 2, 4, 1, 1.07f, 1.7f, 1.58f, 4.2f},  {48, 4, 4, 1, 0.57f, 2.6f, 2.29f, 4.9f}};
+constexpr StreamForm kStreamF32[] = {
+    {8, 1, 8, 1, 1.39f, 1.4f, 2.22f, 3.5f},   {8, 2, 8, 1, 1.22f, 1.7f, 2.71f, 2.8f},
+    {8, 4, 8, 1, 1.65f, 1.65f, 3.7f, 2.8f},   {16, 1, 4, 1, 1.5f, 1.45f, 1.46f, 3.3f},
+    {16, 2, 4, 1, 1.22f, 1.48f, 2.1f, 3.3f},  {16, 4, 4, 1, 0.84f, 2.11f, 2.76f, 3.4f},
+    {32, 2, 4, 1, 1.14f, 1.35f, 3.42f, 3.6f}};
+inline int stream_tiles(const StreamForm& f, int64_t T, int rows) {
+    return (rows + 16 * f.nf - 1) / (16 * f.nf) * (int)((T + f.tm - 1) / f.tm);
+}
+inline StreamForm stream_form(int64_t T, int cols, int k, bool pair, bool f32) {
+    const int rows = pair ? 2 * cols : cols, units = (k + 255) / 256;
+    const StreamForm* const table = f32 ? kStreamF32 : kStreamBf16;
+    const int n = f32 ? (int)(sizeof(kStreamF32) / sizeof(kStreamF32[0]))
+                      : (int)(sizeof(kStreamBf16) / sizeof(kStreamBf16[0]));
+    const StreamForm* best = nullptr;
+    int best_shares = 1;
+    float least = 0;
+    for (int i = 0; i < n; ++i) {
+        const StreamForm& f = table[i];
+        // (where the fits hold; gate and up rows are two fragments at least)
+        if ((f.tm == 8 && T > 8) || (f.tm == 16 && T > 16 && !f32) || (f.tm > 16 && T <= 16) ||
+            (pair && f.nf == 1))
+            continue;
+        const int tiles = stream_tiles(f, T, rows);
+        for (int z = 1; z <= (pair ? 1 : kMostShares); z *= 2) {
+            if (z > 1 && (z * f.nw > units || tiles > kMostSharing / z)) break;
+            const unsigned per = 256u * f.per, rounds = ((unsigned)tiles * z + per - 1) / per;
+            const unsigned its = (unsigned)(units + f.nw * z - 1) / (unsigned)(f.nw * z);
+            const float t = f.start + (float)rounds * (f.round + f.iter * (float)its) +
+                            (z > 1 ? f.share : 0.0f);
+            if (!best || t < least) best = &f, best_shares = z, least = t;
+        }
+    }
+    StreamForm f = *best;
+    f.shares = best_shares;
+    f.time = least;
+    return f;
+}
+
+// Whether the product [T, k] x [n, k] (block: the dense block of width n and h of width k) streams its
+// weights, by estimated time, or converts them first (the bytes at 5 TB/s, then the best dense form, and
+// 6 us for the launch and the dense form's reads of what was just written).  us, streamed / converted, bf16: 256 tokens, 2048 to 8192 21 / 34, 384 29 / 35, 768 56 / 50;
+// 8192 to 2048 384 23 / 38, 512 40 / 36; fp32: 512 tokens, 8192 to 2048 109 / 179, 2048 to 16384 261 / 293.
+// Up to kStreamedAlways tokens nothing is converted, so that small batches need no scratch for it.
+struct F4Plan {
+    bool streams;
+    StreamForm up, form;  // of a block's gate and up rows; of the projection, or of its down rows
+    int tiles;            // of `form`
+    size_t part;          // bytes of its partial sums and, behind them, a counter a tile (shares > 1)
+    size_t sums() const { return part - 4 * (size_t)tiles; }
+};
+inline size_t f4_part(const StreamForm& f, int tiles) {
+    if (f.shares == 1) return 0;
+    return (size_t)tiles * ((size_t)f.shares * ((f.tm + 15) / 16 * 16) * 16 * f.nf * 4 + 4);
+}
+inline F4Plan f4_plan(int64_t T, int n, int k, bool block, bool f32) {
+    F4Plan p{T <= kStreamedAlways, {}, {}, 0, 0};
+    if (T > kMostStreamed) return p;
+    p.form = stream_form(T, n, k, false, f32);
+    if (block) p.up = stream_form(T, k, n, true, f32);
+    auto converted = [&](int64_t rows, int64_t deep) {
+        const int64_t e = f32 ? 4 : 2, kt = (deep * e + 127) / 128;
+        const FormId f = pick_form(T, rows, kt, f32, true);
+        const FormCost& c = (f32 ? kFormCostsF32 : kFormCosts)[f];
+        return 6.0f + (float)(rows * deep) * (0.53f + (float)e) / 5e6f +
+               form_time(c, form_tiles(c, T, rows), kt, f != kTiles);
+    };
+    if (!p.streams) {
+        const float c = converted(n, k) + (block ? converted(2 * (int64_t)k, n) : 0.0f);
+        p.streams = p.form.time + (block ? p.up.time : 0.0f) < c;
+    }
+    if (p.streams) {
+        p.tiles = stream_tiles(p.form, T, n);
+        p.part = f4_part(p.form, p.tiles);
+    }
+    return p;
+}
+
+// The most partial sums that any batch of up to T tokens needs: the form is the same within every 16
+// tokens but the first, whose halves differ.
+inline size_t f4_part_reserve(int64_t T, int n, int k, bool f32) {
+    size_t most = 0;
+    for (int64_t t = 8; t < T + 16 && t <= kMostStreamed; t += t == 8 ? 8 : 16) {
+        const int64_t at = t < T ? t : T;
+        if (at < 1) break;
+        const StreamForm f = stream_form(at, n, k, false, f32);
+        const size_t b = f4_part(f, stream_tiles(f, at, n));
+        most = b > most ? b : most;
+    }
+    return most;
+}
+
+}  // namespace elb

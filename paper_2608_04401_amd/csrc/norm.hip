@@ -112,6 +112,9 @@ __device__ __forceinline__ void load_gate(const NormIn<T>& in, int64_t row, int 
     else if (in.gate_kind == ELB_GATE_FULL) g.load(in.gate + row * in.d + c);
 }
 
+// Blocks of up to 1024 threads in rows of 2^20: a launch dimension stays below 2^32 threads.
+constexpr int kNormRow = 1 << 20;
+
 // N threads a row (a wave, or the whole block), eight columns of each of KEEP groups a thread.
 template <class T, int N, int KEEP>
 __global__ __launch_bounds__(N == 64 ? 256 : N) void norm_forward(NormIn<T> in, float eps,
@@ -120,7 +123,7 @@ __global__ __launch_bounds__(N == 64 ? 256 : N) void norm_forward(NormIn<T> in, 
     __shared__ float sh[2][16];
     constexpr int RPB = N == 64 ? 4 : 1;
     const int tid = threadIdx.x % N, d = in.d;
-    const int64_t row = (int64_t)dense_block_number() * RPB + threadIdx.x / N;
+    const int64_t row = ((int64_t)blockIdx.y * kNormRow + blockIdx.x) * RPB + threadIdx.x / N;
     if (row >= in.rows) return;  // a whole wave, or a whole block
     Packed<T> x[KEEP], b[KEEP], g[KEEP], wp[KEEP], wn[KEEP];
 #pragma unroll
@@ -394,8 +397,10 @@ template <class T, int N, int KEEP>
 void forward(const NormIn<T>& in, float eps, T* sum, T* normed, float* r_post, float* r_pre,
              hipStream_t s) {
     const int64_t blocks = N == 64 ? (in.rows + 3) / 4 : in.rows;
-    ELB_LAUNCH((norm_forward<T, N, KEEP>), grid_of(blocks), dim3(N == 64 ? 256 : N), 0, s, in, eps,
-               sum, normed, r_post, r_pre);
+    const dim3 grid((unsigned)(blocks < kNormRow ? blocks : kNormRow),
+                    (unsigned)((blocks + kNormRow - 1) / kNormRow));
+    ELB_LAUNCH((norm_forward<T, N, KEEP>), grid, dim3(N == 64 ? 256 : N), 0, s, in, eps, sum, normed,
+               r_post, r_pre);
 }
 
 template <class T>

@@ -94,6 +94,21 @@ def test_every_code_and_scale(dtype):
         assert torch.equal(y.double(), want.t()[at % k])
 
 
+def test_a_group_that_holds_no_number():
+    """A weight group with an infinity or a NaN makes its row's products NaN, and no other's."""
+    g = gen(4)
+    w = normal(g, 48, 96)
+    w[5, 40], w[17, 0] = float("inf"), float("nan")
+    W, s = B.elb_quantize_f4(w)
+    for T in (1, 20, 3000):
+        for dtype in (BF16, F32):
+            y = B.elb_linear_f4(torch.ones((T, 96), dtype=dtype, device="cuda"), W, s)
+            torch.cuda.synchronize()
+            bad = torch.zeros(48, dtype=torch.bool, device="cuda")
+            bad[[5, 17]] = True
+            assert bool(y[:, bad].isnan().all()) and not bool(y[:, ~bad].isnan().any())
+
+
 SIZES = [(32, 16), (64, 32), (96, 48), (160, 16), (256, 528), (1056, 80), (2048, 1040), (8192, 64)]
 
 

@@ -62,6 +62,14 @@ def test_the_headline_layer(weights):
 
 
 @pytest.mark.parametrize("weights", ["bf16", "f4"])
+def test_wide_layers(weights):
+    """Rows longer than a wave's share of tokens in registers, and expert widths past a unit."""
+    for T, d, N, m, K in ((1, 2112, 8, 64, 2), (13, 2240, 5, 128, 3), (3, 4096, 4, 576, 2),
+                          (16, 6144, 3, 64, 3)):
+        check(layer(T, d, N, m, weights), K=K)
+
+
+@pytest.mark.parametrize("weights", ["bf16", "f4"])
 def test_one_expert_for_all_and_all_for_one(weights):
     """Every token on the same expert; every token on all experts; a router of zeros (ties: the
     lowest ids)."""

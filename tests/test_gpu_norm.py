@@ -162,6 +162,27 @@ def test_a_row_alone_and_what_lies_around():
 
 
 @pytest.mark.gpu
+def test_more_rows_than_a_launch_dimension():
+    """More than 2^20 blocks: rows in the second and third row of the launch."""
+    for d, T in ((528, (1 << 21) + 5), (16, (1 << 22) + 7)):
+        x = torch.empty((T, d), dtype=BF16, device="cuda")
+        at = [0, 1, (1 << 20) - 1, 1 << 20, (1 << 20) + 1, T - 9, T - 1]
+        x.fill_(2.0)
+        g = torch.Generator(device="cuda")
+        g.manual_seed(d)
+        rows = torch.randn((len(at), d), generator=g, device="cuda").to(BF16)
+        x[at] = rows
+        w = torch.ones(d, dtype=BF16, device="cuda")
+        _, normed = B.elb_norm_forward(x, w_pre=w)
+        _, want = B.elb_norm_forward(rows, w_pre=w)
+        torch.cuda.synchronize()
+        assert torch.equal(normed[at], want)
+        rest = torch.ones(T, dtype=torch.bool, device="cuda")
+        rest[at] = False
+        assert bool((normed[rest] == 1).all())
+
+
+@pytest.mark.gpu
 def test_no_tokens():
     for gate in ("none", "channel", "token", "full"):
         v = inputs(0, 64, BF16, gate)
