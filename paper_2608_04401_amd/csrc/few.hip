@@ -15,7 +15,7 @@ namespace elb {
 
 namespace {
 
-constexpr int kUpWaves = 8, kDownWaves = 8;
+constexpr int kUpWaves = 8, kDownWaves = 8;  // (routing by counting: a token a wave, up to 8)
 
 // The experts that some token has selected (list[0 .. used)), and of each its tokens: a bit for each,
 // the slot t K + j of each (where its bit is set), and their slots in order.
@@ -72,20 +72,21 @@ struct FewIn {
 __device__ __forceinline__ bf16x8_t as_frag(u32x4_t v) { return __builtin_bit_cast(bf16x8_t, v); }
 
 // ------------------------------------------------------------------------------------------
-// Launch 1.  NG: groups of 16 experts; DMA: x, W_router and the weights on 16-byte boundaries.
+// Launch 1.  XR: rows of x, 8 or 16; DMA: x, W_router and the weights on 16-byte boundaries.
 // ------------------------------------------------------------------------------------------
-template <class W, int KMAX, bool DMA>
+template <class W, int KMAX, int XR, bool DMA>
 __global__ __launch_bounds__(64 * kUpWaves) void few_up(FewIn in, XTable xt) {
     typedef Stream<W, 4, true, DMA> B;
-    // a wave's LDS: a unit of weights, then its partial tiles; before that two units of the router
-    constexpr int PART = (B::BYTES + 255) / 256 * 256, SLOT = PART + 4096;
-    constexpr int RUNIT = 32 * 128 + 16 * 128;  // 32 rows of W_router, 16 of x
-    static_assert(2 * RUNIT <= SLOT, "");
+    // a wave's LDS: a unit of weights, then its partial tiles; before that RN units of the router, as
+    // many as fit (one token: the router 4.5 us with three, 5.2 with two of 16 rows)
+    constexpr int PART = (B::BYTES + 255) / 256 * 256;
+    constexpr int RUNIT = 32 * 128 + XR * 128, RN = XR == 8 ? 3 : 2;  // 32 rows of W_router, XR of x
+    constexpr int SLOT = PART + 4096 > RN * RUNIT ? PART + 4096 : RN * RUNIT;
     __shared__ __attribute__((aligned(1024))) char sm[kUpWaves * SLOT];
     __shared__ float logits[RW][16 * 65];
     __shared__ Slots slots;
     __shared__ float sorted[kUpWaves][64];
-    __shared__ int order[kUpWaves][64];
+    __shared__ int order[kUpWaves][64], rank[kUpWaves][64];
     __shared__ int sk[16], sids[16 * kLaneMaxK];
     __shared__ float sw[16 * kLaneMaxK];
     const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, hq = lane >> 4;
@@ -96,6 +97,7 @@ __global__ __launch_bounds__(64 * kUpWaves) void few_up(FewIn in, XTable xt) {
 
     if (blockIdx.x == 0)
         for (int i = tid; i < d / 64; i += 64 * kUpWaves) in.count[i] = 0;
+    rank[wave][lane] = 0;
 
     // the tokens' operands of this wave's share of the contraction, where it is at most 256 long
     const int units = (d + W::KU - 1) / W::KU;
@@ -111,39 +113,62 @@ __global__ __launch_bounds__(64 * kUpWaves) void few_up(FewIn in, XTable xt) {
 
     // ---- router: wave w has slice w % 4 of the contraction and experts 32 (w / 4) .. + 31 ----
     {
-        Copier<KC, 32, 2, 1, false, DMA> cw;
-        Copier<KC, 16, 2, 1, false, DMA> cx;
         int first, count;
         router_slice(d, wave & 3, first, count);
         const int e0 = 32 * (wave >> 2);
         const int n = (count + 1) / 2;  // units of two steps of 32
-        cw.init(in.router + (int64_t)(e0 < N ? e0 : 0) * d + first * 32, nullptr, 2 * (int64_t)d,
-                e0 < N ? N - e0 : 0, count * 32, lane, 0);
-        cx.init(in.x + first * 32, nullptr, 2 * (int64_t)d, T, count * 32, lane, 0);
-        auto issue = [&](int u) {
-            const int at = (u & 1) * RUNIT;
-            cw.issue(u, n, lds + at, slot + at, lane, 0);
-            cx.issue(u, n, lds + at + 4096, slot + at + 4096, lane, 0);
+        // Byte offsets of the lane's copies: rows 8 i + lane / 8 of W_router and of x (past the last
+        // one that again, whose logits no token or expert takes), chunk kc_swz(row, lane % 8).  (Copier's
+        // bounds for each unit take longer than its copies: one token's router 5.0 us with them.)
+        uint32_t off[4 + XR / 8], swz[2];
+#pragma unroll
+        for (int i = 0; i < 4 + XR / 8; ++i) {
+            int r = 8 * (i < 4 ? i : i - 4) + (lane >> 3);
+            if (i < 2) swz[i] = kc_swz(r, lane & 7) * 16;
+            if (i < 4) r = e0 + r < N ? e0 + r : N - 1;
+            else r = r < T ? r : T - 1;
+            off[i] = ((uint32_t)r * (uint32_t)d + (uint32_t)first * 32u) * 2u;
+        }
+        auto issue = [&](int u, int at) {
+            u = u < n ? u : n - 1;  // past the last one: that again, so that the waits' counts hold
+            const bool whole = 2 * u + 1 < count;
+#pragma unroll
+            for (int i = 0; i < 4 + XR / 8; ++i) {
+                // of a unit of one step the lower half alone is read
+                const uint32_t o = off[i] + (uint32_t)u * 128u + (whole ? swz[i & 1] : swz[i & 1] & 63u);
+                const char* const src = (const char*)(i < 4 ? in.router : in.x);
+                if constexpr (DMA)
+                    asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2"
+                                 :: "s"(lds + at * RUNIT + i * 1024), "v"(o), "s"(src)
+                                 : "memory", "m0");
+                else
+                    copy16_any(slot + at * RUNIT + i * 1024 + lane * 16, src + o);
+            }
         };
         f32x4_t acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
-        issue(0);
-        issue(1);
+        constexpr int RI = 4 + XR / 8;  // copy instructions of a unit
+#pragma unroll
+        for (int u = 0; u < RN; ++u)
+            if (n > 0) issue(u, u);
+        int at = 0;
         for (int u = 0; u < n; ++u) {
-            ELB_WAIT_VMCNT(6);  // the unit after this one
+            ELB_WAIT_VMCNT((RN - 1) * RI);  // all but the units after this one
             asm volatile("" ::: "memory");
-            const char* const p = slot + (u & 1) * RUNIT;
+            const char* const p = slot + at * RUNIT;
+            const int xr = l16 % XR;
             u32x4_t a[2], b[2][2];
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
-                a[s] = *reinterpret_cast<const u32x4_t*>(p + 4096 + l16 * 128 +
-                                                         kc_swz(l16, 4 * s + hq) * 16);
+                a[s] = *reinterpret_cast<const u32x4_t*>(p + 4096 + xr * 128 +
+                                                         kc_swz(xr, 4 * s + hq) * 16);
 #pragma unroll
                 for (int g = 0; g < 2; ++g)
                     b[s][g] = *reinterpret_cast<const u32x4_t*>(p + (16 * g + l16) * 128 +
                                                                 kc_swz(l16, 4 * s + hq) * 16);
             }
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the unit is free again
-            issue(u + 2);  // past the last one: zeros
+            issue(u + RN, at);
+            at = at + 1 == RN ? 0 : at + 1;
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
@@ -162,30 +187,40 @@ __global__ __launch_bounds__(64 * kUpWaves) void few_up(FewIn in, XTable xt) {
     }
     ELB_WAIT_VMCNT(0);  // the last copies, before their LDS is used again; and x
     __syncthreads();
-    if (T <= kUpWaves) {
-        // a wave per token, a lane per expert: its logit, and its rank by counting the (key, id)
-        // pairs before it, in the order of route_token_x16's network (one token: 3.5 us from here to
-        // the selection, 4.5 by that; with two tokens a wave 5.8 and 4.6)
-        if (wave < T) {
-            const int t = wave;
+    if constexpr (XR == 8) {
+        // Waves share a token, a lane per expert: its logit, and its rank by counting the (key, id) pairs
+        // before it, in the order of route_token_x16's network (one token: 3.4 us from here to the
+        // selection, 4.5 by that).
+        const int parts = T > 4 ? 1 : T > 2 ? 2 : T > 1 ? 4 : 8;  // waves a token
+        const int t = wave / parts, part = wave % parts;
+        float key = 0.0f;
+        if (t < T) {
             float l = -INFINITY;
             if (lane < N) {
                 l = logits[0][t * 65 + lane];
 #pragma unroll
                 for (int q = 1; q < RW; ++q) l += logits[q][t * 65 + lane];
             }
-            const float key = N == 64 ? order_key(l) : order_key_any(l);
+            key = N == 64 ? order_key(l) : order_key_any(l);
             const int image = ord_flip32(__float_as_int(key));
             const int64_t mine = ((int64_t)image << 32) | (uint32_t)(63 - lane);
-            int rank = 0;
+            int before = 0;
+            const int n = 64 / parts;
+            for (int j0 = n * part; j0 < n * (part + 1); j0 += 8)
 #pragma unroll
-            for (int j = 0; j < 64; ++j) {
-                const int64_t other =
-                    ((int64_t)__builtin_amdgcn_readlane(image, j) << 32) | (uint32_t)(63 - j);
-                rank += other > mine;
-            }
-            sorted[t][rank] = key;
-            order[t][rank] = lane;
+                for (int q = 0; q < 8; ++q) {
+                    const int j = j0 + q;
+                    const int64_t other =
+                        ((int64_t)__builtin_amdgcn_readlane(image, j) << 32) | (uint32_t)(63 - j);
+                    before += other > mine;
+                }
+            atomicAdd(&rank[t][lane], before);
+        }
+        __syncthreads();
+        if (t < T && part == 0) {
+            const int r = rank[t][lane];
+            sorted[t][r] = key;
+            order[t][r] = lane;
         }
         __syncthreads();
         if (tid < 16 * kUpWaves) {  // whole waves: 16 lanes a token
@@ -474,17 +509,23 @@ __global__ __launch_bounds__(64 * kDownWaves) void few_down(FewIn in) {
     }
 }
 
+template <class W, int XR, bool DMA>
+void run_up(const FewIn& in, unsigned blocks, hipStream_t s) {
+    const XTable xt = make_xtable(in.N);
+    if (in.K <= 8)
+        ELB_LAUNCH((few_up<W, 8, XR, DMA>), dim3(blocks), dim3(64 * kUpWaves), 0, s, in, xt);
+    else
+        ELB_LAUNCH((few_up<W, kLaneMaxK, XR, DMA>), dim3(blocks), dim3(64 * kUpWaves), 0, s, in, xt);
+}
+
 template <class W, bool DMA>
 hipError_t few(const FewIn& in, int cus, hipStream_t s) {
     {
         ProfileScope prof("few_up", s);
         const int most = (in.T * in.K < in.N ? in.T * in.K : in.N) * (in.m / 32);
-        const dim3 blocks((unsigned)(most < cus ? most : cus));
-        const XTable xt = make_xtable(in.N);
-        if (in.K <= 8)
-            ELB_LAUNCH((few_up<W, 8, DMA>), blocks, dim3(64 * kUpWaves), 0, s, in, xt);
-        else
-            ELB_LAUNCH((few_up<W, kLaneMaxK, DMA>), blocks, dim3(64 * kUpWaves), 0, s, in, xt);
+        const unsigned blocks = most < cus ? most : cus;
+        if (in.T <= 8) run_up<W, 8, DMA>(in, blocks, s);
+        else run_up<W, 16, DMA>(in, blocks, s);
         if (hipError_t e = hipGetLastError()) return e;
     }
     ProfileScope prof("few_down", s);
