@@ -181,9 +181,13 @@ __global__ __launch_bounds__(64 * NW) void stream_f4(StreamIn<X> in) {
            lane);
     typename B::Pending pending = {};
     auto issue = [&](int u) {
+        const bool whole = DMA && (u + 1) * 256 <= in.k;
 #pragma unroll
-        for (int q = 0; q < SUB; ++q)
-            a.issue(SUB * u + q, SUB * u1, lds + q * TM * 128, slot + q * TM * 128, lane, 0);
+        for (int q = 0; q < SUB; ++q) {
+            const int t = SUB * u + q;
+            if (whole) issue_whole(a, (uint32_t)t * 128u, lds + q * TM * 128);
+            else a.issue(t, SUB * u1, lds + q * TM * 128, slot + q * TM * 128, lane, 0);
+        }
         b.issue(u, u1, lds + AB, slot + AB, lane, pending);
     };
     f32x4_t acc[MT][NF];
