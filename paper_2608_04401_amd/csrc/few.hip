@@ -76,7 +76,7 @@ __device__ __forceinline__ bf16x8_t as_frag(u32x4_t v) { return __builtin_bit_ca
 // ------------------------------------------------------------------------------------------
 template <class W, int KMAX, int XR, bool DMA>
 __global__ __launch_bounds__(64 * kUpWaves) void few_up(FewIn in, XTable xt) {
-    typedef Stream<W, 4, true, DMA> B;
+    typedef Stream<W, 4, true, DMA, true> B;
     // a wave's LDS: a unit of weights, then its partial tiles; before that RN units of the router, as
     // many as fit (one token: the router 4.5 us with three, 5.2 with two of 16 rows)
     constexpr int PART = (B::BYTES + 255) / 256 * 256;
@@ -367,7 +367,7 @@ __global__ __launch_bounds__(64 * kUpWaves) void few_up(FewIn in, XTable xt) {
 // ------------------------------------------------------------------------------------------
 template <class W, bool DMA>
 __global__ __launch_bounds__(64 * kDownWaves) void few_down(FewIn in) {
-    typedef Stream<W, 4, false, DMA> B;
+    typedef Stream<W, 4, false, DMA, true> B;
     constexpr int SUB = W::KU / 64, AB = SUB * 8 * 128;  // eight rows of h
     constexpr int SLOT = (AB + B::BYTES + 255) / 256 * 256;
     static_assert(SLOT >= 4096, "");

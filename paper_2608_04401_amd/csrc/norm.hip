@@ -47,6 +47,30 @@ __device__ __forceinline__ float row_sum(float v, float* sh) {
     return t;
 }
 
+// Two of them behind one barrier
+template <int N>
+__device__ __forceinline__ void row_sum2(float& v, float& u, float* sh, float* sh2) {
+    v = wave_sum(v);
+    u = wave_sum(u);
+    if constexpr (N > 64) {
+        const int wave = threadIdx.x >> 6;
+        if ((threadIdx.x & 63) == 0) {
+            sh[wave] = v;
+            sh2[wave] = u;
+        }
+        __syncthreads();
+        constexpr int W = N / 64;
+        const int at = wave / W * W;
+        v = sh[at];
+        u = sh2[at];
+#pragma unroll
+        for (int i = 1; i < W; ++i) {
+            v += sh[at + i];
+            u += sh2[at + i];
+        }
+    }
+}
+
 // 1 / sqrt(mean of v^2 + eps) of a row.  A sum of squares past fp32's range is taken again of v 2^-64,
 // whose root is in range (the branch is the same for all that work on the row).
 template <int N, int KEEP>
@@ -212,7 +236,7 @@ template <class T, int N, int KEEP, int RPB>
 __global__ __launch_bounds__(N* RPB) void norm_backward(NormIn<T> in, NormGradIn<T> gr) {
     constexpr int W = N * RPB / 64;
     __shared__ float sh[3][2][W];  // per sum and parity of the round
-    __shared__ float cols[RPB > 1 ? RPB * N * 8 : 1];
+    __shared__ float cols[3][RPB > 1 ? RPB * N * 8 : 1];
     const int tid = threadIdx.x % N, sub = threadIdx.x / N, d = in.d;
     const float inv_d = 1.0f / (float)d;
     float acc[3][KEEP][8];
@@ -314,14 +338,14 @@ __global__ __launch_bounds__(N* RPB) void norm_backward(NormIn<T> in, NormGradIn
                 if (gr.dgate && in.gate_kind == ELB_GATE_FULL && live && c < d)
                     store8(gr.dgate + row * d + c, o);
             }
-            if (gr.dgate && in.gate_kind == ELB_GATE_TOKEN) {
-                tok = row_sum<N>(tok, sh[1][ph]);
-                if (live && tid == 0) {
-                    if constexpr (sizeof(T) == 2) gr.dgate[row] = f32_to_bf16(tok);
-                    else gr.dgate[row] = tok;
-                }
+            if (in.w_post || (gr.dgate && in.gate_kind == ELB_GATE_TOKEN)) {
+                row_sum2<N>(m, tok, sh[1][ph], sh[2][ph]);
+                m *= inv_d;
             }
-            if (in.w_post) m = row_sum<N>(m, sh[2][ph]) * inv_d;
+            if (gr.dgate && in.gate_kind == ELB_GATE_TOKEN && live && tid == 0) {
+                if constexpr (sizeof(T) == 2) gr.dgate[row] = f32_to_bf16(tok);
+                else gr.dgate[row] = tok;
+            }
             if (gr.dblock) {
 #pragma unroll
                 for (int i = 0; i < KEEP; ++i) {
@@ -338,29 +362,31 @@ __global__ __launch_bounds__(N* RPB) void norm_backward(NormIn<T> in, NormGradIn
         ph ^= 1;
     }
     // the block's sums, one row of d floats of `part` for each
+    float* const out = gr.part + (int64_t)blockIdx.x * 3 * d;
 #pragma unroll
-    for (int j = 0; j < 3; ++j) {
-        if (!(gr.cols >> j & 1)) continue;
-        float* const out = gr.part + ((int64_t)blockIdx.x * 3 + j) * d;
+    for (int i = 0; i < KEEP; ++i) {
+        const int c = (i * N + tid) * 8;
+        if constexpr (RPB > 1) {
+            static_assert(KEEP == 1, "one pass through LDS");
 #pragma unroll
-        for (int i = 0; i < KEEP; ++i) {
-            const int c = (i * N + tid) * 8;
-            if constexpr (RPB > 1) {
-                __syncthreads();
+            for (int j = 0; j < 3; ++j)
 #pragma unroll
-                for (int q = 0; q < 8; ++q) cols[(sub * 8 + q) * N + tid] = acc[j][i][q];
-                __syncthreads();
-                // 8 N sums by N RPB threads, in the order of the columns
+                for (int q = 0; q < 8; ++q) cols[j][(sub * 8 + q) * N + tid] = acc[j][i][q];
+            __syncthreads();
+            // 3 times 8 N sums by N RPB threads, in the order of the columns
+#pragma unroll
+            for (int j = 0; j < 3; ++j)
                 for (int k = threadIdx.x; k < 8 * N; k += N * RPB) {
                     const int at = k % 8 * N + k / 8;
-                    float t = cols[at];
+                    float t = cols[j][at];
 #pragma unroll
-                    for (int p = 1; p < RPB; ++p) t += cols[p * 8 * N + at];
-                    if (i * N * 8 + k < d) out[i * N * 8 + k] = t;
+                    for (int p = 1; p < RPB; ++p) t += cols[j][p * 8 * N + at];
+                    if (k < d && (gr.cols >> j & 1)) out[(int64_t)j * d + k] = t;
                 }
-            } else if (c < d) {
-                store8(out + c, acc[j][i]);
-            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 3; ++j)
+                if (c < d && (gr.cols >> j & 1)) store8(out + (int64_t)j * d + c, acc[j][i]);
         }
     }
 }
