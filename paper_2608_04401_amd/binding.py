@@ -628,19 +628,27 @@ def _norm_op(residual, block, w_post, w_pre, gate, residual_scale, block_scale, 
     shape, dtype = _matrix("residual" if block is None else "block", like), like.dtype
     T, d = shape
     dt, dev = _dtype_code(like), _device(like)
-    _want("residual" if block is None else "block", like, shape, dtype, dev)
-    if residual is not like:
+    # (addresses and checks one by one: each call that is saved here is 0.1 to 0.2 us of 8)
+    p_res = p_block = p_gate = p_post = p_pre = None
+    if residual is not None:
         _want("residual", residual, shape, dtype, dev)
+        p_res = residual.data_ptr()
+    if block is not None:
+        _want("block", block, shape, dtype, dev)
+        p_block = block.data_ptr()
     if w_post is not None:
         _want("w_post", w_post, (d,), dtype, dev)
+        p_post = w_post.data_ptr()
     if w_pre is not None:
         _want("w_pre", w_pre, (d,), dtype, dev)
+        p_pre = w_pre.data_ptr()
     kind = GATE_NONE
     if gate is not None:
         kind = _gate_kind(gate, T, d)
         _want("gate", gate, gate.shape, dtype, dev)
-    op = NormOp(_ptr(residual), _ptr(block), _ptr(gate), _ptr(w_post), _ptr(w_pre), T, d, kind, dt,
-                residual_scale, block_scale, eps)
+        p_gate = gate.data_ptr()
+    op = NormOp(p_res, p_block, p_gate, p_post, p_pre, T, d, kind, dt, residual_scale, block_scale,
+                eps)
     return op, like, shape, dtype, dev
 
 
@@ -649,26 +657,31 @@ def elb_norm_forward(residual=None, block=None, w_post=None, w_pre=None, gate=No
                      out=None, keep: bool = False):
     """sum = residual_scale residual + block_scale gate * norm(block) (not normalised without
     w_post) and normed = the norm of sum with w_pre (None without).  -> (sum, normed), or with
-    keep=True (sum, normed, kept): kept is what elb_norm_backward needs of the forward pass.
-    gate: [d], [T, 1], [T, d] or None.  out (of sum) may be residual.  Without a block, an out and a
-    residual_scale, sum is residual itself.  Outside autograd: results never require a gradient."""
+    keep=True (sum, normed, kept): kept [2, T] float32, r_post and r_pre, is what elb_norm_backward
+    needs of the forward pass.  gate: [d], [T, 1], [T, d] or None.  out (of sum) may be residual.
+    Without a block, an out and a residual_scale, sum is residual itself.  Outside autograd: results
+    never require a gradient."""
     op, like, shape, dtype, dev = _norm_op(residual, block, w_post, w_pre, gate, residual_scale,
                                            block_scale, eps)
     same = block is None and out is None and residual_scale == 1.0
     if same:
-        total = residual.detach()
-    elif out is None:
-        total = torch.empty_like(like)
+        total, p_sum = residual.detach(), None
     else:
-        _want("out", out, shape, dtype, dev)
-        total = out
-    normed = None if w_pre is None else torch.empty_like(like)
-    kept = (None, None)
+        if out is None:
+            total = torch.empty_like(like)
+        else:
+            _want("out", out, shape, dtype, dev)
+            total = out
+        p_sum = total.data_ptr()
+    normed = p_normed = kept = p_post = p_pre = None
+    if w_pre is not None:
+        normed = torch.empty_like(like)
+        p_normed = normed.data_ptr()
     if keep:
-        kept = tuple(None if w is None else torch.empty(shape[:1], dtype=torch.float32,
-                                                        device=like.device) for w in (w_post, w_pre))
-    status = lib().elb_norm_forward(C.byref(op), None if same else total.data_ptr(), _ptr(normed),
-                                    _ptr(kept[0]), _ptr(kept[1]), _stream())
+        kept = torch.empty((2, shape[0]), dtype=torch.float32, device=like.device)
+        p_post = kept.data_ptr()
+        p_pre = p_post + 4 * shape[0]
+    status = lib().elb_norm_forward(C.byref(op), p_sum, p_normed, p_post, p_pre, _stream())
     if status:
         _check("elb_norm_forward", status)
     return (total, normed, kept) if keep else (total, normed)
@@ -687,22 +700,36 @@ def elb_norm_backward(d_sum, d_normed, sum, block, kept, w_post=None, w_pre=None
     (zero).  sum and kept from elb_norm_forward(..., keep=True), the rest as given to it."""
     op, like, shape, dtype, dev = _norm_op(sum if block is None else None, block, w_post, w_pre,
                                            gate, residual_scale, block_scale, 1.0)
-    for name, t in (("d_sum", d_sum), ("d_normed", d_normed), ("sum", sum)):
-        if t is not None:
-            _want(name, t, shape, dtype, dev)
-    r_post, r_pre = kept
-    _want("kept", r_post, shape[:1], torch.float32, dev)
-    _want("kept", r_pre, shape[:1], torch.float32, dev)
-    out = [torch.empty_like(t) if n and t is not None else None
-           for t, n in zip((like, block, gate, w_post, w_pre), need)]
+    p_dsum = p_dnormed = p_sum = None
+    if d_sum is not None:
+        _want("d_sum", d_sum, shape, dtype, dev)
+        p_dsum = d_sum.data_ptr()
+    if d_normed is not None:
+        _want("d_normed", d_normed, shape, dtype, dev)
+        p_dnormed = d_normed.data_ptr()
+    if sum is not None:
+        _want("sum", sum, shape, dtype, dev)
+        p_sum = sum.data_ptr()
+    _want("kept", kept, (2, shape[0]), torch.float32, dev)
+    p_post = kept.data_ptr()
+    need_res, need_block, need_gate, need_post, need_pre = need
+    d_res = torch.empty_like(like) if need_res else None
+    d_block = torch.empty_like(block) if need_block and block is not None else None
+    d_gate = torch.empty_like(gate) if need_gate and gate is not None else None
+    d_post = torch.empty_like(w_post) if need_post and w_post is not None else None
+    d_pre = torch.empty_like(w_pre) if need_pre and w_pre is not None else None
     stream = _stream()
     ws = workspace(elb_norm_backward_workspace_bytes(*shape), like.device, stream)
     status = lib().elb_norm_backward(
-        C.byref(op), _ptr(d_sum), _ptr(d_normed), _ptr(sum), _ptr(r_post), _ptr(r_pre),
-        *[_ptr(t) for t in out], ws.data_ptr(), ws.numel(), stream)
+        C.byref(op), p_dsum, p_dnormed, p_sum, p_post, p_post + 4 * shape[0],
+        None if d_res is None else d_res.data_ptr(),
+        None if d_block is None else d_block.data_ptr(),
+        None if d_gate is None else d_gate.data_ptr(),
+        None if d_post is None else d_post.data_ptr(),
+        None if d_pre is None else d_pre.data_ptr(), ws.data_ptr(), ws.numel(), stream)
     if status:
         _check("elb_norm_backward", status)
-    return tuple(out)
+    return d_res, d_block, d_gate, d_post, d_pre
 
 
 def elb_quantize_f4(x: torch.Tensor):

@@ -272,12 +272,12 @@ class Around(torch.autograd.Function):
     @staticmethod
     def forward(ctx, residual, block, w_post, w_pre, gate):
         total, normed, kept = B.elb_norm_forward(residual, block, w_post, w_pre, gate, keep=True)
-        ctx.save_for_backward(total, block, w_post, w_pre, gate, *kept)
+        ctx.save_for_backward(total, block, w_post, w_pre, gate, kept)
         return total, normed
 
     @staticmethod
     def backward(ctx, d_sum, d_normed):
-        total, block, w_post, w_pre, gate, *kept = ctx.saved_tensors
+        total, block, w_post, w_pre, gate, kept = ctx.saved_tensors
         n = ctx.needs_input_grad
         g = B.elb_norm_backward(d_sum.contiguous(), d_normed.contiguous(), total, block, kept,
                                 w_post, w_pre, gate, need=(n[0], n[1], n[4], n[2], n[3]))

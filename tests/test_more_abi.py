@@ -246,12 +246,12 @@ def test_binding_refuses_wrong_shapes():
     z = lambda *s, t=torch.bfloat16: torch.zeros(s, dtype=t, device="cuda")
     u8 = lambda *s: z(*s, t=torch.uint8)
     x, w = z(4, 64), z(64)
-    kept = (z(4, t=torch.float32), z(4, t=torch.float32))
+    kept = z(2, 4, t=torch.float32)
     for f in (lambda: B.elb_norm_forward(x, x, gate=z(4)), lambda: B.elb_norm_forward(x, x, gate=z(1, 64)),
               lambda: B.elb_norm_forward(x, z(3, 64)), lambda: B.elb_norm_forward(x, x, w_post=z(32)),
               lambda: B.elb_norm_forward(z(64, 4).t(), w_pre=w),
               lambda: B.elb_norm_backward(z(3, 64), None, x, x, kept),
-              lambda: B.elb_norm_backward(x, None, x, x, (z(3, t=torch.float32), None), w_post=w),
+              lambda: B.elb_norm_backward(x, None, x, x, z(2, 3, t=torch.float32), w_post=w),
               lambda: B.elb_linear_f4(x, u8(16, 16), u8(16, 2)),
               lambda: B.elb_linear_f4(x, u8(16, 32), u8(16, 1)),
               lambda: B.elb_ffn_forward_f4(x, u8(64, 32), u8(64, 2), u8(32, 16), u8(32, 1)),
