@@ -464,11 +464,13 @@ int elb_quantize_f4(const void *x, int64_t rows, int32_t d, int32_t dtype, uint8
  * (n, i) times its group's scale.
  *   x        [T, k]       dtype
  *   W        [n, k / 2]   uint8, W_scale [n, k / 32] uint8   as elb_quantize_f4 lays them out; scale
- *                         bytes from 2 to 252 (others give unspecified, but in-bounds, results)
+ *                         bytes from 2 to 252, or 255, which makes the row's products NaN (others give
+ *                         unspecified, but in-bounds, results)
  *   residual [T, n]       dtype   optional (NULL: none)
  *   y        [T, n]       dtype   output; may be residual, shares memory with no other input
  *   workspace             at least elb_linear_f4_workspace_bytes(T, n, k, dtype) bytes (may be 0)
- * Products are exact, sums fp32, y is rounded once.
+ * Products are exact (of an fp32 x below 2^-100 in magnitude: x is taken to within 2^-124), sums fp32, y
+ * is rounded once.  An infinity in x gives an infinity or a NaN.
  * Requirements: n a positive multiple of 16, k of 32, both at most 2^20; T < 2^31.
  */
 size_t elb_linear_f4_workspace_bytes(int64_t T, int32_t n, int32_t k, int32_t dtype);

@@ -1155,8 +1155,8 @@ int elb_moe_forward_few(const void* x, const void* W_router, const void* W_gate_
     char* const ws = (char*)workspace;
     return hip_status(
         launch_moe_few(x, W_router, W_gate_up, gate_up_scale, W_down, down_scale, residual, T, d, N,
-                       m, *params, ws, (float*)(ws + L.part), (int*)(ws + L.count), y, k_out ? k_out : (int*)(ws + L.k),
-                       ids_out ? ids_out : (int*)(ws + L.ids),
+                       m, *params, ws, (float*)(ws + L.part), (int*)(ws + L.count), y,
+                       k_out ? k_out : (int*)(ws + L.k), ids_out ? ids_out : (int*)(ws + L.ids),
                        w_out ? w_out : (float*)(ws + L.w), cus_per_device(), (hipStream_t)stream),
         "moe_forward_few");
 }

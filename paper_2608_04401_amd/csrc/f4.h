@@ -126,9 +126,9 @@ __device__ __forceinline__ void issue_whole(const C& c, uint32_t at, uint32_t ld
 
 // One wave's copies of a unit of weights: 16 NF rows (PAIR: the second half of them `apart` rows of
 // the tensor further on) of 128 bytes, and the rows' eight scale bytes behind them.  DMA: weights on
-// 16-byte boundaries; otherwise ordinary loads, as for scales whose rows are off 4-byte ones.  NT: weights that a call reads
-// once, with the non-temporal hint (few-token layer, bf16, 8 to 16 tokens: 97 % to 100 % of the time that
-// elb_moe_forward takes, 108 % to 112 % without).
+// 16-byte boundaries; otherwise ordinary loads, as for scales whose rows are off 4-byte ones.  NT:
+// weights that a call reads once, with the non-temporal hint (few-token layer, bf16, 8 to 16 tokens: 97 %
+// to 100 % of the time that elb_moe_forward takes, 108 % to 112 % without).
 template <class W, int NF, bool PAIR, bool DMA, bool NT = false>
 struct Stream {
     static constexpr int ROWS = 16 * NF;
@@ -169,7 +169,7 @@ struct Stream {
     struct Pending {
         uint32_t v[(ROWS + 31) / 32];
     };
-    // unit u to LDS at lds (ldsp: the same as a pointer); past uend zeros
+    // unit u to LDS at lds (ldsp: the same as a pointer); values past the row's end are zeros
     __device__ __forceinline__ void issue(int u, int uend, uint32_t lds, char* ldsp, int lane,
                                           Pending& pending) const {
         if (DMA && u < uend && (int64_t)(u + 1) * 128 <= copy.klen)

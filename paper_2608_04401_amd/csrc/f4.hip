@@ -290,7 +290,7 @@ __global__ __launch_bounds__(64 * NW) void stream_f4(StreamIn<X> in) {
     if constexpr (!PAIR) {
         // The partial sums go past the L2, which blocks elsewhere on the chip do not share: agent-scope
         // stores, done when the counter goes up, and agent-scope loads.  (A release fence would
-        // write the whole L2 back, for each block: some 30 us.)
+        // write the whole L2 back, for each block: the few-token layer's, 31 us.)
         const int64_t tile = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
         float* const mine = in.part + tile * in.shares * (PIECES * 4);
         __shared__ int last;
@@ -342,17 +342,24 @@ template <class X, bool PAIR>
 void stream(StreamIn<X> in, const StreamForm& f, hipStream_t s) {
     constexpr bool F = sizeof(X) == 4;
     in.shares = f.shares;
-    switch (f.tm * 8 + f.nf) {
-        case 8 * 8 + 1: return run_stream<X, 8, PAIR ? 2 : 1, F ? 8 : 16, PAIR>(in, s);
+    const int tile = f.tm * 8 + f.nf;
+    // (those of the type's table; gate and up rows are two fragments at least)
+    if constexpr (!PAIR) {
+        if (tile == 8 * 8 + 1) return run_stream<X, 8, 1, F ? 8 : 16, PAIR>(in, s);
+        if (tile == 16 * 8 + 1) return run_stream<X, 16, 1, F ? 4 : 8, PAIR>(in, s);
+    }
+    if constexpr (F) {
+        if (tile == 8 * 8 + 4) return run_stream<X, 8, 4, 8, PAIR>(in, s);
+    } else {
+        if (tile == 32 * 8 + 4) return run_stream<X, 32, 4, 4, PAIR>(in, s);
+        if (tile == 48 * 8 + 2) return run_stream<X, 48, 2, 4, PAIR>(in, s);
+        if (tile == 48 * 8 + 4) return run_stream<X, 48, 4, 4, PAIR>(in, s);
+    }
+    switch (tile) {
         case 8 * 8 + 2: return run_stream<X, 8, 2, 8, PAIR>(in, s);
-        case 8 * 8 + 4: return run_stream<X, 8, 4, 8, PAIR>(in, s);
-        case 16 * 8 + 1: return run_stream<X, 16, PAIR ? 2 : 1, F ? 4 : 8, PAIR>(in, s);
         case 16 * 8 + 2: return run_stream<X, 16, 2, F ? 4 : 8, PAIR>(in, s);
         case 16 * 8 + 4: return run_stream<X, 16, 4, F ? 4 : 8, PAIR>(in, s);
-        case 32 * 8 + 2: return run_stream<X, 32, 2, 4, PAIR>(in, s);
-        case 32 * 8 + 4: return run_stream<X, 32, F ? 2 : 4, 4, PAIR>(in, s);
-        case 48 * 8 + 2: return run_stream<X, F ? 32 : 48, 2, 4, PAIR>(in, s);
-        default: return run_stream<X, F ? 32 : 48, F ? 2 : 4, 4, PAIR>(in, s);
+        default: return run_stream<X, 32, 2, 4, PAIR>(in, s);
     }
 }
 

@@ -24,10 +24,10 @@ struct StreamForm {
 };
 constexpr StreamForm kStreamBf16[] = {
     {8, 1, 16, 1, 1.2f, 1.75f, 1.6f, 3.5f},   {8, 2, 8, 2, 1.7f, 1.7f, 1.0f, 2.7f},
-    {8, 4, 8, 1, 1.5f, 2.0f, 1.72f, 2.8f},    {16, 1, 8, 1, 1.63f, 1.29f, 0.92f, 3.2f},
-    {16, 2, 8, 1, 1.44f, 1.58f, 1.19f, 2.8f}, {16, 4, 8, 1, 1.5f, 1.8f, 1.88f, 2.9f},
-    {32, 2, 4, 1, 1.34f, 1.35f, 1.24f, 3.5f}, {32, 4, 4, 1, 0.93f, 2.15f, 1.82f, 4.0f},
-    {48, 2, 4, 1, 1.07f, 1.7f, 1.58f, 4.2f},  {48, 4, 4, 1, 0.57f, 2.6f, 2.29f, 4.9f}};
+    {16, 1, 8, 1, 1.63f, 1.29f, 0.92f, 3.2f}, {16, 2, 8, 1, 1.44f, 1.58f, 1.19f, 2.8f},
+    {16, 4, 8, 1, 1.5f, 1.8f, 1.88f, 2.9f},   {32, 2, 4, 1, 1.34f, 1.35f, 1.24f, 3.5f},
+    {32, 4, 4, 1, 0.93f, 2.15f, 1.82f, 4.0f}, {48, 2, 4, 1, 1.07f, 1.7f, 1.58f, 4.2f},
+    {48, 4, 4, 1, 0.57f, 2.6f, 2.29f, 4.9f}};
 constexpr StreamForm kStreamF32[] = {
     {8, 1, 8, 1, 1.39f, 1.4f, 2.22f, 3.5f},   {8, 2, 8, 1, 1.22f, 1.7f, 2.71f, 2.8f},
     {8, 4, 8, 1, 1.65f, 1.65f, 3.7f, 2.8f},   {16, 1, 4, 1, 1.5f, 1.45f, 1.46f, 3.3f},
@@ -68,9 +68,11 @@ inline StreamForm stream_form(int64_t T, int cols, int k, bool pair, bool f32) {
 
 // Whether the product [T, k] x [n, k] (block: the dense block of width n and h of width k) streams its
 // weights, by estimated time, or converts them first (the bytes at 5 TB/s, then the best dense form, and
-// 6 us for the launch and the dense form's reads of what was just written).  us, streamed / converted, bf16: 256 tokens, 2048 to 8192 21 / 34, 384 29 / 35, 768 56 / 50;
-// 8192 to 2048 384 23 / 38, 512 40 / 36; fp32: 512 tokens, 8192 to 2048 109 / 179, 2048 to 16384 261 / 293.
-// Up to kStreamedAlways tokens nothing is converted, so that small batches need no scratch for it.
+// 6 us for the launch and the dense form's reads of what was just written).  us, streamed / converted,
+// bf16: 256 tokens, 2048 to 8192 21 / 34, 384 29 / 35, 768 56 / 50; 8192 to 2048 384 23 / 38, 512
+// 34.5 / 36; fp32: 512 tokens, 8192 to 2048 109 / 179, 2048 to 16384 261 / 293.  (The choice between the
+// two was fitted before the streamed copies lost their bounds, so it converts a little early: at most
+// 4 % at these sizes.)  Up to kStreamedAlways tokens nothing is converted, so that small batches need no scratch for it.
 struct F4Plan {
     bool streams;
     StreamForm up, form;  // of a block's gate and up rows; of the projection, or of its down rows

@@ -78,7 +78,7 @@ template <class W, int KMAX, int XR, bool DMA>
 __global__ __launch_bounds__(64 * kUpWaves) void few_up(FewIn in, XTable xt) {
     typedef Stream<W, 4, true, DMA, true> B;
     // a wave's LDS: a unit of weights, then its partial tiles; before that RN units of the router, as
-    // many as fit (one token: the router 4.5 us with three, 5.2 with two of 16 rows)
+    // many as fit
     constexpr int PART = (B::BYTES + 255) / 256 * 256;
     constexpr int RUNIT = 32 * 128 + XR * 128, RN = XR == 8 ? 3 : 2;  // 32 rows of W_router, XR of x
     constexpr int SLOT = PART + 4096 > RN * RUNIT ? PART + 4096 : RN * RUNIT;
@@ -119,7 +119,8 @@ __global__ __launch_bounds__(64 * kUpWaves) void few_up(FewIn in, XTable xt) {
         const int n = (count + 1) / 2;  // units of two steps of 32
         // Byte offsets of the lane's copies: rows 8 i + lane / 8 of W_router and of x (past the last
         // one that again, whose logits no token or expert takes), chunk kc_swz(row, lane % 8).  (Copier's
-        // bounds for each unit take longer than its copies: one token's router 5.0 us with them.)
+        // bounds for each unit take longer than its copies: one token's router 5.0 us with them, 3.8 with
+        // these.)
         uint32_t off[4 + XR / 8], swz[2];
 #pragma unroll
         for (int i = 0; i < 4 + XR / 8; ++i) {
@@ -484,8 +485,8 @@ __global__ __launch_bounds__(64 * kDownWaves) void few_down(FewIn in) {
         return;
     }
     // The partial sums go past the L2, which blocks elsewhere on the chip do not share: agent-scope
-    // stores, done when the counter goes up, and agent-scope loads.  (A release fence would write
-    // the whole L2 back, for each block: 31 us in place of 2.)
+    // stores, done when the counter goes up, and agent-scope loads: 2.5 us of a token's 7.  (A release
+    // fence would write the whole L2 back, for each block: 31 us more.)
     for (int i = tid; i < T * 64; i += 64 * kDownWaves)
         __hip_atomic_store(mine + share * 1024 + i, sum(i), __ATOMIC_RELAXED,
                            __HIP_MEMORY_SCOPE_AGENT);

@@ -229,3 +229,44 @@ def test_no_tokens():
     assert B.elb_linear_f4(z(0, 64), q, s).shape == (0, 64)
     assert B.elb_ffn_forward_f4(z(0, 64), *codes(gen(1), 128, 64), q, s).shape == (0, 64)
     assert B.elb_quantize_f4(z(0, 64))[0].shape == (0, 32)
+
+
+def test_streams_and_captured_calls():
+    """Products in shares, whole and converted on two streams at once, and captured twice and replayed
+    with eager ones between, give the bits of calls in order."""
+    g = gen(11)
+    W, s = codes(g, 1024, 8192)
+    gu, dn = codes(g, 2 * 1056, 1024), codes(g, 1024, 1056)
+
+    def step(x):
+        y = B.elb_linear_f4(x, W, s)
+        return y, B.elb_ffn_forward_f4(y, *gu, *dn, residual=y)
+
+    both = [normal(g, T, 8192, dtype=dt) for T, dt in ((3, BF16), (40, F32))]
+    both.append(normal(g, 2500, 8192, dtype=BF16))  # converted
+    want = [step(x) for x in both]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = []
+    for _ in range(5):
+        for i, x in enumerate(both):
+            with torch.cuda.stream(streams[i % 2]):
+                got.append((i, step(x)))
+    torch.cuda.synchronize()
+    for i, out in got:
+        assert all(torch.equal(a, b) for a, b in zip(out, want[i]))
+    graphs = []
+    for x in both:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = step(x)
+        graphs.append((graph, x, out))
+    for _ in range(3):
+        for graph, x, out in graphs:
+            x.copy_(normal(g, *x.shape))
+            graph.replay()
+            torch.cuda.synchronize()
+            kept = [t.clone() for t in out]
+            eager = step(x.clone())
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(kept, eager))

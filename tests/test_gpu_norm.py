@@ -302,3 +302,51 @@ def test_in_a_function():
             assert torch.equal(leaf.grad, want[i])
         else:
             assert leaf.grad is None
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_streams_and_a_captured_training_step(dtype):
+    """Forward and backward on two streams at once, and captured twice and replayed with eager ones
+    between, give the bits of calls in order."""
+    sizes = [(1500, 1024, "channel"), (37, 4096, "token")]
+    g = torch.Generator(device="cuda")
+    g.manual_seed(5)
+
+    def inputs(T, d, gate):
+        n = lambda *s: torch.randn(s, generator=g, device="cuda").to(dtype)
+        return [n(T, d), n(T, d), n(d), n(d), n(d) if gate == "channel" else n(T, 1), n(T, d), n(T, d)]
+
+    def step(v):
+        total, normed, kept = B.elb_norm_forward(*v[:5], residual_scale=0.5, keep=True)
+        return (total, normed) + B.elb_norm_backward(v[5], v[6], total, v[1], kept, *v[2:5],
+                                                     residual_scale=0.5)
+
+    both = [inputs(*s) for s in sizes]
+    want = [step(v) for v in both]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = []
+    for _ in range(5):
+        for i in range(2):
+            with torch.cuda.stream(streams[i]):
+                got.append((i, step(both[i])))
+    torch.cuda.synchronize()
+    for i, out in got:
+        assert all(torch.equal(a, b) for a, b in zip(out, want[i]))
+    graphs = []
+    for v in both:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = step(v)
+        graphs.append((graph, v, out))
+    for _ in range(3):
+        for (graph, v, out), size in zip(graphs, sizes):
+            for t, new in zip(v, inputs(*size)):
+                t.copy_(new)
+            graph.replay()
+            torch.cuda.synchronize()
+            kept = [t.clone() for t in out]
+            eager = step([t.clone() for t in v])
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(kept, eager))
