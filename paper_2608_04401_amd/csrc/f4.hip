@@ -359,8 +359,8 @@ void stream(StreamIn<X> in, const StreamForm& f, hipStream_t s) {
         case 8 * 8 + 2: return run_stream<X, 8, 2, 8, PAIR>(in, s);
         case 16 * 8 + 2: return run_stream<X, 16, 2, F ? 4 : 8, PAIR>(in, s);
         case 16 * 8 + 4: return run_stream<X, 16, 4, F ? 4 : 8, PAIR>(in, s);
-        default: return run_stream<X, 32, 2, 4, PAIR>(in, s);
     }
+    if constexpr (!F || !PAIR) return run_stream<X, 32, 2, 4, PAIR>(in, s);
 }
 
 __global__ __launch_bounds__(256) void clear_f4(Counters c) { clear_counters(c.p, c.n); }

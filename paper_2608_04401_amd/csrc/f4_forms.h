@@ -7,15 +7,17 @@
 namespace elb {
 
 constexpr int kMostShares = 16, kMostSharing = 512;  // shares of a tile, blocks of tiles with shares
-constexpr int64_t kStreamedAlways = 64, kMostStreamed = 2048;
+constexpr int64_t kStreamedAlways = 64;
+constexpr int64_t most_streamed(bool f32) { return f32 ? 8192 : 2048; }  // tokens
 
 // The tile and waves of a streamed product, in how many shares its contraction is cut, and its
 // estimated time: start + rounds (round + iter * units of a wave) [+ share] us, with rounds of `per` blocks
-// on each of 256 compute units.  The constants are least-squares fits over 1 to 768 tokens and weights
-// of 1024 to 16384 rows of 512 to 8192 values; over these the choice is 0.4 % slower than the best form
-// on average and 18 % at worst (fp32, 96 tokens, 512 to 4096 11.2 for 9.6).  bf16, us, at both sides: 48
-// tokens, 8192 to 2048: 48 x 32 tiles in four shares 10.5, whole 15.7, 48 x 64 in four 12.0, whole 20.5;
-// 2048 to 16384: 48 x 64 9.0, 32 x 64 12.9, 48 x 32 11.0.
+// on each of 256 compute units.  The constants are least-squares fits to 1494 measured products (1 to
+// 768 tokens, weights of 1024 to 16384 rows of 512 to 8192 values); over these sizes the choice, with
+// that of converting the weights, is 0.3 % slower than the best on average and 18 % at worst (fp32, 384
+// tokens, 512 to 4096: 31.9 for 27.1).  bf16, us, at both sides: 48 tokens, 8192 to 2048: 48 x 32 tiles
+// in four shares 10.7, whole 15.1, 48 x 64 in four 12.9, whole 21.2; 2048 to 16384: 48 x 64 9.3, 32 x 64
+// 13.1, 48 x 32 11.2.
 struct StreamForm {
     int tm, nf, nw, per;
     float start, round, iter, share;
@@ -23,16 +25,16 @@ struct StreamForm {
     float time = 0;
 };
 constexpr StreamForm kStreamBf16[] = {
-    {8, 1, 16, 1, 1.2f, 1.75f, 1.6f, 3.5f},   {8, 2, 8, 2, 1.7f, 1.7f, 1.0f, 2.7f},
-    {16, 1, 8, 1, 1.63f, 1.29f, 0.92f, 3.2f}, {16, 2, 8, 1, 1.44f, 1.58f, 1.19f, 2.8f},
-    {16, 4, 8, 1, 1.5f, 1.8f, 1.88f, 2.9f},   {32, 2, 4, 1, 1.34f, 1.35f, 1.24f, 3.5f},
-    {32, 4, 4, 1, 0.93f, 2.15f, 1.82f, 4.0f}, {48, 2, 4, 1, 1.07f, 1.7f, 1.58f, 4.2f},
-    {48, 4, 4, 1, 0.57f, 2.6f, 2.29f, 4.9f}};
+    {8, 1, 16, 1, 1.31f, 2.15f, 1.29f, 3.68f}, {8, 2, 8, 2, 1.75f, 1.75f, 0.91f, 3.12f},
+    {16, 1, 8, 1, 1.5f, 1.56f, 0.84f, 3.31f},  {16, 2, 8, 1, 1.34f, 1.87f, 1.08f, 3.32f},
+    {16, 4, 8, 1, 1.75f, 1.75f, 1.8f, 3.14f},  {32, 2, 4, 1, 1.53f, 1.43f, 1.2f, 3.5f},
+    {32, 4, 4, 1, 1.21f, 2.13f, 1.82f, 4.12f}, {48, 2, 4, 1, 1.39f, 1.65f, 1.57f, 4.31f},
+    {48, 4, 4, 1, 0.97f, 2.54f, 2.3f, 5.2f}};
 constexpr StreamForm kStreamF32[] = {
-    {8, 1, 8, 1, 1.39f, 1.4f, 2.22f, 3.5f},   {8, 2, 8, 1, 1.22f, 1.7f, 2.71f, 2.8f},
-    {8, 4, 8, 1, 1.65f, 1.65f, 3.7f, 2.8f},   {16, 1, 4, 1, 1.5f, 1.45f, 1.46f, 3.3f},
-    {16, 2, 4, 1, 1.22f, 1.48f, 2.1f, 3.3f},  {16, 4, 4, 1, 0.84f, 2.11f, 2.76f, 3.4f},
-    {32, 2, 4, 1, 1.14f, 1.35f, 3.42f, 3.6f}};
+    {8, 1, 8, 1, 1.25f, 1.83f, 2.0f, 3.44f},   {8, 2, 8, 1, 1.22f, 2.05f, 2.46f, 3.41f},
+    {8, 4, 8, 1, 1.69f, 1.69f, 3.59f, 3.15f},  {16, 1, 4, 1, 1.5f, 1.45f, 1.46f, 3.3f},
+    {16, 2, 4, 1, 1.51f, 1.39f, 2.01f, 3.42f}, {16, 4, 4, 1, 1.22f, 1.79f, 2.78f, 3.5f},
+    {32, 2, 4, 1, 1.4f, 1.61f, 3.28f, 3.7f}};
 inline int stream_tiles(const StreamForm& f, int64_t T, int rows) {
     return (rows + 16 * f.nf - 1) / (16 * f.nf) * (int)((T + f.tm - 1) / f.tm);
 }
@@ -46,9 +48,10 @@ inline StreamForm stream_form(int64_t T, int cols, int k, bool pair, bool f32) {
     float least = 0;
     for (int i = 0; i < n; ++i) {
         const StreamForm& f = table[i];
-        // (where the fits hold; gate and up rows are two fragments at least)
+        // (where the fits hold; gate and up rows are two fragments at least, and of fp32 tokens 32 x 32 tiles
+        // are the best for none)
         if ((f.tm == 8 && T > 8) || (f.tm == 16 && T > 16 && !f32) || (f.tm > 16 && T <= 16) ||
-            (pair && f.nf == 1))
+            (pair && (f.nf == 1 || (f32 && f.tm == 32))))
             continue;
         const int tiles = stream_tiles(f, T, rows);
         for (int z = 1; z <= (pair ? 1 : kMostShares); z *= 2) {
@@ -69,10 +72,10 @@ inline StreamForm stream_form(int64_t T, int cols, int k, bool pair, bool f32) {
 // Whether the product [T, k] x [n, k] (block: the dense block of width n and h of width k) streams its
 // weights, by estimated time, or converts them first (the bytes at 5 TB/s, then the best dense form, and
 // 6 us for the launch and the dense form's reads of what was just written).  us, streamed / converted,
-// bf16: 256 tokens, 2048 to 8192 21 / 34, 384 29 / 35, 768 56 / 50; 8192 to 2048 384 23 / 38, 512
-// 34.5 / 36; fp32: 512 tokens, 8192 to 2048 109 / 179, 2048 to 16384 261 / 293.  (The choice between the
-// two was fitted before the streamed copies lost their bounds, so it converts a little early: at most
-// 4 % at these sizes.)  Up to kStreamedAlways tokens nothing is converted, so that small batches need no scratch for it.
+// bf16: 256 tokens, 2048 to 8192 22 / 34, 384 29 / 35, 768 58 / 50; 8192 to 2048 384 23 / 38, 512
+// 34.3 / 35.9, 2048 118 / 75; fp32, whose three bf16 products take less than one of fp32: 512 tokens,
+// 8192 to 2048 96 / 179, 2048 to 8192 4096 918 / 1064, 16384 4101 / 4161, but 512 to 4096 4096 264 / 158.
+// Up to kStreamedAlways tokens nothing is converted, so that small batches need no scratch for it.
 struct F4Plan {
     bool streams;
     StreamForm up, form;  // of a block's gate and up rows; of the projection, or of its down rows
@@ -86,7 +89,7 @@ inline size_t f4_part(const StreamForm& f, int tiles) {
 }
 inline F4Plan f4_plan(int64_t T, int n, int k, bool block, bool f32) {
     F4Plan p{T <= kStreamedAlways, {}, {}, 0, 0};
-    if (T > kMostStreamed) return p;
+    if (T > most_streamed(f32)) return p;
     p.form = stream_form(T, n, k, false, f32);
     if (block) p.up = stream_form(T, k, n, true, f32);
     auto converted = [&](int64_t rows, int64_t deep) {
@@ -111,7 +114,7 @@ inline F4Plan f4_plan(int64_t T, int n, int k, bool block, bool f32) {
 // tokens but the first, whose halves differ.
 inline size_t f4_part_reserve(int64_t T, int n, int k, bool f32) {
     size_t most = 0;
-    for (int64_t t = 8; t < T + 16 && t <= kMostStreamed; t += t == 8 ? 8 : 16) {
+    for (int64_t t = 8; t < T + 16 && t <= most_streamed(f32); t += t == 8 ? 8 : 16) {
         const int64_t at = t < T ? t : T;
         if (at < 1) break;
         const StreamForm f = stream_form(at, n, k, false, f32);

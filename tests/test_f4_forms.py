@@ -30,18 +30,21 @@ int main() {
 '''
 
 # (T, n, k, fp32): one for each tile, whole and in shares
-LINEAR = [(1, 48, 512, 0), (1, 16, 15552, 0), (1, 5120, 64, 0), (9, 496, 34976, 0), (9, 10000, 32, 0),
-          (9, 736, 52448, 0), (17, 48, 96, 0), (17, 16, 4608, 0), (17, 10000, 32, 0),
-          (17, 736, 52448, 0), (33, 5120, 32, 0), (33, 496, 34976, 0), (33, 10000, 32, 0),
-          (33, 736, 52448, 0), (1, 16, 4096, 0), (1, 16, 117984, 0), (1, 5120, 4096, 0),
-          (1, 496, 34976, 0), (1, 16, 32, 1), (1, 16, 4608, 1), (1, 5120, 32, 1), (1, 496, 23328, 1),
-          (1, 10000, 32, 1), (9, 736, 23328, 1), (17, 30496, 32, 1), (84, 144, 34976, 1),
-          (1, 16, 2048, 1), (1, 16, 52448, 1), (1, 5120, 2048, 1), (1, 496, 34976, 1),
-          (1, 10000, 2048, 1), (1, 736, 34976, 1)]
+LINEAR = [(1, 16, 6240, 0), (1, 16, 112256, 0), (1, 9984, 32, 0), (1, 736, 18880, 0),
+          (1, 16, 32, 0), (1, 16, 15104, 0), (1, 5120, 32, 0), (9, 736, 18880, 0),
+          (9, 9984, 32, 0), (9, 1216, 29472, 0), (17, 16, 32, 0), (17, 16, 4000, 0),
+          (100, 2896, 32, 0), (512, 176, 6240, 0), (130, 1696, 32, 0), (300, 208, 6240, 0),
+          (130, 3376, 32, 0), (300, 208, 15104, 0), (1, 16, 2048, 1), (1, 16, 36832, 1),
+          (1, 5120, 2048, 1), (1, 1216, 9696, 1), (1, 9984, 2048, 1), (1, 1216, 18880, 1),
+          (1, 16, 32, 1), (9, 16, 4000, 1), (300, 224, 32, 1), (130, 128, 4000, 1),
+          (700, 176, 32, 1), (200, 144, 6240, 1), (1500, 144, 32, 1), (300, 80, 15104, 1)]
 # (T, d, m, fp32)
-BLOCK = [(1, 32, 32, 0), (9, 32, 5120, 0), (17, 32, 32, 0), (17, 32, 5120, 0), (33, 32, 2176, 0),
-         (33, 32, 5120, 0), (1, 4096, 32, 0), (1, 32, 32, 1), (1, 32, 5120, 1), (17, 32, 15616, 1),
-         (1, 2048, 32, 1), (1, 2048, 5120, 1)]
+BLOCK = [(1, 2560, 32, 0), (1, 32, 32, 0), (9, 32, 5120, 0), (17, 32, 32, 0), (49, 32, 2176, 0),
+         (33, 32, 2176, 0), (130, 32, 1696, 0), (1, 2048, 32, 1), (1, 2048, 5120, 1),
+         (1, 32, 32, 1), (300, 32, 224, 1)]
+
+# (T, n, k, fp32): weights converted for the dense forms
+CONVERTED = [(384, 8192, 512, 0), (2100, 16, 32, 0), (3000, 4096, 512, 1), (9000, 48, 96, 1)]
 
 
 @pytest.fixture(scope="module")
@@ -74,6 +77,7 @@ def test_sizes_take_every_form(plans):
     met = {projection(p, s[3]) for p, s in zip(plans([s[:3] + (0, s[3]) for s in grid]), grid)
            if p[0]}
     assert met <= listed and len(listed) == len(LINEAR)
+    assert not any(p[0] for p in plans([s[:3] + (0, s[3]) for s in CONVERTED]))
     there = plans([s[:3] + (1, s[3]) for s in BLOCK])
     assert all(p[0] for p in there)
     listed = {(s[3],) + p[1:3] for p, s in zip(there, BLOCK)}
@@ -83,7 +87,7 @@ def test_sizes_take_every_form(plans):
 
 
 def test_scratch_is_within_what_is_reserved(plans):
-    sizes = [(T, n, k, b, f) for T in list(range(1, 100)) + [130, 257, 512, 900, 2048]
+    sizes = [(T, n, k, b, f) for T in list(range(1, 100)) + [130, 257, 512, 900, 2048, 5000, 8192]
              for n, k in ((64, 4608), (512, 8192), (2048, 8192), (736, 52448), (8192, 2048))
              for b in (0, 1) for f in (0, 1)]
     least = {}
@@ -106,7 +110,7 @@ def made(T, k, f32, seed):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("T,n,k,f32", LINEAR)
+@pytest.mark.parametrize("T,n,k,f32", LINEAR + CONVERTED + [(4100, 528, 2048, 1)])
 def test_linear_forms(T, n, k, f32):
     from paper_2608_04401_amd import binding as B
     x, weights = made(T, k, f32, n + k)
