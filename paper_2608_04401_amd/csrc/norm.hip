@@ -236,7 +236,9 @@ template <class T, int N, int KEEP, int RPB>
 __global__ __launch_bounds__(N* RPB) void norm_backward(NormIn<T> in, NormGradIn<T> gr) {
     constexpr int W = N * RPB / 64;
     __shared__ float sh[3][2][W];  // per sum and parity of the round
-    __shared__ float cols[3][RPB > 1 ? RPB * N * 8 : 1];
+    // a row's threads and eight words more, which put the eight columns of a thread in other banks
+    constexpr int CN = N + 8;
+    __shared__ float cols[3][RPB > 1 ? RPB * 8 * CN : 1];
     const int tid = threadIdx.x % N, sub = threadIdx.x / N, d = in.d;
     const float inv_d = 1.0f / (float)d;
     float acc[3][KEEP][8];
@@ -371,16 +373,16 @@ __global__ __launch_bounds__(N* RPB) void norm_backward(NormIn<T> in, NormGradIn
 #pragma unroll
             for (int j = 0; j < 3; ++j)
 #pragma unroll
-                for (int q = 0; q < 8; ++q) cols[j][(sub * 8 + q) * N + tid] = acc[j][i][q];
+                for (int q = 0; q < 8; ++q) cols[j][(sub * 8 + q) * CN + tid] = acc[j][i][q];
             __syncthreads();
             // 3 times 8 N sums by N RPB threads, in the order of the columns
 #pragma unroll
             for (int j = 0; j < 3; ++j)
                 for (int k = threadIdx.x; k < 8 * N; k += N * RPB) {
-                    const int at = k % 8 * N + k / 8;
+                    const int at = k % 8 * CN + k / 8;
                     float t = cols[j][at];
 #pragma unroll
-                    for (int p = 1; p < RPB; ++p) t += cols[j][p * 8 * N + at];
+                    for (int p = 1; p < RPB; ++p) t += cols[j][p * 8 * CN + at];
                     if (k < d && (gr.cols >> j & 1)) out[(int64_t)j * d + k] = t;
                 }
         } else {
