@@ -808,14 +808,20 @@ def elb_ffn_forward_f4(x, W_gate_up, gate_up_scale, W_down, down_scale, residual
     _want("gate_up_scale", gate_up_scale, (2 * m, d // 32), torch.uint8, dev)
     _want("W_down", W_down, (d, m // 2), torch.uint8, dev)
     _want("down_scale", down_scale, (d, m // 32), torch.uint8, dev)
-    _want("residual", residual, (T, d), x.dtype, dev)
-    _want("out", out, (T, d), x.dtype, dev)
-    y = torch.empty_like(x) if out is None else out
+    if residual is not None:
+        _want("residual", residual, (T, d), x.dtype, dev)
+    if out is None:
+        y = torch.empty_like(x)
+    else:
+        _want("out", out, (T, d), x.dtype, dev)
+        y = out
     stream = _stream()
-    ws = workspace(elb_ffn_f4_workspace_bytes(T, d, m, dt), x.device, stream)
-    _check("elb_ffn_forward_f4", lib().elb_ffn_forward_f4(
-        _ptr(x), _ptr(W_gate_up), _ptr(gate_up_scale), _ptr(W_down), _ptr(down_scale),
-        _ptr(residual), T, d, m, dt, _ptr(y), _ptr(ws), ws.numel(), stream))
+    ws, nb = _scratch(elb_ffn_f4_workspace_bytes(T, d, m, dt), x.device, stream)
+    status = lib().elb_ffn_forward_f4(
+        x.data_ptr(), W_gate_up.data_ptr(), gate_up_scale.data_ptr(), W_down.data_ptr(),
+        down_scale.data_ptr(), _ptr(residual), T, d, m, dt, y.data_ptr(), ws, nb, stream)
+    if status:
+        _check("elb_ffn_forward_f4", status)
     return y
 
 
