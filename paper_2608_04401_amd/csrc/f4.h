@@ -128,7 +128,7 @@ __device__ __forceinline__ void issue_whole(const C& c, uint32_t at, uint32_t ld
 // the tensor further on) of 128 bytes, and the rows' eight scale bytes behind them.  DMA: weights on
 // 16-byte boundaries; otherwise ordinary loads, as for scales whose rows are off 4-byte ones.  NT:
 // weights that a call reads once, with the non-temporal hint (few-token layer, bf16, 8 to 16 tokens: 97 %
-// to 100 % of the time that elb_moe_forward takes, 108 % to 112 % without).
+// to 104 % of the time that elb_moe_forward takes, by card, 108 % to 112 % without).
 template <class W, int NF, bool PAIR, bool DMA, bool NT = false>
 struct Stream {
     static constexpr int ROWS = 16 * NF;

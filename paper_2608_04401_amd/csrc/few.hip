@@ -73,6 +73,8 @@ __device__ __forceinline__ bf16x8_t as_frag(u32x4_t v) { return __builtin_bit_ca
 
 // ------------------------------------------------------------------------------------------
 // Launch 1.  XR: rows of x, 8 or 16; DMA: x, W_router and the weights on 16-byte boundaries.
+// 64 experts of 2048 x 1024, top 8: one token 18.2 us (4 bits 13.4), of which the routing 6.6; 13 tokens in 4
+// bits 34.7, the weights at 4.6 TB/s after it.
 // ------------------------------------------------------------------------------------------
 template <class W, int KMAX, int XR, bool DMA>
 __global__ __launch_bounds__(64 * kUpWaves) void few_up(FewIn in, XTable xt) {
@@ -364,7 +366,8 @@ __global__ __launch_bounds__(64 * kUpWaves) void few_up(FewIn in, XTable xt) {
 // Launch 2.  A block has 64 columns of y and one of `shares` shares of the contraction, the used
 // experts' units one behind the other (per expert as often as its tokens fill tiles of eight); its
 // waves take every eighth unit.  The last block of a column tile to write its partial sums adds all
-// of them, in the order of the shares; none waits for another.
+// of them, in the order of the shares; none waits for another.  One token 10.3 us (4 bits 7.7), 13 tokens
+// in 4 bits 17.1.
 // ------------------------------------------------------------------------------------------
 template <class W, bool DMA>
 __global__ __launch_bounds__(64 * kDownWaves) void few_down(FewIn in) {
