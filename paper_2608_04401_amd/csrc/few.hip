@@ -15,7 +15,7 @@ namespace elb {
 
 namespace {
 
-constexpr int kUpWaves = 8, kDownWaves = 8;  // (routing by counting: a token a wave, up to 8)
+constexpr int kUpWaves = 8, kDownWaves = 8;
 
 // The experts that some token has selected (list[0 .. used)), and of each its tokens: a bit for each,
 // the slot t K + j of each (where its bit is set), and their slots in order.
@@ -87,8 +87,8 @@ __global__ __launch_bounds__(64 * kUpWaves) void few_up(FewIn in, XTable xt) {
     __shared__ __attribute__((aligned(1024))) char sm[kUpWaves * SLOT];
     __shared__ float logits[RW][16 * 65];
     __shared__ Slots slots;
-    __shared__ float sorted[kUpWaves][64];
-    __shared__ int order[kUpWaves][64], rank[kUpWaves][64];
+    __shared__ float sorted[XR][64];
+    __shared__ int order[XR][64], rank[XR][64];
     __shared__ int sk[16], sids[16 * kLaneMaxK];
     __shared__ float sw[16 * kLaneMaxK];
     const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, hq = lane >> 4;
@@ -99,7 +99,7 @@ __global__ __launch_bounds__(64 * kUpWaves) void few_up(FewIn in, XTable xt) {
 
     if (blockIdx.x == 0)
         for (int i = tid; i < d / 64; i += 64 * kUpWaves) in.count[i] = 0;
-    rank[wave][lane] = 0;
+    for (int i = wave; i < XR; i += kUpWaves) rank[i][lane] = 0;
 
     // the tokens' operands of this wave's share of the contraction, where it is at most 256 long
     const int units = (d + W::KU - 1) / W::KU;
@@ -190,22 +190,26 @@ __global__ __launch_bounds__(64 * kUpWaves) void few_up(FewIn in, XTable xt) {
     }
     ELB_WAIT_VMCNT(0);  // the last copies, before their LDS is used again; and x
     __syncthreads();
-    if constexpr (XR == 8) {
-        // Waves share a token, a lane per expert: its logit, and its rank by counting the (key, id) pairs
-        // before it, in the order of route_token_x16's network (one token: 3.4 us from here to the
-        // selection, 4.5 by that).
-        const int parts = T > 4 ? 1 : T > 2 ? 2 : T > 1 ? 4 : 8;  // waves a token
-        const int t = wave / parts, part = wave % parts;
-        float key = 0.0f;
-        if (t < T) {
+    // A lane per expert has its logit, and its rank by counting the (key, id) pairs before it, in the
+    // order of route_token_x16's network: a token or two a wave, or several waves a token (from here to
+    // the selection, one token 3.4 us, 4.5 by the network; from 9 tokens on the two take as long).
+    {
+        const int parts = XR > 8 || T > 4 ? 1 : T > 2 ? 2 : T > 1 ? 4 : 8;  // waves a token
+        const int part = wave % parts;
+        float key[XR / 8];
+#pragma unroll
+        for (int h = 0; h < XR / 8; ++h) {
+            const int t = 8 * h + wave / parts;
+            key[h] = 0.0f;
+            if (t >= T) continue;
             float l = -INFINITY;
             if (lane < N) {
                 l = logits[0][t * 65 + lane];
 #pragma unroll
                 for (int q = 1; q < RW; ++q) l += logits[q][t * 65 + lane];
             }
-            key = N == 64 ? order_key(l) : order_key_any(l);
-            const int image = ord_flip32(__float_as_int(key));
+            key[h] = N == 64 ? order_key(l) : order_key_any(l);
+            const int image = ord_flip32(__float_as_int(key[h]));
             const int64_t mine = ((int64_t)image << 32) | (uint32_t)(63 - lane);
             int before = 0;
             const int n = 64 / parts;
@@ -220,45 +224,29 @@ __global__ __launch_bounds__(64 * kUpWaves) void few_up(FewIn in, XTable xt) {
             atomicAdd(&rank[t][lane], before);
         }
         __syncthreads();
-        if (t < T && part == 0) {
-            const int r = rank[t][lane];
-            sorted[t][r] = key;
-            order[t][r] = lane;
+        if (part == 0) {
+#pragma unroll
+            for (int h = 0; h < XR / 8; ++h) {
+                const int t = 8 * h + wave / parts;
+                if (t >= T) continue;
+                const int r = rank[t][lane];
+                sorted[t][r] = key[h];
+                order[t][r] = lane;
+            }
         }
         __syncthreads();
-        if (tid < 16 * kUpWaves) {  // whole waves: 16 lanes a token
+        if (tid < 16 * XR) {  // whole waves: 16 lanes a token
             const int t = tid >> 4, sl = tid & 15;
-            float key[4];
+            float k4[4];
             int id[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                key[i] = sorted[t][4 * sl + i];
+                k4[i] = sorted[t][4 * sl + i];
                 id[i] = order[t][4 * sl + i];
             }
-            route_sorted_x16<KMAX>(key, id, N, K, in.eps, in.mode, in.renorm, xt, t, t < T, sk,
-                                   sids, sw);
+            route_sorted_x16<KMAX>(k4, id, N, K, in.eps, in.mode, in.renorm, xt, t, t < T, sk, sids,
+                                   sw);
         }
-    } else {
-        const int t = tid >> 4, sl = tid & 15;
-        if (tid < 256) {  // whole waves: 16 lanes a token
-            float l4[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int n = 4 * sl + i;
-                l4[i] = -INFINITY;
-                if (n < N) {
-                    l4[i] = logits[0][t * 65 + n];
-#pragma unroll
-                    for (int q = 1; q < RW; ++q) l4[i] += logits[q][t * 65 + n];
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) logits[0][t * 65 + 4 * sl + i] = l4[i];
-        }
-        __syncthreads();
-        if (tid < 256)
-            route_token_x16<KMAX>(logits[0] + t * 65, N, K, in.eps, in.mode, in.renorm, xt, t, t < T,
-                                  sk, sids, sw);
     }
     __syncthreads();
     if (blockIdx.x == 0) {
