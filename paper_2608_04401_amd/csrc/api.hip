@@ -1098,8 +1098,8 @@ static FewLayout few_layout(int64_t T, int d, int m, int K) {
     L.ids = L.k + align_up((size_t)T * 4);
     L.w = L.ids + align_up(rows * 4);
     L.part = L.w + align_up(rows * 4);
-    L.count = L.part + (size_t)(d / 64) * few_shares(d) * 4096;
-    L.total = L.count + align_up((size_t)(d / 64) * 4);
+    L.count = L.part + few_part_bytes(d);
+    L.total = L.count + align_up((size_t)few_tiles(d) * 4);
     return L;
 }
 

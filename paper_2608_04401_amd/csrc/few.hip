@@ -15,7 +15,8 @@ namespace elb {
 
 namespace {
 
-constexpr int kUpWaves = 8, kDownWaves = 8;
+constexpr int kUpWaves = 8, kDownWaves = 16;
+constexpr int kDownFrags = 2;  // of 16 columns, a block of launch 2
 
 // The experts that some token has selected (list[0 .. used)), and of each its tokens: a bit for each,
 // the slot t K + j of each (where its bit is set), and their slots in order.
@@ -63,7 +64,7 @@ struct FewIn {
     bf16_t* y;
     int *k, *ids;
     float* w;
-    float* part;  // partial sums of launch 2 [column tiles, shares, 16, 64], and
+    float* part;  // partial sums of launch 2 [column tiles, shares, 16, columns], and
     int* count;   // how many of a column tile's are written (zeroed by launch 1)
     int shares;
 };
@@ -98,7 +99,7 @@ __global__ __launch_bounds__(64 * kUpWaves) void few_up(FewIn in, XTable xt) {
     const uint32_t lds = lds_address(slot);
 
     if (blockIdx.x == 0)
-        for (int i = tid; i < d / 64; i += 64 * kUpWaves) in.count[i] = 0;
+        for (int i = tid; i < d / (16 * kDownFrags); i += 64 * kUpWaves) in.count[i] = 0;
     for (int i = wave; i < XR; i += kUpWaves) rank[i][lane] = 0;
 
     // the tokens' operands of this wave's share of the contraction, where it is at most 256 long
@@ -351,18 +352,19 @@ __global__ __launch_bounds__(64 * kUpWaves) void few_up(FewIn in, XTable xt) {
 }
 
 // ------------------------------------------------------------------------------------------
-// Launch 2.  A block has 64 columns of y and one of `shares` shares of the contraction, the used
+// Launch 2.  A block has 32 columns of y and one of `shares` shares of the contraction, the used
 // experts' units one behind the other (per expert as often as its tokens fill tiles of eight); its
-// waves take every eighth unit.  The last block of a column tile to write its partial sums adds all
-// of them, in the order of the shares; none waits for another.  One token 10.3 us (4 bits 7.7), 13 tokens
-// in 4 bits 17.1.
+// waves take every sixteenth unit.  The last block of a column tile to write its partial sums adds all
+// of them, in the order of the shares; none waits for another.  64 experts of 2048 x 1024, top 8: one
+// token 9.8 us (4 bits 7.5), 13 tokens in 4 bits 16.5 (64 columns and eight waves: 10.2, 8.0, 17.1).
 // ------------------------------------------------------------------------------------------
 template <class W, bool DMA>
 __global__ __launch_bounds__(64 * kDownWaves) void few_down(FewIn in) {
-    typedef Stream<W, 4, false, DMA, true> B;
+    constexpr int NF = kDownFrags, COLS = 16 * NF;
+    typedef Stream<W, NF, false, DMA, true> B;
     constexpr int SUB = W::KU / 64, AB = SUB * 8 * 128;  // eight rows of h
     constexpr int SLOT = (AB + B::BYTES + 255) / 256 * 256;
-    static_assert(SLOT >= 4096, "");
+    static_assert(SLOT >= NF * 1024, "");
     __shared__ __attribute__((aligned(1024))) char sm[kDownWaves * SLOT];
     __shared__ Slots slots;
     __shared__ int last;
@@ -377,7 +379,7 @@ __global__ __launch_bounds__(64 * kDownWaves) void few_down(FewIn in) {
     const int v0 = units * share / in.shares + wave, v1 = units * (share + 1) / in.shares;
     const int64_t w_bytes = W::row_bytes((int64_t)d * m);
     B b0;
-    b0.init(in.down, in.d_scale, 64 * tile, 64, 0, d, m, lane);
+    b0.init(in.down, in.d_scale, COLS * tile, COLS, 0, d, m, lane);
     // rows of h: chunk lane % 8 of row lane / 8, in each of the unit's k-tiles of 64
     const uint64_t hb = (uint64_t)in.h;
     const u32x4_t hr = {uniform((uint32_t)hb), uniform((uint32_t)(hb >> 32)) & 0xffffu,
@@ -402,9 +404,9 @@ __global__ __launch_bounds__(64 * kDownWaves) void few_down(FewIn in) {
         }
         return e;
     };
-    f32x4_t acc[4];
+    f32x4_t acc[NF];
 #pragma unroll
-    for (int f = 0; f < 4; ++f) acc[f] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    for (int f = 0; f < NF; ++f) acc[f] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     int pass = 0, e = v0 < v1 ? issue(v0, 0) : 0;
     for (int v = v0; v < v1;) {
         ELB_WAIT_VMCNT(0);
@@ -414,12 +416,12 @@ __global__ __launch_bounds__(64 * kDownWaves) void few_down(FewIn in) {
         const int rank = __popc(tokens & ((1u << l16) - 1)) - 8 * pass;
         const bool live = (tokens >> l16 & 1) && rank >= 0 && rank < 8;
         const int r = live ? rank : 0;
-        typename W::Half w[4][2];
+        typename W::Half w[NF][2];
         u32x4_t x[2][W::J];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
 #pragma unroll
-            for (int f = 0; f < 4; ++f) W::read(w[f][h], slot + AB, 64, f, h, l16, hq);
+            for (int f = 0; f < NF; ++f) W::read(w[f][h], slot + AB, COLS, f, h, l16, hq);
 #pragma unroll
             for (int i = 0; i < W::J; ++i) {
                 const int run = h * W::J + i;  // of 32 values
@@ -445,7 +447,7 @@ __global__ __launch_bounds__(64 * kDownWaves) void few_down(FewIn in) {
                 if (k0 + (h * W::J + i) * 32 >= m) break;
                 if (!live) x[h][i] = u32x4_t{0, 0, 0, 0};
 #pragma unroll
-                for (int f = 0; f < 4; ++f)
+                for (int f = 0; f < NF; ++f)
                     acc[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[f][h].get(i),
                                                                      as_frag(x[h][i]), acc[f], 0, 0,
                                                                      0);
@@ -453,11 +455,11 @@ __global__ __launch_bounds__(64 * kDownWaves) void few_down(FewIn in) {
     }
     f32x4_t* const part = reinterpret_cast<f32x4_t*>(slot);
 #pragma unroll
-    for (int f = 0; f < 4; ++f) part[f * 64 + lane] = acc[f];
+    for (int f = 0; f < NF; ++f) part[f * 64 + lane] = acc[f];
     __syncthreads();
-    // value i: token i / 64, column i % 64
+    // value i: token i / COLS, column i % COLS
     auto sum = [&](int i) {
-        const int t = i >> 6, col = i & 63;
+        const int t = i / COLS, col = i % COLS;
         const int at = ((col >> 4) * 64 + ((col & 15) >> 2) * 16 + t) * 4 + (col & 3);
         float v = reinterpret_cast<const float*>(sm)[at];
 #pragma unroll
@@ -465,21 +467,21 @@ __global__ __launch_bounds__(64 * kDownWaves) void few_down(FewIn in) {
             v += reinterpret_cast<const float*>(sm + q * SLOT)[at];
         return v;
     };
-    float* const mine = in.part + (int64_t)tile * in.shares * 1024;
+    float* const mine = in.part + (int64_t)tile * in.shares * (16 * COLS);
     auto put = [&](int i, float v) {
-        const int64_t o = (int64_t)(i >> 6) * d + 64 * tile + (i & 63);
+        const int64_t o = (int64_t)(i / COLS) * d + COLS * tile + i % COLS;
         if (in.residual) v += bf16_to_f32(in.residual[o]);
         in.y[o] = f32_to_bf16(v);
     };
     if (in.shares == 1) {
-        for (int i = tid; i < T * 64; i += 64 * kDownWaves) put(i, sum(i));
+        for (int i = tid; i < T * COLS; i += 64 * kDownWaves) put(i, sum(i));
         return;
     }
     // The partial sums go past the L2, which blocks elsewhere on the chip do not share: agent-scope
     // stores, done when the counter goes up, and agent-scope loads: 2.5 us of a token's 7.  (A release
     // fence would write the whole L2 back, for each block: 31 us more.)
-    for (int i = tid; i < T * 64; i += 64 * kDownWaves)
-        __hip_atomic_store(mine + share * 1024 + i, sum(i), __ATOMIC_RELAXED,
+    for (int i = tid; i < T * COLS; i += 64 * kDownWaves)
+        __hip_atomic_store(mine + share * (16 * COLS) + i, sum(i), __ATOMIC_RELAXED,
                            __HIP_MEMORY_SCOPE_AGENT);
     ELB_WAIT_VMCNT(0);
     __syncthreads();
@@ -488,11 +490,11 @@ __global__ __launch_bounds__(64 * kDownWaves) void few_down(FewIn in) {
                                       __HIP_MEMORY_SCOPE_AGENT) == in.shares - 1;
     __syncthreads();
     if (!last) return;
-    for (int i = tid; i < T * 64; i += 64 * kDownWaves) {
+    for (int i = tid; i < T * COLS; i += 64 * kDownWaves) {
         float p[16], v = 0.f;
 #pragma unroll
         for (int q = 0; q < 16; ++q)
-            p[q] = q < in.shares ? __hip_atomic_load(mine + q * 1024 + i, __ATOMIC_RELAXED,
+            p[q] = q < in.shares ? __hip_atomic_load(mine + q * (16 * COLS) + i, __ATOMIC_RELAXED,
                                                      __HIP_MEMORY_SCOPE_AGENT)
                                  : 0.f;
 #pragma unroll
@@ -521,17 +523,21 @@ hipError_t few(const FewIn& in, int cus, hipStream_t s) {
         if (hipError_t e = hipGetLastError()) return e;
     }
     ProfileScope prof("few_down", s);
-    ELB_LAUNCH((few_down<W, DMA>), dim3(in.d / 64, in.shares), dim3(64 * kDownWaves), 0, s, in);
+    ELB_LAUNCH((few_down<W, DMA>), dim3(few_tiles(in.d), in.shares), dim3(64 * kDownWaves), 0, s,
+               in);
     return hipGetLastError();
 }
 
 }  // namespace
 
 // shares of launch 2's contraction: so many that its blocks fill the compute units
+int few_tiles(int d) { return d / (16 * kDownFrags); }
 int few_shares(int d) {
-    const int n = 256 / (d / 64);
+    const int n = 256 / few_tiles(d);
     return n < 1 ? 1 : n > 16 ? 16 : n;
 }
+
+size_t few_part_bytes(int d) { return (size_t)few_shares(d) * 16 * d * 4; }
 
 hipError_t launch_moe_few(const void* x, const void* Wr, const void* Wgu, const uint8_t* gu_scale,
                           const void* Wd, const uint8_t* d_scale, const void* res, int64_t T, int d,
