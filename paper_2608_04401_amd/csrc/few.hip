@@ -6,8 +6,8 @@
 // All tokens are one MFMA tile of 16 rows.  In launch 1 every block routes all of them for itself (the
 // same bits as the other router paths: the same chains, sums and per-token code), instead of waiting
 // for a launch that does, and then takes its share of the used experts' gate and up rows.  In launch 2
-// the experts lie one behind the other in one long contraction: a token's h is zero for experts that it
-// has not selected, its routing weight is in h already, so the products' sum is the combine.
+// the experts lie one behind the other in one long contraction, of which a token's sums take what belongs
+// to experts that it has selected; its routing weight is in h already, so the products' sum is the combine.
 #include "f4.h"
 #include "route_lane.h"
 
@@ -440,18 +440,26 @@ __global__ __launch_bounds__(64 * kDownWaves) void few_down(FewIn in) {
         }
         if (v < v1) e = issue(v, pass);
         __builtin_amdgcn_sched_barrier(0);
+        // A lane's sums are those of token l16: where that has not selected the expert they stay what they
+        // were.  (Zeros for its h would not do: 0 times a weight that is infinite or NaN is NaN.)
+        f32x4_t sum[NF];
+#pragma unroll
+        for (int f = 0; f < NF; ++f) sum[f] = acc[f];
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int i = 0; i < W::J; ++i) {
                 if (k0 + (h * W::J + i) * 32 >= m) break;
-                if (!live) x[h][i] = u32x4_t{0, 0, 0, 0};
 #pragma unroll
                 for (int f = 0; f < NF; ++f)
-                    acc[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[f][h].get(i),
-                                                                     as_frag(x[h][i]), acc[f], 0, 0,
+                    sum[f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[f][h].get(i),
+                                                                     as_frag(x[h][i]), sum[f], 0, 0,
                                                                      0);
             }
+#pragma unroll
+        for (int f = 0; f < NF; ++f)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) acc[f][q] = live ? sum[f][q] : acc[f][q];
     }
     f32x4_t* const part = reinterpret_cast<f32x4_t*>(slot);
 #pragma unroll

@@ -123,6 +123,48 @@ def test_a_token_alone_and_nan():
         assert bool((d <= 2.0 ** -7 * (1 + y[keep].float().abs())).all())
 
 
+@pytest.mark.parametrize("weights", ["bf16", "f4"])
+@pytest.mark.parametrize("T", [2, 9, 16])
+def test_weights_that_are_no_number_stay_with_their_tokens(T, weights):
+    """An infinity or a NaN among an expert's weights reaches the tokens that have selected it, a weight of
+    the down product in its own column alone; everything else keeps its bits.  (Rows of y in several shares
+    of the contraction and in one; an expert of more than eight tokens, which takes two passes.)"""
+    for d, N, m, K, mode in ((128, 16, 64, 4, B.MODE_ELBOW), (512, 64, 320, 8, B.MODE_ELBOW),
+                             (256, 16, 192, 12, B.MODE_TOPK), (4160, 5, 64, 2, B.MODE_TOPK)):
+        v = layer(T, d, N, m, weights)
+        kw = {"K": K, "mode": mode, "residual": v["residual"]}
+        y, r = call(v, debug=True, **kw)
+        torch.cuda.synchronize()
+        on = (r["ids"][None] == torch.arange(N, device="cuda")[:, None, None]).any(-1)  # [N, T]
+        tokens = on.sum(1)
+        e = int(torch.where(tokens < T, tokens, -1).argmax())
+        assert 0 < tokens[e] < T, (d, N)
+        cols = [5, d - 3]
+        w = dict(v, scales={k: t.clone() for k, t in v["scales"].items()})
+        if weights == "f4":
+            w["scales"]["down_scale"][e, cols[0], 0] = 255
+            w["scales"]["down_scale"][e, cols[1], -1] = 255
+        else:
+            w["W_down"] = v["W_down"].clone()
+            w["W_down"][e, cols[0], 3] = float("inf")
+            w["W_down"][e, cols[1], m - 1] = float("nan")
+        bad = call(w, **kw)
+        torch.cuda.synchronize()
+        hit = torch.zeros_like(y, dtype=torch.bool)
+        hit[:, cols] = on[e][:, None]
+        assert torch.equal(bad[~hit], y[~hit]), (d, N)
+        assert not bool(bad[hit].isfinite().any()), (d, N)
+        w = dict(v, scales={k: t.clone() for k, t in v["scales"].items()})
+        if weights == "f4":
+            w["scales"]["gate_up_scale"][e, 3, -1] = 255
+        else:
+            w["W_gate_up"] = v["W_gate_up"].clone()
+            w["W_gate_up"][e, m + 3, 7] = float("nan")
+        bad = call(w, **kw)
+        torch.cuda.synchronize()
+        assert torch.equal(bad[~on[e]], y[~on[e]]) and bool(bad[on[e]].isnan().all()), (d, N)
+
+
 def test_no_tokens():
     v = layer(1, 64, 8, 64, "bf16")
     assert call(v, x=v["x"][:0].contiguous(), K=2).shape == (0, 64)
