@@ -412,7 +412,8 @@ typedef struct {
  *   sum    [T, d] dtype  output, or NULL: not written; may be residual
  *   normed [T, d] dtype  output; NULL exactly where w_pre is
  *   r_post [T], r_pre [T] float  optional outputs (NULL: not written), for elb_norm_backward; r_post
- *                        is written only with w_post, r_pre only with w_pre
+ *                        is written only with w_post, r_pre only with w_pre.  Of a root mean square
+ *                        above 2^126 they are subnormal numbers, with digits to 2^-149
  * Apart from sum and residual, outputs share memory with no other tensor.
  */
 int elb_norm_forward(const elb_norm *op, void *sum, void *normed, float *r_post, float *r_pre,

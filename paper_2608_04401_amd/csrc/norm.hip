@@ -71,8 +71,9 @@ __device__ __forceinline__ void row_sum2(float& v, float& u, float* sh, float* s
     }
 }
 
-// 1 / sqrt(mean of v^2 + eps) of a row.  A sum of squares past fp32's range is taken again of v 2^-64,
-// whose root is in range (the branch is the same for all that work on the row).
+// 1 / sqrt(mean of v^2 + eps) of a row.  A sum of squares past fp32's range is taken again of v 2^-72:
+// the largest squares are below 2^112 then, and 16384 of them below 2^126 (the branch is the same for all
+// that work on the row).
 template <int N, int KEEP>
 __device__ __forceinline__ float row_rstd(const float (&v)[KEEP][8], int d, float eps, float* sh) {
     float a = 0.0f;
@@ -87,12 +88,12 @@ __device__ __forceinline__ float row_rstd(const float (&v)[KEEP][8], int d, floa
     for (int i = 0; i < KEEP; ++i)
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
-            const float t = v[i][q] * 0x1p-64f;
+            const float t = v[i][q] * 0x1p-72f;
             a = fmaf(t, t, a);
         }
     if (N > 64) __syncthreads();
     a = row_sum<N>(a, sh);
-    return 0x1p-64f / sqrtf(a / (float)d);
+    return 0x1p-72f / sqrtf(a / (float)d);
 }
 
 // Eight values as loaded, in as many registers as they have words (dense.h's Eight lets the compiler

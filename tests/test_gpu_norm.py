@@ -136,6 +136,63 @@ def test_magnitudes(std):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("d", [16, 64, 1040, 2048, 9008, 16384])
+def test_rows_up_to_the_largest_numbers(d, dtype):
+    """Rows whose sum of squares passes fp32's range, up to the largest numbers, through either norm and
+    back.  r of a root mean square above 2^126 is a subnormal number: off by half of 2^-149, 2^-22 of the
+    least r (2^-128) and so of what it is a factor of."""
+    sub = 2.0 ** -22
+    g = torch.Generator(device="cuda")
+    g.manual_seed(d)
+    n = lambda *s: torch.randn(s, generator=g, device="cuda")
+    w = (1 + 0.3 * n(d)).to(dtype)
+    for size in (1e18, 3e36, 7e36, 1e37, 8e37, 3e38):
+        x = size * (0.5 + 0.5 * torch.rand((3, d), generator=g, device="cuda"))
+        x[0] = size
+        x = (x * n(3, d).sign()).to(dtype)
+        # (x as the residual, and as a block's output, halved)
+        for v in ({"residual": x}, {"block": x, "block_scale": 0.5}):
+            alpha, beta = 1.0, v.get("block_scale", 1.0)
+            total, normed, kept = B.elb_norm_forward(w_pre=w, keep=True, **v)
+            torch.cuda.synchronize()
+            s, nn, r = R.norm_forward(v.get("residual"), v.get("block"), None, w, None, alpha, beta, EPS)
+            within(total, *s, label="%g" % size)
+            within(normed, nn[0], nn[1] + 1.01 * sub * nn[0].abs(), label="%g" % size)
+            off = (kept[1].double() - r[1]).abs() / r[1]
+            assert float(off.max()) <= R.ROW + 8 * R.U24 + sub, size
+            # gradients as large as keep those of the rows in the normal range
+            d_normed = (1e20 * n(3, d)).to(dtype)
+            grads = B.elb_norm_backward(None, d_normed, total, v.get("block"), kept, w_pre=w,
+                                        block_scale=beta)
+            want = R.norm_backward(None, d_normed, total, v.get("block"), kept, None, w, None, alpha,
+                                   beta)
+            torch.cuda.synchronize()
+            for got, ref in zip(grads, want):
+                assert (got is None) == (ref is None)
+                if got is not None:
+                    within(got, *ref, label="%g" % size)
+        res = n(3, d).to(dtype)
+        total, normed, kept = B.elb_norm_forward(res, x, w, w, keep=True)
+        torch.cuda.synchronize()
+        s, nn, r = R.norm_forward(res, x, w, w, None, 1.0, 1.0, EPS)
+        p = (s[0] - res.double()).abs()
+        within(total, s[0], s[1] + 1.01 * sub * p, label="%g" % size)
+        # of s: sub at most of p, and through the mean of squares as much again of the row's largest
+        rel = sub * (p.amax(-1) / s[0].square().mean(-1).sqrt())[:, None]
+        within(normed, nn[0], nn[1] + 1.01 * (sub * p * r[1][:, None] * w.double().abs() +
+                                              rel * nn[0].abs()), label="%g" % size)
+        d_sum = (1e20 * n(3, d)).to(dtype)
+        grads = B.elb_norm_backward(d_sum, None, total, x, kept, w, w)
+        want = R.norm_backward(d_sum, None, total, x, kept, w, w, None, 1.0, 1.0)
+        torch.cuda.synchronize()
+        for got, ref in zip(grads, want):
+            assert (got is None) == (ref is None)
+            if got is not None:
+                within(got, *ref, label="%g" % size)
+
+
+@pytest.mark.gpu
 def test_a_row_alone_and_what_lies_around():
     """A row's results do not depend on the batch; nothing beside the outputs is written; a NaN or
     an infinity stays in its row."""
