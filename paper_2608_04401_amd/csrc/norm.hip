@@ -71,9 +71,9 @@ __device__ __forceinline__ void row_sum2(float& v, float& u, float* sh, float* s
     }
 }
 
-// 1 / sqrt(mean of v^2 + eps) of a row.  A sum of squares past fp32's range is taken again of v 2^-72:
-// the largest squares are below 2^112 then, and 16384 of them below 2^126 (the branch is the same for all
-// that work on the row).
+// 1 / sqrt(mean of v^2 + eps) of a row.  Where that leaves fp32's range it is taken again of v 2^-72 and
+// eps 2^-144: the largest squares are below 2^112 then, and 16384 of them below 2^126 (the branch is the
+// same for all that work on the row).
 template <int N, int KEEP>
 __device__ __forceinline__ float row_rstd(const float (&v)[KEEP][8], int d, float eps, float* sh) {
     float a = 0.0f;
@@ -82,7 +82,8 @@ __device__ __forceinline__ float row_rstd(const float (&v)[KEEP][8], int d, floa
 #pragma unroll
         for (int q = 0; q < 8; ++q) a = fmaf(v[i][q], v[i][q], a);
     a = row_sum<N>(a, sh);
-    if (__builtin_expect(a < INFINITY, 1)) return 1.0f / sqrtf(a / (float)d + eps);
+    const float ms = a / (float)d + eps;
+    if (__builtin_expect(ms < INFINITY, 1)) return 1.0f / sqrtf(ms);
     a = 0.0f;
 #pragma unroll
     for (int i = 0; i < KEEP; ++i)
@@ -93,7 +94,7 @@ __device__ __forceinline__ float row_rstd(const float (&v)[KEEP][8], int d, floa
         }
     if (N > 64) __syncthreads();
     a = row_sum<N>(a, sh);
-    return 0x1p-72f / sqrtf(a / (float)d);
+    return 0x1p-72f / sqrtf(a / (float)d + eps * 0x1p-72f * 0x1p-72f);
 }
 
 // Eight values as loaded, in as many registers as they have words (dense.h's Eight lets the compiler

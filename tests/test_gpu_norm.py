@@ -193,6 +193,21 @@ def test_rows_up_to_the_largest_numbers(d, dtype):
 
 
 @pytest.mark.gpu
+def test_a_large_eps():
+    """eps counts beside a sum of squares past fp32's range, and so does its own sum with the mean."""
+    for d in (64, 2048, 16384):
+        for size, eps in ((1e19, 3e38), (1.7e19, 3e38), (1e25, 3e38), (1e-3, 3e38), (1e20, 1e35)):
+            x = inputs(3, d, F32, "none", std=size)["residual"]
+            w = torch.ones(d, device="cuda")
+            _, normed = B.elb_norm_forward(x, w_pre=w, eps=eps)
+            torch.cuda.synchronize()
+            # (eps as the call takes it, in fp32)
+            eps = float(torch.tensor(eps, dtype=F32))
+            within(normed, *R.norm_forward(x, None, None, w, None, 1.0, 1.0, eps)[1],
+                   label="%g %g" % (size, eps))
+
+
+@pytest.mark.gpu
 def test_a_row_alone_and_what_lies_around():
     """A row's results do not depend on the batch; nothing beside the outputs is written; a NaN or
     an infinity stays in its row."""
