@@ -72,8 +72,9 @@ __device__ __forceinline__ void row_sum2(float& v, float& u, float* sh, float* s
 }
 
 // 1 / sqrt(mean of v^2 + eps) of a row.  Where that leaves fp32's range it is taken again of v 2^-72 and
-// eps 2^-144: the largest squares are below 2^112 then, and 16384 of them below 2^126 (the branch is the
-// same for all that work on the row).
+// eps 2^-144: the largest squares are below 2^112 then, and 16384 of them below 2^126.  Near the lower end
+// (eps and the row both tiny), where squares lose digits, of v 2^72 and eps 2^144: less than 2^42 and at
+// least 2^-5.  (The branch is the same for all that work on the row.)
 template <int N, int KEEP>
 __device__ __forceinline__ float row_rstd(const float (&v)[KEEP][8], int d, float eps, float* sh) {
     float a = 0.0f;
@@ -83,18 +84,19 @@ __device__ __forceinline__ float row_rstd(const float (&v)[KEEP][8], int d, floa
         for (int q = 0; q < 8; ++q) a = fmaf(v[i][q], v[i][q], a);
     a = row_sum<N>(a, sh);
     const float ms = a / (float)d + eps;
-    if (__builtin_expect(ms < INFINITY, 1)) return 1.0f / sqrtf(ms);
+    if (__builtin_expect(ms < INFINITY && ms >= 0x1p-102f, 1)) return 1.0f / sqrtf(ms);
+    const float scale = ms < 1.0f ? 0x1p72f : 0x1p-72f;
     a = 0.0f;
 #pragma unroll
     for (int i = 0; i < KEEP; ++i)
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
-            const float t = v[i][q] * 0x1p-72f;
+            const float t = v[i][q] * scale;
             a = fmaf(t, t, a);
         }
     if (N > 64) __syncthreads();
     a = row_sum<N>(a, sh);
-    return 0x1p-72f / sqrtf(a / (float)d + eps * 0x1p-72f * 0x1p-72f);
+    return scale / sqrtf(a / (float)d + eps * scale * scale);
 }
 
 // Eight values as loaded, in as many registers as they have words (dense.h's Eight lets the compiler

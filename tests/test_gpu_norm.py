@@ -208,6 +208,22 @@ def test_a_large_eps():
 
 
 @pytest.mark.gpu
+def test_a_small_eps():
+    """An eps below the normal numbers beside rows whose squares are."""
+    for d in (64, 2048, 16384):
+        for eps in (1e-45, 1e-42, 1e-39, 1.2e-38, 1e-31, 1e-30):
+            for size in (0.0, 1e-23, 1e-22, 1e-20, 3e-16, 1e-15):
+                x = inputs(3, d, F32, "none", std=size)["residual"]
+                w = torch.ones(d, device="cuda")
+                _, normed = B.elb_norm_forward(x, w_pre=w, eps=eps)
+                torch.cuda.synchronize()
+                # (eps as the call takes it, in fp32)
+                within(normed, *R.norm_forward(x, None, None, w, None, 1.0, 1.0,
+                                               float(torch.tensor(eps, dtype=F32)))[1],
+                       label="%g %g" % (size, eps))
+
+
+@pytest.mark.gpu
 def test_a_row_alone_and_what_lies_around():
     """A row's results do not depend on the batch; nothing beside the outputs is written; a NaN or
     an infinity stays in its row."""
