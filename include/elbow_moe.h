@@ -464,9 +464,9 @@ int elb_quantize_f4(const void *x, int64_t rows, int32_t d, int32_t dtype, uint8
  * A projection with 4-bit weights: y_tn = [residual_tn +] sum_i x_ti W_ni, W_ni the value of code
  * (n, i) times its group's scale.
  *   x        [T, k]       dtype
- *   W        [n, k / 2]   uint8, W_scale [n, k / 32] uint8   as elb_quantize_f4 lays them out; scale
- *                         bytes from 2 to 252, or 255, which makes the row's products NaN (others give
- *                         unspecified, but in-bounds, results)
+ *   W        [n, k / 2]   uint8, W_scale [n, k / 32] uint8   as elb_quantize_f4 lays them out, with any
+ *                         scale byte: a zero is one at every scale but 255, which makes the row's products
+ *                         NaN; values of 2^128 and more (bytes 253, 254) make them infinite or NaN
  *   residual [T, n]       dtype   optional (NULL: none)
  *   y        [T, n]       dtype   output; may be residual, shares memory with no other input
  *   workspace             at least elb_linear_f4_workspace_bytes(T, n, k, dtype) bytes (may be 0)

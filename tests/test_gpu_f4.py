@@ -109,6 +109,43 @@ def test_a_group_that_holds_no_number():
             assert bool(y[:, bad].isnan().all()) and not bool(y[:, ~bad].isnan().any())
 
 
+def test_zeros_at_every_scale():
+    """Codes of zero, of either sign, are zeros at every scale byte but 255, streamed and converted:
+    other quantisers give a group of zeros a scale of 0."""
+    n, k = 256, 32
+    q = torch.zeros((n, k // 2), dtype=torch.uint8, device="cuda")
+    q[:] = torch.tensor([0x00, 0x88, 0x08, 0x80] * 4, device="cuda")
+    s = torch.arange(n, device="cuda").to(torch.uint8)[:, None].contiguous()
+    for dtype, tokens in ((BF16, (1, 20, 100, 3000)), (F32, (1, 20, 100, 9000))):
+        for T in tokens:
+            x = normal(gen(T), T, k, std=1e30, dtype=dtype)
+            y = B.elb_linear_f4(x, q, s)
+            torch.cuda.synchronize()
+            assert not bool(y[:, :255].any()) and bool(y[:, 255].isnan().all()), (dtype, T)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_codes_at_the_scales_that_the_quantiser_does_not_write(dtype):
+    """Scale bytes 0, 1, 253 and 254: each code is exact, those from 2^128 on give no number (an infinity,
+    or a NaN: an fp32 x of 1 has parts of zero, and zero times an infinity is one)."""
+    k = 32
+    q = torch.zeros((4, k // 2), dtype=torch.uint8, device="cuda")
+    q[:] = torch.tensor([0x10, 0x32, 0x54, 0x76, 0x98, 0xBA, 0xDC, 0xFE] * 2, device="cuda")
+    s = torch.tensor([0, 1, 253, 254], dtype=torch.uint8, device="cuda")[:, None]
+    # a row for each code alone: zeros at the other places
+    code = torch.stack([q & 15, q >> 4], -1).flatten(-2)
+    alone = (code[:, None, :] * torch.eye(k, dtype=torch.uint8, device="cuda")).flatten(0, 1)
+    W, s = R.pack_f4(alone), s.repeat_interleave(k, 0).contiguous()
+    want = R.from_f4(W, s).sum(-1)
+    number = want.abs() < 2.0 ** 128
+    assert int((~number).sum()) == 2 * 2 * 2 + 4 * 2 * 2  # 4 and 6; 2, 3, 4 and 6, either sign
+    for T in (1, 32, 100, 3000, 9000):
+        y = B.elb_linear_f4(torch.ones((T, k), dtype=dtype, device="cuda"), W, s)
+        torch.cuda.synchronize()
+        assert torch.equal(y.double()[:, number], want[number].expand(T, -1)), T
+        assert not bool(y[:, ~number].isfinite().any()), T
+
+
 SIZES = [(32, 16), (64, 32), (96, 48), (160, 16), (256, 528), (1056, 80), (2048, 1040), (8192, 64)]
 
 
