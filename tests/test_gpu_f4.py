@@ -194,6 +194,30 @@ def test_fp32_tokens_keep_their_bits():
         assert bool(((y - x).abs()[small] <= 2.0 ** -120).all())
 
 
+def test_small_fp32_tokens_are_taken_to_within_2_to_the_minus_124():
+    """The parts of an fp32 x below 2^-100 leave the normal range one after the other, the lowest
+    first; what is lost of x stays below 2^-124 (W has one weight of 1 a row)."""
+    k, n = 256, 256
+    q = torch.zeros((n, k), dtype=torch.uint8, device="cuda")
+    q[torch.arange(n), torch.arange(n)] = 2
+    W, s = R.pack_f4(q), torch.full((n, k // 32), 127, dtype=torch.uint8, device="cuda")
+    g = gen(2)
+    top = 2.0 ** -100
+    edge = [top * (1 - 2.0 ** -24), top * (1 - 2.0 ** -16), top * (1 - 2.0 ** -8)]
+    for e in range(-127, -100):  # mantissas of 24 bits, all ones, and ones in single parts
+        for f in (1 + 2.0 ** -23, 2 - 2.0 ** -23, 1 + 2.0 ** -8, 1 + 2.0 ** -16, 2 - 2.0 ** -7):
+            edge.append(f * 2.0 ** e)
+    edge = torch.tensor(edge, dtype=torch.float64).float().cuda()
+    for T in (1, 20, 64, 300, 9000):
+        x = (1 + torch.rand((T, k), generator=g, device="cuda")) * torch.exp2(
+            torch.randint(-127, -101, (T, k), generator=g, device="cuda").float())
+        x = x * normal(g, T, k).sign()
+        x[0, :edge.numel()] = edge
+        y = B.elb_linear_f4(x, W, s)
+        torch.cuda.synchronize()
+        assert float((y.double() - x.double()).abs().max()) <= 2.0 ** -124, T
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("T", [1, 16, 20, 50, 64, 65, 300])
 def test_block(T, dtype):
