@@ -341,28 +341,13 @@ Counters f4_counters(const F4Plan& p, void* part) {
 }
 
 template <class X, bool PAIR>
-void stream(StreamIn<X> in, const StreamForm& f, hipStream_t s) {
-    constexpr bool F = sizeof(X) == 4;
+hipError_t stream(StreamIn<X> in, const StreamForm& f, hipStream_t s) {
     in.shares = f.shares;
-    const int tile = f.tm * 8 + f.nf;
-    // (those of the type's table; gate and up rows are two fragments at least)
-    if constexpr (!PAIR) {
-        if (tile == 8 * 8 + 1) return run_stream<X, 8, 1, F ? 8 : 16, PAIR>(in, s);
-        if (tile == 16 * 8 + 1) return run_stream<X, 16, 1, F ? 4 : 8, PAIR>(in, s);
-    }
-    if constexpr (F) {
-        if (tile == 8 * 8 + 4) return run_stream<X, 8, 4, 8, PAIR>(in, s);
-    } else {
-        if (tile == 32 * 8 + 4) return run_stream<X, 32, 4, 4, PAIR>(in, s);
-        if (tile == 48 * 8 + 2) return run_stream<X, 48, 2, 4, PAIR>(in, s);
-        if (tile == 48 * 8 + 4) return run_stream<X, 48, 4, 4, PAIR>(in, s);
-    }
-    switch (tile) {
-        case 8 * 8 + 2: return run_stream<X, 8, 2, 8, PAIR>(in, s);
-        case 16 * 8 + 2: return run_stream<X, 16, 2, F ? 4 : 8, PAIR>(in, s);
-        case 16 * 8 + 4: return run_stream<X, 16, 4, F ? 4 : 8, PAIR>(in, s);
-    }
-    if constexpr (!F || !PAIR) return run_stream<X, 32, 2, 4, PAIR>(in, s);
+    const bool known = with_form<sizeof(X) == 4, PAIR>(f, [&](auto t) {
+        typedef decltype(t) Form;
+        run_stream<X, Form::TM, Form::NF, Form::NW, PAIR>(in, s);
+    });
+    return known ? hipGetLastError() : hipErrorInvalidValue;
 }
 
 __global__ __launch_bounds__(256) void clear_f4(Counters c) { clear_counters(c.p, c.n); }
@@ -387,9 +372,8 @@ hipError_t streamed(const F4Plan& p, const void* x, const uint8_t* W, const uint
         ELB_LAUNCH(clear_f4, dim3(1), dim3(256), 0, s, c);
     }
     ProfileScope prof("linear_f4", s);
-    stream<T, false>({(const T*)x, W, W_scale, (const T*)res, (T*)y, T_, n, k, 1, (float*)part, c.p,
-                      {nullptr, 0}}, p.form, s);
-    return hipGetLastError();
+    return stream<T, false>({(const T*)x, W, W_scale, (const T*)res, (T*)y, T_, n, k, 1, (float*)part,
+                             c.p, {nullptr, 0}}, p.form, s);
 }
 
 template <class T>
@@ -411,9 +395,9 @@ hipError_t block(const F4Plan& p, const void* x, const uint8_t* Wgu, const uint8
     if (p.streams) {
         {
             ProfileScope prof("gate_up_f4", s);
-            stream<T, true>({(const T*)x, Wgu, gu_scale, nullptr, (T*)h, T_, m, d, 1, nullptr, nullptr,
-                             f4_counters(p, part)}, p.up, s);
-            if (hipError_t e = hipGetLastError()) return e;
+            if (hipError_t e = stream<T, true>({(const T*)x, Wgu, gu_scale, nullptr, (T*)h, T_, m, d, 1,
+                                                nullptr, nullptr, f4_counters(p, part)}, p.up, s))
+                return e;
         }
         return streamed<T>(p, h, Wd, d_scale, res, T_, d, m, y, part, true, s);
     }

@@ -2,6 +2,8 @@
 // converted for the dense forms.  Usable from host code without HIP (for tests).
 #pragma once
 
+#include <utility>
+
 #include "forms.h"
 
 namespace elb {
@@ -35,6 +37,39 @@ constexpr StreamForm kStreamF32[] = {
     {8, 4, 8, 1, 1.69f, 1.69f, 3.59f, 3.15f},  {16, 1, 4, 1, 1.5f, 1.45f, 1.46f, 3.3f},
     {16, 2, 4, 1, 1.51f, 1.39f, 2.01f, 3.42f}, {16, 4, 4, 1, 1.22f, 1.79f, 2.78f, 3.5f},
     {32, 2, 4, 1, 1.4f, 1.61f, 3.28f, 3.7f}};
+// (gate and up rows are two fragments at least, and of fp32 tokens 32 x 32 tiles are the best for none)
+constexpr bool pair_takes(const StreamForm& f, bool f32) {
+    return f.nf > 1 && !(f32 && f.tm == 32);
+}
+
+// Calls call(Tile<tm, nf, nw>) for a form of the table, so that what is planned is what is launched; false
+// for a form that is not of it (PAIR: or that gate and up rows do not take).
+template <int TM_, int NF_, int NW_>
+struct Tile {
+    static constexpr int TM = TM_, NF = NF_, NW = NW_;
+};
+template <bool F32, bool PAIR, size_t I, class Call>
+bool call_form(const StreamForm& form, Call&& call) {
+    constexpr StreamForm t = (F32 ? kStreamF32 : kStreamBf16)[I];
+    if constexpr (!PAIR || pair_takes(t, F32)) {
+        if (form.tm == t.tm && form.nf == t.nf && form.nw == t.nw) {
+            call(Tile<t.tm, t.nf, t.nw>{});
+            return true;
+        }
+    }
+    return false;
+}
+template <bool F32, bool PAIR, class Call, size_t... I>
+bool with_form(const StreamForm& form, Call&& call, std::index_sequence<I...>) {
+    return (call_form<F32, PAIR, I>(form, call) || ...);
+}
+template <bool F32, bool PAIR, class Call>
+bool with_form(const StreamForm& form, Call&& call) {
+    constexpr size_t n = F32 ? sizeof(kStreamF32) / sizeof(kStreamF32[0])
+                             : sizeof(kStreamBf16) / sizeof(kStreamBf16[0]);
+    return with_form<F32, PAIR>(form, call, std::make_index_sequence<n>{});
+}
+
 inline int stream_tiles(const StreamForm& f, int64_t T, int rows) {
     return (rows + 16 * f.nf - 1) / (16 * f.nf) * (int)((T + f.tm - 1) / f.tm);
 }
@@ -48,10 +83,9 @@ inline StreamForm stream_form(int64_t T, int cols, int k, bool pair, bool f32) {
     float least = 0;
     for (int i = 0; i < n; ++i) {
         const StreamForm& f = table[i];
-        // (where the fits hold; gate and up rows are two fragments at least, and of fp32 tokens 32 x 32 tiles
-        // are the best for none)
+        // (where the fits hold)
         if ((f.tm == 8 && T > 8) || (f.tm == 16 && T > 16 && !f32) || (f.tm > 16 && T <= 16) ||
-            (pair && (f.nf == 1 || (f32 && f.tm == 32))))
+            (pair && !pair_takes(f, f32)))
             continue;
         const int tiles = stream_tiles(f, T, rows);
         for (int z = 1; z <= (pair ? 1 : kMostShares); z *= 2) {

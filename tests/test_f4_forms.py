@@ -98,6 +98,59 @@ def test_scratch_is_within_what_is_reserved(plans):
             least[s[1:]] = p[7]
 
 
+LAUNCH = r'''
+#include <cstdio>
+#include "f4_forms.h"
+template <bool F32, bool PAIR>
+void ask(elb::StreamForm f) {
+    int tm = 0, nf = 0, nw = 0;
+    const bool known = elb::with_form<F32, PAIR>(f, [&](auto t) {
+        tm = decltype(t)::TM, nf = decltype(t)::NF, nw = decltype(t)::NW;
+    });
+    printf("%d %d %d %d %d %d %d %d %d\n", F32, PAIR, f.tm, f.nf, f.nw, known, tm, nf, nw);
+}
+template <bool F32, bool PAIR, size_t N>
+void all(const elb::StreamForm (&table)[N]) {
+    for (elb::StreamForm f : table) {
+        ask<F32, PAIR>(f);
+        f.nw *= 2;
+        ask<F32, PAIR>(f);
+        f.tm = 24;
+        ask<F32, PAIR>(f);
+    }
+}
+int main() {
+    all<false, false>(elb::kStreamBf16);
+    all<false, true>(elb::kStreamBf16);
+    all<true, false>(elb::kStreamF32);
+    all<true, true>(elb::kStreamF32);
+}
+'''
+
+
+def test_what_is_planned_is_what_is_launched(plans):
+    """The launch takes tile and waves from the planned form: each of the table is known with its own, but
+    those that gate and up rows never take; no other is."""
+    with tempfile.TemporaryDirectory() as d:
+        src, exe = os.path.join(d, "t.cpp"), os.path.join(d, "t")
+        open(src, "w").write(LAUNCH)
+        subprocess.check_call(["g++", "-O1", "-std=c++17", "-I", CSRC, src, "-o", exe])
+        out = subprocess.run([exe], check=True, text=True, stdout=subprocess.PIPE).stdout
+    rows = [tuple(map(int, line.split())) for line in out.splitlines()]
+    assert len(rows) == 3 * 2 * (9 + 7)
+    known = set()
+    for i, (f32, pair, tm, nf, nw, found, *got) in enumerate(rows):
+        assert got == ([tm, nf, nw] if found else [0, 0, 0])
+        if i % 3:  # not of the table
+            assert not found
+        elif not pair:
+            assert found
+        if found:
+            known.add((f32, pair, tm, nf))
+    up = {(s[3], 1) + p[1:3] for s, p in zip(BLOCK, plans([s[:3] + (1, s[3]) for s in BLOCK]))}
+    assert {k for k in known if k[1]} == up
+
+
 def made(T, k, f32, seed):
     from paper_2608_04401_amd import binding as B
     g = torch.Generator(device="cuda")
