@@ -1099,7 +1099,7 @@ static FewLayout few_layout(int64_t T, int d, int m, int K) {
     L.w = L.ids + align_up(rows * 4);
     L.part = L.w + align_up(rows * 4);
     L.count = L.part + few_part_bytes(d);
-    L.total = L.count + align_up((size_t)few_tiles(d) * 4);
+    L.total = L.count + align_up(few_count_bytes(d));
     return L;
 }
 

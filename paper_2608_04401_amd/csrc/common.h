@@ -243,9 +243,9 @@ hipError_t launch_linear(const void* x, const void* W, const void* res, int64_t 
                          int dtype, void* part, void* y, hipStream_t s);
 
 // the whole layer for at most ELB_FEW_TOKENS tokens (few.hip); scale pointers null: bf16 experts.
-// h: scratch [T K, m] bf16; part: few_part_bytes(d) of partial sums; count: few_tiles(d) counters
-int few_tiles(int d);
+// h: scratch [T K, m] bf16; part: few_part_bytes(d) of partial sums; count: few_count_bytes(d) of counters
 size_t few_part_bytes(int d);
+size_t few_count_bytes(int d);
 hipError_t launch_moe_few(const void* x, const void* Wr, const void* Wgu, const uint8_t* gu_scale,
                           const void* Wd, const uint8_t* d_scale, const void* res, int64_t T, int d,
                           int N, int m, const elb_route_params& p, void* h, float* part, int* count,

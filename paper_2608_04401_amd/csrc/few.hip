@@ -64,7 +64,7 @@ struct FewIn {
     bf16_t* y;
     int *k, *ids;
     float* w;
-    float* part;  // partial sums of launch 2 [column tiles, shares, 16, columns], and
+    float* part;  // shares > 1: partial sums of launch 2 [column tiles, shares, 16, columns], and
     int* count;   // how many of a column tile's are written (zeroed by launch 1)
     int shares;
 };
@@ -98,7 +98,7 @@ __global__ __launch_bounds__(64 * kUpWaves) void few_up(FewIn in, XTable xt) {
     char* const slot = sm + wave * SLOT;
     const uint32_t lds = lds_address(slot);
 
-    if (blockIdx.x == 0)
+    if (blockIdx.x == 0 && in.shares > 1)
         for (int i = tid; i < d / (16 * kDownFrags); i += 64 * kUpWaves) in.count[i] = 0;
     for (int i = wave; i < XR; i += kUpWaves) rank[i][lane] = 0;
 
@@ -511,6 +511,13 @@ __global__ __launch_bounds__(64 * kDownWaves) void few_down(FewIn in) {
     }
 }
 
+// shares of launch 2's contraction: so many that its blocks fill the compute units
+int few_tiles(int d) { return d / (16 * kDownFrags); }
+int few_shares(int d) {
+    const int n = 256 / few_tiles(d);
+    return n < 1 ? 1 : n > 16 ? 16 : n;
+}
+
 template <class W, int XR, bool DMA>
 void run_up(const FewIn& in, unsigned blocks, hipStream_t s) {
     const XTable xt = make_xtable(in.N);
@@ -538,14 +545,12 @@ hipError_t few(const FewIn& in, int cus, hipStream_t s) {
 
 }  // namespace
 
-// shares of launch 2's contraction: so many that its blocks fill the compute units
-int few_tiles(int d) { return d / (16 * kDownFrags); }
-int few_shares(int d) {
-    const int n = 256 / few_tiles(d);
-    return n < 1 ? 1 : n > 16 ? 16 : n;
+// no share joins another where there is one alone
+size_t few_part_bytes(int d) {
+    const int n = few_shares(d);
+    return n > 1 ? (size_t)n * 16 * d * 4 : 0;
 }
-
-size_t few_part_bytes(int d) { return (size_t)few_shares(d) * 16 * d * 4; }
+size_t few_count_bytes(int d) { return few_shares(d) > 1 ? (size_t)few_tiles(d) * 4 : 0; }
 
 hipError_t launch_moe_few(const void* x, const void* Wr, const void* Wgu, const uint8_t* gu_scale,
                           const void* Wd, const uint8_t* d_scale, const void* res, int64_t T, int d,

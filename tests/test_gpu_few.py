@@ -1,5 +1,7 @@
 """GPU: the whole layer for a few tokens in two launches, experts in bf16 and in 4 bits; and a run of
 norm, layer, norm as a decoder step has it, captured and replayed."""
+import ctypes
+
 import pytest
 import torch
 
@@ -163,6 +165,24 @@ def test_weights_that_are_no_number_stay_with_their_tokens(T, weights):
         bad = call(w, **kw)
         torch.cuda.synchronize()
         assert torch.equal(bad[~on[e]], y[~on[e]]) and bool(bad[on[e]].isnan().all()), (d, N)
+
+
+def test_nothing_behind_the_workspace_is_written():
+    """A workspace of the size asked for, with the product in shares and whole."""
+    for T, d, m, K in ((1, 512, 64, 2), (16, 4160, 64, 2), (3, 8192, 128, 1)):
+        v = layer(T, d, 8, m, "bf16")
+        want = call(v, K=K)
+        nb = B.elb_moe_few_workspace_bytes(T, d, 8, m, K)
+        ws = torch.full((nb + 4096,), 7, dtype=torch.uint8, device="cuda")
+        y = torch.empty_like(want)
+        p = B.RouteParams(K, 1e-8, B.MODE_ELBOW, 0)
+        ptr = lambda t: t.data_ptr()
+        assert B.lib().elb_moe_forward_few(
+            ptr(v["x"]), ptr(v["W_router"]), ptr(v["W_gate_up"]), None, ptr(v["W_down"]), None, None,
+            T, d, 8, m, ctypes.byref(p), ptr(y), ptr(ws), nb, None, None, None,
+            torch.cuda.current_stream().cuda_stream) == 0
+        torch.cuda.synchronize()
+        assert torch.equal(y, want) and bool((ws[nb:] == 7).all())
 
 
 def test_no_tokens():

@@ -222,6 +222,15 @@ def test_workspace_sizes():
             last = n
 
 
+def test_few_token_workspace_without_shares():
+    """Above 4096 columns the down product is not cut into shares: routing and h alone."""
+    f = B.lib().elb_moe_few_workspace_bytes
+    up = lambda n: -(-n // 256) * 256
+    for T, d, m, K in ((1, 8192, 64, 1), (16, 4160, 128, 8), (3, 1 << 20, 64, 2)):
+        assert f(T, d, 8, m, K) == up(T * K * m * 2) + up(T * 4) + 2 * up(T * K * 4)
+    assert f(1, 4096, 8, 64, 1) >= 2 * 16 * 4096 * 4
+
+
 def test_binding_refuses_host_tensors_types_and_shapes():
     z = torch.zeros
     x, u8 = z(4, 64), lambda *s: torch.zeros(s, dtype=torch.uint8)
