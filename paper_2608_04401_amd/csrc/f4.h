@@ -22,7 +22,6 @@ namespace elb {
 namespace {
 
 typedef __bf16 bf16x2v_t __attribute__((ext_vector_type(2)));
-typedef uint32_t u32x2_byte_t __attribute__((ext_vector_type(2), aligned(1)));
 typedef uint32_t u32_byte_t __attribute__((aligned(1)));
 
 // eight 4-bit weights times a power of two
@@ -134,7 +133,6 @@ struct Stream {
     static constexpr int ROWS = 16 * NF;
     static constexpr int BYTES = ROWS * 128 + (W::SCALES ? (ROWS + 31) / 32 * 256 : 0);
     typedef Copier<KC, ROWS, 1, 1, PAIR, DMA> C;
-    static constexpr int N = C::N + (W::SCALES ? (ROWS + 31) / 32 : 0);  // copy instructions
     C copy;
     const uint8_t* scale[(ROWS + 31) / 32];  // of the lane's rows
     int groups;                              // of a row

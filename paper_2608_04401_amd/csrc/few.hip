@@ -77,7 +77,7 @@ __device__ __forceinline__ bf16x8_t as_frag(u32x4_t v) { return __builtin_bit_ca
 // 64 experts of 2048 x 1024, top 8: one token 18.2 us (4 bits 13.4), of which the routing 6.6; 13 tokens in 4
 // bits 34.7, the weights at 4.6 TB/s after it.
 // ------------------------------------------------------------------------------------------
-template <class W, int KMAX, int XR, bool DMA>
+template <class W, int XR, bool DMA>
 __global__ __launch_bounds__(64 * kUpWaves) void few_up(FewIn in, XTable xt) {
     typedef Stream<W, 4, true, DMA, true> B;
     // a wave's LDS: a unit of weights, then its partial tiles; before that RN units of the router, as
@@ -245,8 +245,7 @@ __global__ __launch_bounds__(64 * kUpWaves) void few_up(FewIn in, XTable xt) {
                 k4[i] = sorted[t][4 * sl + i];
                 id[i] = order[t][4 * sl + i];
             }
-            route_sorted_x16<KMAX>(k4, id, N, K, in.eps, in.mode, in.renorm, xt, t, t < T, sk, sids,
-                                   sw);
+            route_sorted_x16(k4, id, N, K, in.eps, in.mode, in.renorm, xt, t, t < T, sk, sids, sw);
         }
     }
     __syncthreads();
@@ -518,23 +517,17 @@ int few_shares(int d) {
     return n < 1 ? 1 : n > 16 ? 16 : n;
 }
 
-template <class W, int XR, bool DMA>
-void run_up(const FewIn& in, unsigned blocks, hipStream_t s) {
-    const XTable xt = make_xtable(in.N);
-    if (in.K <= 8)
-        ELB_LAUNCH((few_up<W, 8, XR, DMA>), dim3(blocks), dim3(64 * kUpWaves), 0, s, in, xt);
-    else
-        ELB_LAUNCH((few_up<W, kLaneMaxK, XR, DMA>), dim3(blocks), dim3(64 * kUpWaves), 0, s, in, xt);
-}
-
 template <class W, bool DMA>
 hipError_t few(const FewIn& in, int cus, hipStream_t s) {
     {
         ProfileScope prof("few_up", s);
         const int most = (in.T * in.K < in.N ? in.T * in.K : in.N) * (in.m / 32);
         const unsigned blocks = most < cus ? most : cus;
-        if (in.T <= 8) run_up<W, 8, DMA>(in, blocks, s);
-        else run_up<W, 16, DMA>(in, blocks, s);
+        const XTable xt = make_xtable(in.N);
+        if (in.T <= 8)
+            ELB_LAUNCH((few_up<W, 8, DMA>), dim3(blocks), dim3(64 * kUpWaves), 0, s, in, xt);
+        else
+            ELB_LAUNCH((few_up<W, 16, DMA>), dim3(blocks), dim3(64 * kUpWaves), 0, s, in, xt);
         if (hipError_t e = hipGetLastError()) return e;
     }
     ProfileScope prof("few_down", s);

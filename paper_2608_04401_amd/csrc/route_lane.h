@@ -451,7 +451,6 @@ __device__ __forceinline__ float row_last(float v) {
 // of the group calls this (valid: the token exists; only valid groups write).
 // lds_hist (optional): a 64-bin LDS histogram to which each selected expert of a valid token
 // adds one (the dispatch's per-group counts).
-template <int KMAX>
 __device__ __forceinline__ void route_sorted_x16(const float (&key)[4], const int (&id)[4], int N,
                                                  int K, float eps, int mode, int renorm,
                                                  const XTable& xt, int64_t t, bool valid,
@@ -593,8 +592,7 @@ __device__ __forceinline__ void route_token_x16(float* row, int N, int K, float 
         key[i] = __int_as_float(ord_flip32((int)(v[i] >> 32)));
         id[i] = NP - 1 - (int)(uint32_t)v[i];
     }
-    route_sorted_x16<KMAX>(key, id, N, K, eps, mode, renorm, xt, t, valid, kout, ids, wout,
-                           lds_hist);
+    route_sorted_x16(key, id, N, K, eps, mode, renorm, xt, t, valid, kout, ids, wout, lds_hist);
 }
 
 // ---- the router's summation order ----
