@@ -414,7 +414,8 @@ typedef struct {
  *   r_post [T], r_pre [T] float  optional outputs (NULL: not written), for elb_norm_backward; r_post
  *                        is written only with w_post, r_pre only with w_pre.  Of a root mean square
  *                        above 2^126 they are subnormal numbers, with digits to 2^-149
- * Apart from sum and residual, outputs share memory with no other tensor.
+ * Apart from sum and residual, outputs share memory with no other tensor.  A call with neither sum nor
+ * normed asks for nothing: it enqueues nothing and writes no r_post either.
  */
 int elb_norm_forward(const elb_norm *op, void *sum, void *normed, float *r_post, float *r_pre,
                      void *stream);

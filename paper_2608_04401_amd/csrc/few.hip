@@ -355,7 +355,7 @@ __global__ __launch_bounds__(64 * kUpWaves) void few_up(FewIn in, XTable xt) {
 // experts' units one behind the other (per expert as often as its tokens fill tiles of eight); its
 // waves take every sixteenth unit.  The last block of a column tile to write its partial sums adds all
 // of them, in the order of the shares; none waits for another.  64 experts of 2048 x 1024, top 8: one
-// token 9.8 us (4 bits 7.5), 13 tokens in 4 bits 16.5 (64 columns and eight waves: 10.2, 8.0, 17.1).
+// token 9.8 us (4 bits 7.3), 13 tokens in 4 bits 16.1 (64 columns and eight waves: 10.2, 8.0, 17.1).
 // ------------------------------------------------------------------------------------------
 template <class W, bool DMA>
 __global__ __launch_bounds__(64 * kDownWaves) void few_down(FewIn in) {
